@@ -33,6 +33,13 @@
  *   etc_refer_kind           arena (Refer), all kinds or one
  *   etc_plan_* queries      host: dimensions, pieces, arena sizes, send and
  *                            chunk layouts, receive counts, pairing, roles
+ * and the operators of a training step that read and write those states, with
+ * results that do not depend on the configuration a rank is in:
+ *   etc_embed, etc_embed_grad      device: lookup in a rank's share of the
+ *                                  vocabulary, and the table's gradient
+ *   etc_dropout, etc_dropout_grad  device: bias, dropout and residual, with a
+ *                                  mask that is a function of seed and place
+ *   etc_adam                       device: an optimizer step over the arenas
  * Moving messages between GPUs is the caller's business (a grouped
  * send/recv or all-to-all-v with the counts from etc_plan_send_layout).
  *
@@ -57,14 +64,15 @@
  *            are laid out in tensor order (role-1 copies last), each starting
  *            at a multiple of 128 elements (the up half of gate/up directly
  *            after gate); element offsets are the same in all four arenas.
- *            Bytes between tensors are never read or written.
+ *            A migration never reads or writes bytes between tensors.
  *   Messages. Message s->d holds four kind sections (param, master, m, v),
  *            each the routed boxes in d's arena order, every box row-major
  *            in full-tensor coordinates and starting at a multiple of 8
  *            elements (zero padded).  A send buffer holds the messages in
  *            target order, each at a multiple of 256 bytes.
  *   Memory.  The caller owns every arena, send buffer, message and output
- *            buffer.  All device pointers must be 256-byte aligned.  On
+ *            buffer.  All device pointers must be 256-byte aligned, those of
+ *            an operator's matrices and ids by their elements only.  On
  *            MI355X a copy whose read and write addresses differ modulo
  *            1 KB runs 2-4 % slower.  With every arena and send-buffer base
  *            a multiple of 1 KB, the layouts above keep the two congruent
@@ -442,6 +450,149 @@ ETC_API int etc_pack_kind(const etc_plan_t* plan, int src_rank, int kind, const 
  * nothing is routed.  Errors as etc_unpack, and INVALID_ARG for a bad kind. */
 ETC_API int etc_unpack_kind(const etc_plan_t* plan, int dst_rank, int kind, const void* const* msg,
                             void* dst_arena, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Operators of a training step
+ *
+ * They work on matrices whose rows are contiguous and `ld` elements apart:
+ * activations have a row per token, tables a row per id.  Sums are taken in
+ * 32 bits and rounded once, to the output's type.  Results depend on the
+ * arguments alone: every sum has a fixed order (no atomics), so the same call
+ * gives the same bits.  Matrices of no elements may have data NULL; a call
+ * without work returns ETC_OK.  An input may overlap an output only where a
+ * call says so.
+ * Errors of all: INVALID_ARG (NULL, a size, type or stride that does not fit),
+ * ALIGN (a pointer not aligned to its elements, an arena or workspace not to
+ * 256 bytes), UNSUPPORTED (more than 2^31 - 1 ids, rows of a table or columns),
+ * HIP. */
+
+enum { ETC_DTYPE_BF16 = 0, ETC_DTYPE_F32 = 1 };
+enum { ETC_IDS_I32 = 0, ETC_IDS_I64 = 1 };
+
+/* rows x cols elements in device memory; element (i, j) at data + i * ld + j.
+ * ld >= cols for an output; an input may repeat rows (ld = 0 .. cols - 1).
+ * `data` NULL stands for an optional matrix that is absent. */
+typedef struct {
+  void* data;
+  int64_t rows, cols, ld;
+  int32_t dtype;           /* ETC_DTYPE_* */
+  int32_t reserved;        /* 0 */
+} etc_matrix;
+
+/* count whole numbers in device memory */
+typedef struct {
+  const void* data;
+  int64_t count;
+  int32_t dtype;           /* ETC_IDS_* */
+  int32_t reserved;        /* 0 */
+} etc_ids;
+
+/* Dropout with a mask that is never stored: element (i, j) of a matrix is
+ * dropped where u < t, with t = floor(65536 p + 1/2) and u the (j mod 8)-th of
+ * the eight 16-bit numbers (low half of each word first) of
+ *   Philox4x32-10(counter = (j / 8, r mod 2^32, r / 2^32, call),
+ *                 key = (seed mod 2^32, seed / 2^32)),   r = row0 + i
+ * (Salmon, Moraes, Dror and Shaw, "Parallel Random Numbers: As Easy as 1, 2,
+ * 3", SC 2011), and else multiplied by 65536 / (65536 - t).  A dropped element
+ * counts as 0 whatever it holds, NaN included; p = 1 drops all.  So a rank
+ * that holds some rows of a batch (row0 = its first) uses the mask that the
+ * whole batch has in any other configuration, and the backward pass finds the
+ * forward's from the same numbers. */
+typedef struct {
+  uint64_t seed;
+  int64_t row0;            /* global number of the matrix's first row, >= 0 */
+  double p;                /* 0 .. 1, taken to the nearest multiple of 2^-16 */
+  uint32_t call;           /* distinguishes the dropouts of one step */
+  uint32_t reserved;       /* 0 */
+} etc_dropout_desc;
+
+/* out[i, :] = drop(scale * table[k_i, :] + pos_table[positions[i], :]) with
+ * k_i = tokens[i] - row0.  An id outside the table (k_i < 0 or >= table rows:
+ * another rank's share of the vocabulary, or padding) contributes nothing, a
+ * position outside pos_table likewise.  table and pos_table are of one type,
+ * out of either; positions and pos_table are both given or both absent, and
+ * positions has the tokens' count.  drop.p = 0: no dropout.  With TP > 1 the
+ * caller adds the ranks' results, and passes pos_table and dropout where they
+ * are to be applied once. */
+typedef struct {
+  etc_ids tokens, positions;
+  etc_matrix table, pos_table, out;
+  etc_dropout_desc drop;
+  int64_t row0;            /* id of the table's first row */
+  double scale;
+} etc_embed_args;
+ETC_API int etc_embed(const etc_embed_args* args, void* stream);
+
+/* The gradient of etc_embed's table (ETC_DTYPE_F32, such as that tensor's part
+ * of a gradient arena in the arenas' layout):
+ *   dtable[r, :] = (accumulate ? dtable[r, :] : 0)
+ *                  + scale * sum of drop'(grad[i, :]) over i with tokens[i] - row0 = r,
+ * where drop' keeps and scales what the lookup's dropout kept.  Without
+ * `accumulate` every row is written, rows of no token with zeros; with it
+ * those are not touched.  The gradient of pos_table is the same with the
+ * positions as ids and scale 1.
+ * The ids are sorted first, then each run of equal ids is summed; ids outside
+ * the table are skipped.  workspace: etc_embed_grad_workspace's bytes, for the
+ * same sizes or larger ones. */
+typedef struct {
+  etc_ids tokens;
+  etc_matrix grad, dtable;
+  etc_dropout_desc drop;
+  int64_t row0;
+  double scale;
+  void* workspace;         /* device, 256-byte aligned */
+  uint64_t workspace_bytes;
+  int32_t accumulate;
+  int32_t reserved;        /* 0 */
+} etc_embed_grad_args;
+ETC_API int etc_embed_grad(const etc_embed_grad_args* args, void* stream);
+ETC_API int etc_embed_grad_workspace(int64_t ntokens, int64_t table_rows, int64_t cols, uint64_t* bytes);
+
+/* A block's epilogue: out = residual + drop(x + bias).  x, bias (one row of
+ * x's columns), residual and out are of one type; bias and residual may be
+ * absent.  out may be x or residual itself (same data and ld). */
+typedef struct {
+  etc_matrix x, bias, residual, out;
+  etc_dropout_desc drop;
+} etc_dropout_args;
+ETC_API int etc_dropout(const etc_dropout_args* args, void* stream);
+
+/* Its backward: dx = drop'(grad), of grad's type (dx may be grad itself), and
+ * dbias (ETC_DTYPE_F32, one row, may be absent)
+ *   = (accumulate ? dbias : 0) + the sum over rows of drop'(grad), unrounded.
+ * The residual's gradient is grad.  workspace: etc_dropout_grad_workspace's
+ * bytes; only read or written with dbias, and may be NULL without. */
+typedef struct {
+  etc_matrix grad, dx, dbias;
+  etc_dropout_desc drop;
+  void* workspace;         /* device, 256-byte aligned */
+  uint64_t workspace_bytes;
+  int32_t accumulate;
+  int32_t reserved;        /* 0 */
+} etc_dropout_grad_args;
+ETC_API int etc_dropout_grad(const etc_dropout_grad_args* args, void* stream);
+ETC_API int etc_dropout_grad_workspace(int64_t rows, int64_t cols, uint64_t* bytes);
+
+/* One step of Adam with decoupled weight decay over elements [first, first +
+ * count) of a rank's four arenas (arena[k]: kind k), in place, with the
+ * gradients of an fp32 arena of the same layout (read only):
+ *   g = grad_scale[0] * grad   (1 if grad_scale is NULL)
+ *   m = beta1 m + (1 - beta1) g       v = beta2 v + (1 - beta2) g^2
+ *   master -= lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ *                 + weight_decay master)
+ *   param = master rounded to bf16, to nearest even
+ * grad_scale is one fp32 number in device memory, such as a clipping factor.
+ * A whole arena is one range; the elements between its tensors, which no
+ * migration reads, are stepped with it. */
+typedef struct {
+  void* arena[4];          /* device, 256-byte aligned */
+  const void* grad;        /* device, 256-byte aligned */
+  const void* grad_scale;  /* device, 4-byte aligned, or NULL */
+  uint64_t first, count;
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;            /* 1 for the first step */
+} etc_adam_args;
+ETC_API int etc_adam(const etc_adam_args* args, void* stream);
 
 /* Text of the calling thread's last error ("" if none).  Valid until the
  * thread's next failing call. */

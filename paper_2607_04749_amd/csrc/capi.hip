@@ -26,6 +26,22 @@ int fail(int code, const std::string& msg) {
   return code;
 }
 
+}  // namespace
+
+namespace etc {
+
+int set_error(int code, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {  // no memory for the text: the code says enough
+  }
+  return code;
+}
+
+}  // namespace etc
+
+namespace {
+
 int hip_fail(hipError_t e, const char* what) {
   return fail(ETC_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }

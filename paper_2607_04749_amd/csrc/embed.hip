@@ -1,0 +1,92 @@
+// embed.hip -- the lookup of a rank's share of the vocabulary, with scaling,
+// positions and dropout in one pass (etc_embed).
+//
+//   out[i, :] = drop(scale * table[id_i - row0, :] + pos_table[position_i, :])
+//
+// HBM bound: it reads the rows that occur and writes one row per token.  A
+// lane moves one block of eight columns.
+#include <hip/hip_runtime.h>
+
+#include "ops.hpp"
+
+namespace etc {
+
+namespace {
+
+constexpr uint32_t kThreads = 256;
+
+template <typename T>
+struct EmbedArgs {
+  Mat<const T> table, pos;  // pos.p NULL: no positions
+  Ids tokens, positions;
+  int64_t row0;
+  uint64_t rows, pos_rows;
+  float scale;
+  Drop drop;
+  BlockGrid grid;
+};
+
+template <typename T, typename O, bool kDrop>
+__global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> out) {
+  const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+  if (at >= a.grid.n) return;
+  uint32_t i, block, width;
+  a.grid.place(at, &i, &block, &width);
+  const uint64_t col = uint64_t(block) * kBlockCols;
+  float v[8] = {};
+  // unsigned: an id below row0 becomes a large row
+  const uint64_t k = uint64_t(a.tokens.at(i)) - uint64_t(a.row0);
+  if (k < a.rows) {
+    load8(a.table.p + int64_t(k) * a.table.ld + col, width, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+  }
+  if (a.pos.p) {
+    const uint64_t q = uint64_t(a.positions.at(i));
+    if (q < a.pos_rows) {
+      float w[8];
+      load8(a.pos.p + int64_t(q) * a.pos.ld + col, width, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+  }
+  if (kDrop) a.drop.apply(i, block, v);
+  store8(out.p + int64_t(i) * out.ld + col, width, v);
+}
+
+template <typename T, typename O>
+hipError_t launch(const etc_embed_args& x, const Drop& drop, hipStream_t stream) {
+  EmbedArgs<T> a{};
+  a.table = {static_cast<const T*>(x.table.data), x.table.ld};
+  a.pos = {static_cast<const T*>(x.pos_table.data), x.pos_table.ld};
+  a.row0 = x.row0;
+  a.rows = uint64_t(x.table.rows);
+  a.pos_rows = uint64_t(x.pos_table.rows);
+  a.scale = float(x.scale);
+  return for_row_runs(x.out.rows, x.out.cols, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+    auto ids = [&](const etc_ids& v) {
+      const bool wide = v.dtype == ETC_IDS_I64;
+      return Ids{v.data ? static_cast<const char*>(v.data) + first * (wide ? 8 : 4) : nullptr, wide};
+    };
+    a.tokens = ids(x.tokens);
+    a.positions = ids(x.positions);
+    a.drop = drop;
+    a.drop.row0 += uint64_t(first);
+    a.grid = grid;
+    const Mat<O> out{static_cast<O*>(x.out.data) + first * x.out.ld, x.out.ld};
+    const dim3 wgs((grid.n + kThreads - 1) / kThreads), block(kThreads);
+    if (drop.limit) hipLaunchKernelGGL((embed_kernel<T, O, true>), wgs, block, 0, stream, a, out);
+    else hipLaunchKernelGGL((embed_kernel<T, O, false>), wgs, block, 0, stream, a, out);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+hipError_t launch_embed(const etc_embed_args& a, const Drop& drop, hipStream_t stream) {
+  const bool t32 = a.table.dtype == ETC_DTYPE_F32, o32 = a.out.dtype == ETC_DTYPE_F32;
+  if (t32) return o32 ? launch<float, float>(a, drop, stream) : launch<float, bf16>(a, drop, stream);
+  return o32 ? launch<bf16, float>(a, drop, stream) : launch<bf16, bf16>(a, drop, stream);
+}
+
+}  // namespace etc

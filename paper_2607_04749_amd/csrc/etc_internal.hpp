@@ -12,6 +12,9 @@
 
 namespace etc {
 
+// Keeps `msg` as the calling thread's last error and returns `code`.
+int set_error(int code, const char* msg) noexcept;
+
 // ---------------------------------------------------------------------------
 // Logical tensors and rank layouts (host)
 // ---------------------------------------------------------------------------

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from operator import index
 
 import numpy as np
@@ -35,6 +36,8 @@ COST_INF = 1 << 50
 MAX_PEERS = 256
 DEFRAG_NONE, DEFRAG_OCCUPANCY, DEFRAG_EFFICIENCY = 0, 1, 2
 ESIZE = (2, 4, 4, 4)
+DTYPE_BF16, DTYPE_F32 = 0, 1
+IDS_I32, IDS_I64 = 0, 1
 
 
 class ModelDesc(ctypes.Structure):
@@ -120,6 +123,11 @@ def _load():
     L.etc_unpack_kind.argtypes = [vp, ctypes.c_int, ctypes.c_int, vp, vp, vp]
     L.etc_plan_message.argtypes = [vp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, i32p]
     L.etc_plan_refer.argtypes = [vp, ctypes.c_int, vp, ctypes.c_int, i32p]
+    for name in ("etc_embed", "etc_embed_grad", "etc_dropout", "etc_dropout_grad", "etc_adam"):
+        getattr(L, name).argtypes = [ctypes.c_char_p, vp]
+    i64 = ctypes.c_int64
+    L.etc_embed_grad_workspace.argtypes = [i64, i64, i64, u64p]
+    L.etc_dropout_grad_workspace.argtypes = [i64, i64, u64p]
     L.etc_last_error.argtypes = []
     L.etc_last_error.restype = ctypes.c_char_p
     if len(hip_runtimes()) > 1:
@@ -490,3 +498,163 @@ def etc_unpack_kind(plan, dst_rank, kind, msgs, dst_arena, stream=None):
     _check(_lib.etc_unpack_kind(plan.handle, dst_rank, kind, m,
                                 _kind_arena(plan, SIDE_DST, dst_rank, kind, dst_arena, "dst_arena"),
                                 _stream(stream)), "etc_unpack_kind")
+
+
+# ---------------------------------------------------------------------------
+# Operators of a training step.  Their arguments are C structs, packed here
+# field by field in the order of include/etc.h.
+
+_MATRIX, _IDS, _DROP = "Pqqqii", "Pqii", "QqdII"
+_NO_MATRIX, _NO_IDS, _NO_DROP = (0, 0, 0, 0, 0, 0), (0, 0, 0, 0), (0, 0, 0.0, 0, 0)
+_EMBED = struct.Struct("@" + 2 * _IDS + 3 * _MATRIX + _DROP + "qd")
+_EMBED_GRAD = struct.Struct("@" + _IDS + 2 * _MATRIX + _DROP + "qdPQii")
+_DROPOUT = struct.Struct("@" + 4 * _MATRIX + _DROP)
+_DROPOUT_GRAD = struct.Struct("@" + 3 * _MATRIX + _DROP + "PQii")
+_ADAM = struct.Struct("@4PPPQQdddddq")
+_MATRIX_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+_IDS_DTYPES = {torch.int32: IDS_I32, torch.int64: IDS_I64}
+
+
+class Dropout:
+    """Dropout of share p, as a function of (seed, call, global row, column):
+    `call` distinguishes the dropouts of one step, row0 is the global number
+    of the matrix's first row.  One object serves any number of calls."""
+
+    def __init__(self, p, seed, call=0, row0=0):
+        seed, call, row0 = index(seed), index(call), index(row0)
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p must lie in 0 .. 1, got {p}")
+        if not (0 <= seed < 1 << 64 and 0 <= call < 1 << 32 and 0 <= row0 < 1 << 63):
+            raise ValueError("seed, call and row0 must fit 64, 32 and 63 bits")
+        self._fields = (seed, row0, float(p), call, 0)
+
+    @property
+    def p(self):
+        return self._fields[2]
+
+
+def _drop(dropout):
+    return _NO_DROP if dropout is None else dropout._fields
+
+
+def _device_of(x, what):
+    """The current device's number; the operator's tensors have to be there."""
+    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} must be a tensor on the current GPU")
+    return x.get_device()
+
+
+def _matrix(x, what, device):
+    """Fields of an etc_matrix: a tensor of two dimensions with contiguous
+    rows, or a contiguous one of any (its last dimension is the row)."""
+    dtype = _MATRIX_DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"{what} must be bfloat16 or float32, not {x.dtype}")
+    if x.get_device() != device:
+        raise ValueError(f"{what} must be a tensor on the current GPU")
+    if x.dim() == 2:
+        rows, cols = x.shape
+        ld, step = x.stride()
+        if step != 1 and cols > 1 and rows:
+            raise ValueError(f"the rows of {what} must be contiguous")
+        return x.data_ptr(), rows, cols, ld if rows > 1 else cols, dtype, 0
+    if x.dim() == 0 or not x.is_contiguous():
+        raise ValueError(f"{what} must have two dimensions or be contiguous")
+    cols = x.shape[-1]
+    return x.data_ptr(), x.numel() // cols if cols else 0, cols, cols, dtype, 0
+
+
+def _ids(x, what, device):
+    dtype = _IDS_DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"{what} must be int32 or int64, not {x.dtype}")
+    if x.get_device() != device or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor on the current GPU")
+    return x.data_ptr(), x.numel(), dtype, 0
+
+
+def _workspace(x, device):
+    if x is None:
+        return 0, 0
+    if x.get_device() != device or not x.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current GPU")
+    return x.data_ptr(), x.numel() * x.element_size()
+
+
+def etc_embed(tokens, table, out, row0=0, scale=1.0, positions=None, pos_table=None, dropout=None, stream=None):
+    """out[i] = drop(scale * table[tokens[i] - row0] + pos_table[positions[i]]);
+    ids outside the table count as zero.  out: [.., table columns], one row
+    per token; dropout: a Dropout."""
+    d = _device_of(out, "out")
+    t = _ids(tokens, "tokens", d)
+    q = _NO_IDS if positions is None else _ids(positions, "positions", d)
+    p = _NO_MATRIX if pos_table is None else _matrix(pos_table, "pos_table", d)
+    _check(_lib.etc_embed(_EMBED.pack(*t, *q, *_matrix(table, "table", d), *p, *_matrix(out, "out", d),
+                                      *_drop(dropout), row0, scale), _stream(stream)), "etc_embed")
+
+
+def etc_embed_grad_bytes(ntokens, table_rows, cols):
+    """Bytes of etc_embed_grad's workspace."""
+    n = ctypes.c_uint64()
+    _check(_lib.etc_embed_grad_workspace(ntokens, table_rows, cols, ctypes.byref(n)), "etc_embed_grad_workspace")
+    return n.value
+
+
+def etc_embed_grad(tokens, grad, dtable, workspace, row0=0, scale=1.0, dropout=None, accumulate=False, stream=None):
+    """dtable (float32) = or += scale * the sum of drop'(grad[i]) over the
+    tokens of each row; dropout: the lookup's."""
+    d = _device_of(dtable, "dtable")
+    _check(_lib.etc_embed_grad(_EMBED_GRAD.pack(*_ids(tokens, "tokens", d), *_matrix(grad, "grad", d),
+                                                *_matrix(dtable, "dtable", d), *_drop(dropout), row0, scale,
+                                                *_workspace(workspace, d), bool(accumulate), 0),
+                               _stream(stream)), "etc_embed_grad")
+
+
+def etc_dropout(x, out, dropout=None, bias=None, residual=None, stream=None):
+    """out = residual + drop(x + bias); out may be x or residual itself."""
+    d = _device_of(out, "out")
+    b = _NO_MATRIX if bias is None else _matrix(bias, "bias", d)
+    r = _NO_MATRIX if residual is None else _matrix(residual, "residual", d)
+    _check(_lib.etc_dropout(_DROPOUT.pack(*_matrix(x, "x", d), *b, *r, *_matrix(out, "out", d), *_drop(dropout)),
+                            _stream(stream)), "etc_dropout")
+
+
+def etc_dropout_grad_bytes(rows, cols):
+    """Bytes of etc_dropout_grad's workspace, needed with dbias."""
+    n = ctypes.c_uint64()
+    _check(_lib.etc_dropout_grad_workspace(rows, cols, ctypes.byref(n)), "etc_dropout_grad_workspace")
+    return n.value
+
+
+def etc_dropout_grad(grad, dx, dropout=None, dbias=None, workspace=None, accumulate=False, stream=None):
+    """dx = drop'(grad) (dx may be grad itself); dbias (float32) = or += its sum over rows."""
+    d = _device_of(dx, "dx")
+    b = _NO_MATRIX if dbias is None else _matrix(dbias, "dbias", d)
+    _check(_lib.etc_dropout_grad(_DROPOUT_GRAD.pack(*_matrix(grad, "grad", d), *_matrix(dx, "dx", d), *b,
+                                                    *_drop(dropout), *_workspace(workspace, d), bool(accumulate), 0),
+                                 _stream(stream)), "etc_dropout_grad")
+
+
+def etc_adam(arenas, grad, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, first=0,
+             count=None, stream=None):
+    """One Adam step over elements [first, first + count) of a rank's four
+    arenas (by default all from `first` on), in place.  grad: an fp32 arena of
+    the same layout; grad_scale: one float32 on the GPU, or None.  Tensors are
+    checked against the range (ValueError if short)."""
+    if len(arenas) != 4:
+        raise ValueError(f"arenas needs 4 arenas, got {len(arenas)}")
+    first = index(first)
+    if count is None and isinstance(arenas[1], int):
+        raise ValueError("count is needed where arenas are pointers")
+    count = arenas[1].numel() * arenas[1].element_size() // 4 - first if count is None else index(count)
+    if first < 0 or count < 0:
+        raise ValueError("first and count must not be negative")
+    end = first + count
+    a = [_buf(arenas[k], end * ESIZE[k], "arenas", k) or 0 for k in range(4)]
+    s = 0
+    if grad_scale is not None:
+        if not isinstance(grad_scale, int) and grad_scale.dtype != torch.float32:
+            raise ValueError("grad_scale must be float32")
+        s = _buf(grad_scale, 4, "grad_scale")
+    _check(_lib.etc_adam(_ADAM.pack(*a, _buf(grad, 4 * end, "grad") or 0, s, first, count, lr, beta1, beta2, eps,
+                                    weight_decay, step), _stream(stream)), "etc_adam")
