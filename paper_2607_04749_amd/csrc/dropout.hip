@@ -120,8 +120,7 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
 }  // namespace
 
 uint64_t dropout_grad_bytes(uint64_t rows, uint64_t cols) {
-  const uint64_t step = grad_step(rows);
-  return (rows + step - 1) / step * cols * sizeof(float);
+  return std::min<uint64_t>((rows + 31) / 32, 2048) * cols * sizeof(float);
 }
 
 hipError_t launch_dropout(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {

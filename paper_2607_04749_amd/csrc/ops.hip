@@ -151,6 +151,8 @@ int etc_embed_grad(const etc_embed_grad_args* a, void* stream) {
   if (a->dtable.dtype != ETC_DTYPE_F32) return fail(ETC_ERR_INVALID_ARG, "dtable must be ETC_DTYPE_F32");
   if (a->reserved != 0) return fail(ETC_ERR_INVALID_ARG, "reserved must be 0");
   if (a->dtable.rows == 0 || a->dtable.cols == 0 || (a->tokens.count == 0 && a->accumulate)) return ETC_OK;
+  if (!etc::embed_grad_fits(uint64_t(a->tokens.count), uint64_t(a->dtable.cols)))
+    return fail(ETC_ERR_UNSUPPORTED, "too many tokens and columns for one call");
   const uint64_t need = etc::embed_grad_sizes(uint64_t(a->tokens.count), uint64_t(a->dtable.rows), uint64_t(a->dtable.cols)).total;
   if ((rc = check_workspace(a->workspace, a->workspace_bytes, need))) return rc;
   return launched(etc::launch_embed_grad(*a, drop, static_cast<hipStream_t>(stream)), "embed_grad");

@@ -143,9 +143,12 @@ hipError_t for_row_runs(int64_t rows, int64_t cols, F launch) {
 
 // The launchers take checked arguments: types, sizes and strides fit.
 struct EmbedGradSizes {
-  uint64_t keys, order, total;  // byte offsets in the workspace, and its length
+  uint64_t keys[2], order[2], counts, parts;  // byte offsets in the workspace
+  uint64_t total;                             // its length
 };
 EmbedGradSizes embed_grad_sizes(uint64_t ntokens, uint64_t rows, uint64_t cols);
+// whether a call's launches are within the 2^32 lanes that a grid may have
+bool embed_grad_fits(uint64_t ntokens, uint64_t cols);
 uint64_t dropout_grad_bytes(uint64_t rows, uint64_t cols);
 
 hipError_t launch_embed(const etc_embed_args& a, const Drop& drop, hipStream_t stream);

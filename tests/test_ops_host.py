@@ -173,6 +173,8 @@ REFUSED = [
     (lambda: embed_grad(dtable=mat(9, 16)), INVALID), (lambda: embed_grad(dtable=mat(9, 16, F32, ld=8)), INVALID),
     (lambda: embed_grad(ws=0), INVALID), (lambda: embed_grad(ws=PTR + 128), ALIGN),
     (lambda: embed_grad(nbytes=8), INVALID), (lambda: embed_grad(reserved=1), INVALID),
+    (lambda: embed_grad(tokens=ids((1 << 31) - 1), grad=mat((1 << 31) - 1, (1 << 31) - 1, ld=0),
+                        dtable=mat(1, (1 << 31) - 1, F32)), UNSUPPORTED),
     (lambda: embed_grad(scale=NAN), INVALID), (lambda: embed_grad(d=drop(p=2.0)), INVALID),
     (lambda: dropout(out=mat(3, 16, F32)), INVALID), (lambda: dropout(out=mat(3, 17)), INVALID),
     (lambda: dropout(bias=mat(2, 16)), INVALID), (lambda: dropout(bias=mat(1, 8)), INVALID),
@@ -231,6 +233,12 @@ def test_workspaces_grow_with_their_sizes():
         got = [etc.etc_dropout_grad_bytes(n, cols) for n in sizes]
         assert got == sorted(got) and got[0] == 0
     assert etc.etc_embed_grad_bytes(8192, 50304, 2048) < 64 << 20
+    rng = np.random.default_rng(2)
+    for ask in (lambda n, c: etc.etc_embed_grad_bytes(n, 9, c), etc.etc_dropout_grad_bytes):
+        for _ in range(2000):
+            n, c = (int(np.exp(rng.random() * np.log(hi))) for hi in (1 << 20, 20000))
+            more = int(np.exp(rng.random() * np.log(1 + n)))
+            assert ask(n, c) <= ask(n + more, c) and ask(n, c) <= ask(n, c + 1) and ask(n, c) <= ask(n, 2 * c)
 
 
 @pytest.mark.parametrize("bad", (dict(p=-0.1), dict(p=1.5), dict(p=NAN), dict(seed=-1), dict(seed=1 << 64),
