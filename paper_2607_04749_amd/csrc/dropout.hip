@@ -25,52 +25,141 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(BlockGrid grid, Drop 
   uint32_t i, block, width;
   grid.place(at, &i, &block, &width);
   const uint64_t col = uint64_t(block) * kBlockCols;
-  float v[8], b[8] = {}, r[8] = {};
-  load8(x.p + int64_t(i) * x.ld + col, width, v);
-  if (bias) load8(bias + col, width, b);
-  if (residual.p) load8(residual.p + int64_t(i) * residual.ld + col, width, r);
+  Raw8<T> rx, rb, rr;
+  rb.zero();
+  rr.zero();
+  rx.load(x.p + int64_t(i) * x.ld + col, width);
+  if (residual.p) rr.load(residual.p + int64_t(i) * residual.ld + col, width);
+  if (bias) rb.load(bias + col, width);
+  float v[8], w[8];
+  rx.widen(v);
+  rb.widen(w);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += b[e];
+  for (int e = 0; e < 8; ++e) v[e] += w[e];
   if (kDrop) drop.apply(i, block, v);
+  rr.widen(w);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += r[e];
+  for (int e = 0; e < 8; ++e) v[e] += w[e];
   store8(out.p + int64_t(i) * out.ld + col, width, v);
 }
 
-// dx, and the sums of a slab of columns over the rows [first, first + step) for the bias.
+// ---------------------------------------------------------------------------
+// Backward with the bias's gradient.  A workgroup takes `step` rows of a slab of
+// `lanes` blocks of columns: a lane keeps its block's sums over the rows that
+// it visits, the workgroup adds its lanes' and writes one row of partial
+// sums, and a second launch adds those up.
+
 struct GradShape {
-  uint32_t rows, cols, step;
+  uint32_t rows, cols;
+  uint32_t lane_bits;  // 1 << lane_bits blocks of columns side by side, the other lanes further rows
+  uint32_t slabs;      // slabs side by side
+  uint32_t step, parts;
+
+  uint32_t down() const { return kThreads >> lane_bits; }  // rows that a workgroup visits at once
 };
+
+constexpr uint32_t kBatch = 2;     // rows in flight per lane
+constexpr uint64_t kWgs = 2048;    // workgroups wanted at most
+constexpr uint32_t kSlab = 64;     // blocks of a slab at most
+
+GradShape grad_shape(uint32_t rows, uint32_t cols) {
+  GradShape g{rows, cols, 0, 0, 0, 0};
+  const uint32_t nb = blocks_per_row(cols);
+  while ((1u << g.lane_bits) < std::min(nb, kSlab)) ++g.lane_bits;
+  g.slabs = (nb + kSlab - 1) / kSlab;
+  const uint64_t least = g.down() * kBatch;  // at least 8
+  g.step = uint32_t(std::min<uint64_t>(INT32_MAX, (uint64_t(rows) * g.slabs + kWgs * least - 1) / (kWgs * least) * least));
+  g.step = std::max(g.step, uint32_t(least));
+  g.parts = (rows + g.step - 1) / g.step;
+  return g;
+}
 
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Drop drop, Mat<const T> grad, Mat<T> dx,
                                                                 float* partial) {
-  const uint64_t col = (uint64_t(blockIdx.y) * kThreads + threadIdx.x) * kBlockCols;
-  if (col >= g.cols) return;
-  const uint32_t width = uint32_t(g.cols - col < kBlockCols ? g.cols - col : kBlockCols);
-  const uint64_t first = uint64_t(blockIdx.x) * g.step, end = first + g.step < g.rows ? first + g.step : g.rows;
+  __shared__ float shared[kThreads][kBlockCols + 1];
+  const uint32_t part = blockIdx.x / g.slabs, across = threadIdx.x & ((1u << g.lane_bits) - 1);
+  const uint32_t block = (blockIdx.x - part * g.slabs) * kSlab + across;
+  const uint64_t col = uint64_t(block) * kBlockCols;
+  const uint32_t width = col >= g.cols ? 0 : uint32_t(g.cols - col < kBlockCols ? g.cols - col : kBlockCols);
+  const uint32_t down = kThreads >> g.lane_bits;
+  const uint32_t end = uint32_t(min(uint64_t(g.rows), (uint64_t(part) + 1) * g.step));
   float sum[8] = {};
-  for (uint64_t i = first; i < end; ++i) {
-    float v[8];
-    load8(grad.p + int64_t(i) * grad.ld + col, width, v);
-    if (kDrop) drop.apply(i, uint32_t(col / kBlockCols), v);
+  if (width) {
+    for (uint64_t i0 = uint64_t(part) * g.step + (threadIdx.x >> g.lane_bits); i0 < end; i0 += down * kBatch) {
+      Raw8<T> raw[kBatch];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += v[e];
-    store8(dx.p + int64_t(i) * dx.ld + col, width, v);
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint64_t i = i0 + b * down;
+        raw[b].load(grad.p + int64_t(i < end ? i : i0) * grad.ld + col, width);
+      }
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint64_t i = i0 + b * down;
+        if (i >= end) break;
+        float v[8];
+        raw[b].widen(v);
+        if (kDrop) drop.apply(i, block, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        store8(dx.p + int64_t(i) * dx.ld + col, width, v);
+      }
+    }
   }
-  if (partial) store8(partial + uint64_t(blockIdx.x) * g.cols + col, width, sum);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) shared[threadIdx.x][e] = sum[e];
+  __syncthreads();
+  // a column's sums lie `1 << lane_bits` lanes apart
+  for (uint32_t c = threadIdx.x; c < (kBlockCols << g.lane_bits); c += kThreads) {
+    float total = 0.0f;
+    for (uint32_t k = 0; k < down; ++k) total += shared[(k << g.lane_bits) + c / kBlockCols][c % kBlockCols];
+    const uint64_t to = uint64_t(blockIdx.x - part * g.slabs) * kSlab * kBlockCols + c;
+    if (to < g.cols) partial[uint64_t(part) * g.cols + to] = total;
+  }
 }
 
-__global__ __launch_bounds__(kThreads) void dbias_kernel(const float* partial, uint32_t n, uint32_t cols, float* dbias,
-                                                         uint32_t accumulate) {
-  const uint32_t col = blockIdx.x * kThreads + threadIdx.x;
-  if (col >= cols) return;
+// dx alone
+template <typename T, bool kDrop>
+__global__ __launch_bounds__(kThreads) void dropout_dx_kernel(BlockGrid grid, Drop drop, Mat<const T> grad, Mat<T> dx) {
+  const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+  if (at >= grid.n) return;
+  uint32_t i, block, width;
+  grid.place(at, &i, &block, &width);
+  const uint64_t col = uint64_t(block) * kBlockCols;
+  Raw8<T> raw;
+  raw.load(grad.p + int64_t(i) * grad.ld + col, width);
+  float v[8];
+  raw.widen(v);
+  if (kDrop) drop.apply(i, block, v);
+  store8(dx.p + int64_t(i) * dx.ld + col, width, v);
+}
+
+constexpr uint32_t kJoinCols = 32, kJoinRows = 32;
+
+__global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float* partial, uint32_t n, uint32_t cols,
+                                                                    float* dbias, uint32_t accumulate) {
+  __shared__ float shared[kJoinRows][kJoinCols + 1];
+  const uint32_t c = threadIdx.x % kJoinCols, r = threadIdx.x / kJoinCols;
+  const uint64_t col = uint64_t(blockIdx.x) * kJoinCols + c;
   float sum = 0.0f;
-  for (uint32_t k = 0; k < n; ++k) sum += partial[uint64_t(k) * cols + col];
+  if (col < cols) {
+    uint32_t k = r;
+    for (; k + 3 * kJoinRows < n; k += 4 * kJoinRows) {
+      float v[4];
+#pragma unroll
+      for (uint32_t b = 0; b < 4; ++b) v[b] = partial[uint64_t(k + b * kJoinRows) * cols + col];
+      sum += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; k < n; k += kJoinRows) sum += partial[uint64_t(k) * cols + col];
+  }
+  shared[r][c] = sum;
+  __syncthreads();
+  if (r != 0 || col >= cols) return;
+  sum = 0.0f;
+#pragma unroll
+  for (uint32_t k = 0; k < kJoinRows; ++k) sum += shared[k][c];
   dbias[col] = (accumulate ? dbias[col] : 0.0f) + sum;
 }
-
-uint32_t grad_step(uint64_t rows) { return uint32_t(std::max<uint64_t>(32, (rows + 2047) / 2048)); }
 
 template <typename T>
 hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {
@@ -94,13 +183,26 @@ hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream
 }
 
 template <typename T>
+hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
+  return for_row_runs(a.grad.rows, a.grad.cols, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+    const Mat<const T> grad{static_cast<const T*>(a.grad.data) + first * a.grad.ld, a.grad.ld};
+    const Mat<T> dx{static_cast<T*>(a.dx.data) + first * a.dx.ld, a.dx.ld};
+    Drop d = drop;
+    d.row0 += uint64_t(first);
+    const dim3 wgs((grid.n + kThreads - 1) / kThreads), block(kThreads);
+    if (drop.limit) hipLaunchKernelGGL((dropout_dx_kernel<T, true>), wgs, block, 0, stream, grid, d, grad, dx);
+    else hipLaunchKernelGGL((dropout_dx_kernel<T, false>), wgs, block, 0, stream, grid, d, grad, dx);
+    return hipGetLastError();
+  });
+}
+
+template <typename T>
 hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
-  const uint32_t rows = uint32_t(a.grad.rows), cols = uint32_t(a.grad.cols);
-  const GradShape g{rows, cols, grad_step(rows)};
-  const uint32_t parts = (rows + g.step - 1) / g.step;
-  float* partial = a.dbias.data ? static_cast<float*>(a.workspace) : nullptr;
-  if (rows) {
-    const dim3 wgs(parts, (blocks_per_row(cols) + kThreads - 1) / kThreads), block(kThreads);
+  if (!a.dbias.data) return launch_dx<T>(a, drop, stream);
+  const GradShape g = grad_shape(uint32_t(a.grad.rows), uint32_t(a.grad.cols));
+  float* partial = static_cast<float*>(a.workspace);
+  if (g.parts) {
+    const dim3 wgs(g.parts * g.slabs), block(kThreads);
     const Mat<const T> grad{static_cast<const T*>(a.grad.data), a.grad.ld};
     const Mat<T> dx{static_cast<T*>(a.dx.data), a.dx.ld};
     if (drop.limit)
@@ -110,17 +212,17 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.dbias.data) {
-    hipLaunchKernelGGL(dbias_kernel, dim3((cols + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, partial, parts,
-                       cols, static_cast<float*>(a.dbias.data), uint32_t(a.accumulate != 0));
-  }
+  hipLaunchKernelGGL(dbias_kernel, dim3((g.cols + kJoinCols - 1) / kJoinCols), dim3(kJoinCols * kJoinRows), 0, stream,
+                     partial, g.parts, g.cols, static_cast<float*>(a.dbias.data), uint32_t(a.accumulate != 0));
   return hipGetLastError();
 }
 
 }  // namespace
 
+// At most rows / 8 parts, and kWgs / slabs of them where steps are longer: it
+// grows with rows and cols, so a workspace serves smaller calls.
 uint64_t dropout_grad_bytes(uint64_t rows, uint64_t cols) {
-  return std::min<uint64_t>((rows + 31) / 32, 2048) * cols * sizeof(float);
+  return std::min((rows + 7) / 8 * cols, kWgs * kSlab * kBlockCols + cols) * sizeof(float);
 }
 
 hipError_t launch_dropout(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {

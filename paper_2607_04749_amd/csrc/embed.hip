@@ -33,23 +33,19 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> 
   uint32_t i, block, width;
   a.grid.place(at, &i, &block, &width);
   const uint64_t col = uint64_t(block) * kBlockCols;
-  float v[8] = {};
   // unsigned: an id below row0 becomes a large row
   const uint64_t k = uint64_t(a.tokens.at(i)) - uint64_t(a.row0);
-  if (k < a.rows) {
-    load8(a.table.p + int64_t(k) * a.table.ld + col, width, v);
+  const uint64_t q = a.pos.p ? uint64_t(a.positions.at(i)) : 0;
+  Raw8<T> word, place;
+  word.zero();
+  place.zero();
+  if (k < a.rows) word.load(a.table.p + int64_t(k) * a.table.ld + col, width);
+  if (q < a.pos_rows) place.load(a.pos.p + int64_t(q) * a.pos.ld + col, width);
+  float v[8], w[8];
+  word.widen(v);
+  place.widen(w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-  }
-  if (a.pos.p) {
-    const uint64_t q = uint64_t(a.positions.at(i));
-    if (q < a.pos_rows) {
-      float w[8];
-      load8(a.pos.p + int64_t(q) * a.pos.ld + col, width, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += w[e];
-    }
-  }
+  for (int e = 0; e < 8; ++e) v[e] = v[e] * a.scale + w[e];
   if (kDrop) a.drop.apply(i, block, v);
   store8(out.p + int64_t(i) * out.ld + col, width, v);
 }
@@ -61,7 +57,7 @@ hipError_t launch(const etc_embed_args& x, const Drop& drop, hipStream_t stream)
   a.pos = {static_cast<const T*>(x.pos_table.data), x.pos_table.ld};
   a.row0 = x.row0;
   a.rows = uint64_t(x.table.rows);
-  a.pos_rows = uint64_t(x.pos_table.rows);
+  a.pos_rows = x.pos_table.data ? uint64_t(x.pos_table.rows) : 0;
   a.scale = float(x.scale);
   return for_row_runs(x.out.rows, x.out.cols, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto ids = [&](const etc_ids& v) {

@@ -210,8 +210,11 @@ struct SumArgs {
 __device__ __forceinline__ void write_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
                                           uint32_t width, const float (&sum)[8]) {
   float* to = out.p + int64_t(row) * out.ld + col;
-  float v[8] = {};
-  if (a.accumulate) load8(to, width, v);
+  Raw8<float> before;
+  before.zero();
+  if (a.accumulate) before.load(to, width);
+  float v[8];
+  before.widen(v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += sum[e] * a.scale;
   store8(to, width, v);
@@ -266,13 +269,13 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   float sum[8] = {};
   for (uint32_t at = lo; at < hi && run < a.rows; at += kBatch) {
     uint32_t key[kBatch], i[kBatch];
-    float v[kBatch][8];
+    Raw8<T> raw[kBatch];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t x = min(at + b, hi - 1);
       key[b] = at + b < hi ? a.keys[x] : kNone;
       i[b] = a.order[x];
-      load8(grad.p + int64_t(i[b]) * grad.ld + col, width, v[b]);
+      raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
@@ -286,9 +289,11 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
         for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
         if (run >= a.rows) break;  // from here on, ids outside the table
       }
-      if (kDrop) a.drop.apply(i[b], block, v[b]);
+      float v[8];
+      raw[b].widen(v);
+      if (kDrop) a.drop.apply(i[b], block, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[b][e];
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }
   }
   if (run >= a.rows) return;
@@ -321,8 +326,10 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   if (width) {
     // part 0 is this chunk's own
     for (uint32_t k = wave; k <= parts; k += kSumWaves) {
+      Raw8<float> part;
+      part.load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width);
       float v[8];
-      load8(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width, v);
+      part.widen(v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }

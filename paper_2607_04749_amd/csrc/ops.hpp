@@ -35,38 +35,63 @@ typedef uint32_t u32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));  // a
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ float widen(bf16 x) { return float(x); }
-__device__ __forceinline__ float widen(float x) { return x; }
+// Eight elements of a row as they are in memory, or the n < 8 that a row's last
+// block has.  Loading and widening are apart, so that a kernel can have several
+// rows' loads in flight: a value that is widened where it is loaded, on one side
+// of a branch on n, is waited for right there.  Loads and stores are 16 bytes
+// wide at any element's address: rows of odd widths start anywhere, and the
+// hardware splits what crosses a line.
+template <typename T>
+struct Raw8;
 
-// Eight elements, or the n < 8 that a row's last block has (the rest read as 0).
-// Loads and stores are 16 bytes wide at any element's address: rows of odd
-// widths start anywhere, and the hardware splits what crosses a line.
-__device__ __forceinline__ void load8(const bf16* p, uint32_t n, float (&v)[8]) {
-  if (n >= 8) {
-    const u32x4_e2 w = *reinterpret_cast<const u32x4_e2*>(p);
+template <>
+struct Raw8<bf16> {
+  u32x4_e2 w;
+  __device__ __forceinline__ void load(const bf16* p, uint32_t n) {
+    if (n >= 8) {
+      w = *reinterpret_cast<const u32x4_e2*>(p);
+    } else {  // elements past the end repeat the last one
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e)
+        w[e] = q[2 * e < n ? 2 * e : n - 1] | uint32_t(q[2 * e + 1 < n ? 2 * e + 1 : n - 1]) << 16;
+    }
+  }
+  __device__ __forceinline__ void zero() { w = 0; }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[2 * e] = __uint_as_float(w[e] << 16);
       v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
     }
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) v[e] = e < n ? widen(p[e]) : 0.0f;
   }
-}
-__device__ __forceinline__ void load8(const float* p, uint32_t n, float (&v)[8]) {
-  if (n >= 8) {
-    const u32x4_e4 a = *reinterpret_cast<const u32x4_e4*>(p), b = *reinterpret_cast<const u32x4_e4*>(p + 4);
+};
+
+template <>
+struct Raw8<float> {
+  u32x4_e4 a, b;
+  __device__ __forceinline__ void load(const float* p, uint32_t n) {
+    if (n >= 8) {
+      a = *reinterpret_cast<const u32x4_e4*>(p);
+      b = *reinterpret_cast<const u32x4_e4*>(p + 4);
+    } else {
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) {
+        a[e] = q[e < n ? e : n - 1];
+        b[e] = q[e + 4 < n ? e + 4 : n - 1];
+      }
+    }
+  }
+  __device__ __forceinline__ void zero() { a = 0, b = 0; }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = __uint_as_float(a[e]);
       v[e + 4] = __uint_as_float(b[e]);
     }
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.0f;
   }
-}
+};
 
 // Rounds to nearest even, once: v holds the whole result in 32 bits.
 __device__ __forceinline__ void store8(bf16* p, uint32_t n, const float (&v)[8]) {
