@@ -18,28 +18,61 @@ namespace {
 
 constexpr uint32_t kThreads = 256;
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
 struct AdamArgs {
   bf16* param;
   float *master, *m, *v;
   const float *grad, *grad_scale;
-  uint64_t n;
+  uint64_t first, end;  // the range
+  uint64_t start;       // of the launch: the first unit's first element
   float beta1, rest1, beta2, rest2;  // rest = 1 - beta, from 64 bits
   float step_size;                   // lr / (1 - beta1^t)
   float root;                        // 1 / (1 - beta2^t)
   float eps, decay;                  // decay = lr * weight_decay
 };
 
+// A lane steps the four elements of one 16-byte unit of the fp32 arenas, as far
+// as they lie in the range.
+constexpr uint32_t kUnit = 4;
+
+__device__ __forceinline__ void adam_step(const AdamArgs& a, float c, float grad, float& w, float& m, float& v) {
+  const float g = grad * c;
+  m = a.beta1 * m + a.rest1 * g;
+  v = a.beta2 * v + a.rest2 * (g * g);
+  w -= a.step_size * m / (sqrtf(v * a.root) + a.eps) + a.decay * w;
+}
+
 __global__ __launch_bounds__(kThreads) void adam_kernel(AdamArgs a) {
+  const uint64_t at = a.start + (uint64_t(blockIdx.x) * kThreads + threadIdx.x) * kUnit;
+  if (at >= a.end) return;
   const float c = a.grad_scale ? *a.grad_scale : 1.0f;
-  for (uint64_t i = uint64_t(blockIdx.x) * kThreads + threadIdx.x; i < a.n; i += uint64_t(gridDim.x) * kThreads) {
-    const float g = a.grad[i] * c, w = a.master[i];
-    const float m = a.beta1 * a.m[i] + a.rest1 * g;
-    const float v = a.beta2 * a.v[i] + a.rest2 * (g * g);
-    const float x = w - (a.step_size * m / (sqrtf(v * a.root) + a.eps) + a.decay * w);
+  if (at >= a.first && at + kUnit <= a.end) {
+    const f32x4 g = *reinterpret_cast<const f32x4*>(a.grad + at);
+    f32x4 w = *reinterpret_cast<const f32x4*>(a.master + at), m = *reinterpret_cast<const f32x4*>(a.m + at),
+          v = *reinterpret_cast<const f32x4*>(a.v + at);
+    bf16x4 p;
+#pragma unroll
+    for (uint32_t e = 0; e < kUnit; ++e) {
+      float we = w[e], me = m[e], ve = v[e];
+      adam_step(a, c, g[e], we, me, ve);
+      w[e] = we, m[e] = me, v[e] = ve;
+    }
+    p = __builtin_convertvector(w, bf16x4);
+    *reinterpret_cast<f32x4*>(a.master + at) = w;
+    *reinterpret_cast<f32x4*>(a.m + at) = m;
+    *reinterpret_cast<f32x4*>(a.v + at) = v;
+    *reinterpret_cast<bf16x4*>(a.param + at) = p;
+    return;
+  }
+  for (uint64_t i = at < a.first ? a.first : at; i < at + kUnit && i < a.end; ++i) {
+    float w = a.master[i], m = a.m[i], v = a.v[i];
+    adam_step(a, c, a.grad[i], w, m, v);
+    a.master[i] = w;
     a.m[i] = m;
     a.v[i] = v;
-    a.master[i] = x;
-    a.param[i] = bf16(x);
+    a.param[i] = bf16(w);
   }
 }
 
@@ -47,13 +80,14 @@ __global__ __launch_bounds__(kThreads) void adam_kernel(AdamArgs a) {
 
 hipError_t launch_adam(const etc_adam_args& x, hipStream_t stream) {
   AdamArgs a{};
-  a.param = static_cast<bf16*>(x.arena[0]) + x.first;
-  a.master = static_cast<float*>(x.arena[1]) + x.first;
-  a.m = static_cast<float*>(x.arena[2]) + x.first;
-  a.v = static_cast<float*>(x.arena[3]) + x.first;
-  a.grad = static_cast<const float*>(x.grad) + x.first;
+  a.param = static_cast<bf16*>(x.arena[0]);
+  a.master = static_cast<float*>(x.arena[1]);
+  a.m = static_cast<float*>(x.arena[2]);
+  a.v = static_cast<float*>(x.arena[3]);
+  a.grad = static_cast<const float*>(x.grad);
   a.grad_scale = static_cast<const float*>(x.grad_scale);
-  a.n = x.count;
+  a.first = x.first;
+  a.end = x.first + x.count;
   a.beta1 = float(x.beta1);
   a.rest1 = float(1.0 - x.beta1);
   a.beta2 = float(x.beta2);
@@ -62,9 +96,14 @@ hipError_t launch_adam(const etc_adam_args& x, hipStream_t stream) {
   a.root = float(1.0 / (1.0 - std::pow(x.beta2, double(x.step))));
   a.eps = float(x.eps);
   a.decay = float(x.lr * x.weight_decay);
-  const uint64_t wgs = std::min<uint64_t>((x.count + kThreads - 1) / kThreads, 65536);
-  hipLaunchKernelGGL(adam_kernel, dim3(uint32_t(wgs)), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  constexpr uint64_t most = uint64_t(1) << 32;  // elements of a launch: 2^30 lanes
+  for (a.start = x.first / kUnit * kUnit; a.start < a.end; a.start += most) {
+    const uint64_t units = (std::min(a.end - a.start, most) + kUnit - 1) / kUnit;
+    hipLaunchKernelGGL(adam_kernel, dim3(uint32_t((units + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace etc

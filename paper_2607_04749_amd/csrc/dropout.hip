@@ -31,12 +31,14 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(BlockGrid grid, Drop 
   rx.load(x.p + int64_t(i) * x.ld + col, width);
   if (residual.p) rr.load(residual.p + int64_t(i) * residual.ld + col, width);
   if (bias) rb.load(bias + col, width);
+  uint32_t bits[4];
+  if (kDrop) drop.bits(i, block, bits);  // while the loads are on their way
   float v[8], w[8];
   rx.widen(v);
   rb.widen(w);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += w[e];
-  if (kDrop) drop.apply(i, block, v);
+  if (kDrop) drop.apply(bits, v);
   rr.widen(w);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += w[e];
@@ -97,9 +99,11 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
         if (i >= end) break;
+        uint32_t bits[4];
+        if (kDrop) drop.bits(i, block, bits);
         float v[8];
         raw[b].widen(v);
-        if (kDrop) drop.apply(i, block, v);
+        if (kDrop) drop.apply(bits, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += v[e];
         store8(dx.p + int64_t(i) * dx.ld + col, width, v);
@@ -128,9 +132,11 @@ __global__ __launch_bounds__(kThreads) void dropout_dx_kernel(BlockGrid grid, Dr
   const uint64_t col = uint64_t(block) * kBlockCols;
   Raw8<T> raw;
   raw.load(grad.p + int64_t(i) * grad.ld + col, width);
+  uint32_t bits[4];
+  if (kDrop) drop.bits(i, block, bits);
   float v[8];
   raw.widen(v);
-  if (kDrop) drop.apply(i, block, v);
+  if (kDrop) drop.apply(bits, v);
   store8(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 

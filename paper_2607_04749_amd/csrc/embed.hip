@@ -41,12 +41,14 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> 
   place.zero();
   if (k < a.rows) word.load(a.table.p + int64_t(k) * a.table.ld + col, width);
   if (q < a.pos_rows) place.load(a.pos.p + int64_t(q) * a.pos.ld + col, width);
+  uint32_t bits[4];
+  if (kDrop) a.drop.bits(i, block, bits);  // while the loads are on their way
   float v[8], w[8];
   word.widen(v);
   place.widen(w);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = v[e] * a.scale + w[e];
-  if (kDrop) a.drop.apply(i, block, v);
+  if (kDrop) a.drop.apply(bits, v);
   store8(out.p + int64_t(i) * out.ld + col, width, v);
 }
 

@@ -289,9 +289,11 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
         for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
         if (run >= a.rows) break;  // from here on, ids outside the table
       }
+      uint32_t bits[4];
+      if (kDrop) a.drop.bits(i[b], block, bits);
       float v[8];
       raw[b].widen(v);
-      if (kDrop) a.drop.apply(i[b], block, v);
+      if (kDrop) a.drop.apply(bits, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }

@@ -11,12 +11,21 @@
 
 namespace etc {
 
+// a ^ b ^ c, in one instruction where there is one
+__host__ __device__ inline uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+#else
+  return a ^ b ^ c;
+#endif
+}
+
 __host__ __device__ inline void philox4x32_10(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int round = 0; round < 10; ++round) {
     const uint64_t a = uint64_t(0xD2511F53u) * c[0], b = uint64_t(0xCD9E8D57u) * c[2];
-    c[0] = uint32_t(b >> 32) ^ c[1] ^ k0;
-    c[2] = uint32_t(a >> 32) ^ c[3] ^ k1;
+    c[0] = xor3(uint32_t(b >> 32), c[1], k0);
+    c[2] = xor3(uint32_t(a >> 32), c[3], k1);
     c[1] = uint32_t(b);
     c[3] = uint32_t(a);
     k0 += 0x9E3779B9u;
@@ -40,15 +49,14 @@ struct Drop {
     w[3] = call;
     philox4x32_10(w, k0, k1);
   }
-  // v scaled where kept and 0 where dropped, whatever it is (a product with 0 would keep NaN)
-  __device__ __forceinline__ void apply(uint64_t i, uint32_t block, float (&v)[8]) const {
-    uint32_t w[4];
-    bits(i, block, w);
+  // v scaled where kept and 0 where dropped, whatever it is (a product with 0
+  // would keep NaN); limit >= 1.  A number is in the upper half of a word for the
+  // comparison: below the limit where the word is at most (limit << 16) - 1,
+  // which for 65536 is any word, whatever the lower half holds.
+  __device__ __forceinline__ void apply(const uint32_t (&w)[4], float (&v)[8]) const {
+    const uint32_t top = (limit << 16) - 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t u = e % 2 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu;
-      v[e] = u < limit ? 0.0f : v[e] * scale;
-    }
+    for (int e = 0; e < 8; ++e) v[e] = (e % 2 ? w[e / 2] : w[e / 2] << 16) > top ? v[e] * scale : 0.0f;
   }
 };
 
