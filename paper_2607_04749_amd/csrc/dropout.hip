@@ -28,8 +28,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(BlockGrid grid, Drop 
   Raw8<T> rx, rb, rr;
   rb.zero();
   rr.zero();
-  rx.load(x.p + int64_t(i) * x.ld + col, width);
-  if (residual.p) rr.load(residual.p + int64_t(i) * residual.ld + col, width);
+  rx.template load<true>(x.p + int64_t(i) * x.ld + col, width);
+  if (residual.p) rr.template load<true>(residual.p + int64_t(i) * residual.ld + col, width);
   if (bias) rb.load(bias + col, width);
   uint32_t bits[4];
   if (kDrop) drop.bits(i, block, bits);  // while the loads are on their way
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(BlockGrid grid, Drop 
   rr.widen(w);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += w[e];
-  store8(out.p + int64_t(i) * out.ld + col, width, v);
+  store8<true>(out.p + int64_t(i) * out.ld + col, width, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
         if (kDrop) drop.apply(bits, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += v[e];
-        store8(dx.p + int64_t(i) * dx.ld + col, width, v);
+        store8<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
       }
     }
   }
@@ -131,13 +131,13 @@ __global__ __launch_bounds__(kThreads) void dropout_dx_kernel(BlockGrid grid, Dr
   grid.place(at, &i, &block, &width);
   const uint64_t col = uint64_t(block) * kBlockCols;
   Raw8<T> raw;
-  raw.load(grad.p + int64_t(i) * grad.ld + col, width);
+  raw.template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
   uint32_t bits[4];
   if (kDrop) drop.bits(i, block, bits);
   float v[8];
   raw.widen(v);
   if (kDrop) drop.apply(bits, v);
-  store8(dx.p + int64_t(i) * dx.ld + col, width, v);
+  store8<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 
 constexpr uint32_t kJoinCols = 32, kJoinRows = 32;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float
 
 template <typename T>
 hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {
-  return for_row_runs(a.x.rows, a.x.cols, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+  return for_row_runs(a.x.rows, a.x.cols, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto at = [&](const etc_matrix& m) {
       return Mat<T>{m.data ? static_cast<T*>(m.data) + first * m.ld : nullptr, m.ld};
     };
@@ -178,19 +178,19 @@ hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream
     Drop d = drop;
     d.row0 += uint64_t(first);
     const dim3 wgs((grid.n + kThreads - 1) / kThreads), block(kThreads);
-    if (drop.limit)
-      hipLaunchKernelGGL((dropout_kernel<T, true>), wgs, block, 0, stream, grid, d, Mat<const T>{x.p, x.ld}, bias,
-                         Mat<const T>{r.p, r.ld}, out);
-    else
-      hipLaunchKernelGGL((dropout_kernel<T, false>), wgs, block, 0, stream, grid, d, Mat<const T>{x.p, x.ld}, bias,
-                         Mat<const T>{r.p, r.ld}, out);
+#define ETC_DROPOUT(...)                                                                                          \
+  hipLaunchKernelGGL((dropout_kernel<T, __VA_ARGS__>), wgs, block, 0, stream, grid, d, Mat<const T>{x.p, x.ld}, bias, \
+                     Mat<const T>{r.p, r.ld}, out)
+    if (drop.limit) ETC_DROPOUT(true);
+    else ETC_DROPOUT(false);
+#undef ETC_DROPOUT
     return hipGetLastError();
   });
 }
 
 template <typename T>
 hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
-  return for_row_runs(a.grad.rows, a.grad.cols, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+  return for_row_runs(a.grad.rows, a.grad.cols, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     const Mat<const T> grad{static_cast<const T*>(a.grad.data) + first * a.grad.ld, a.grad.ld};
     const Mat<T> dx{static_cast<T*>(a.dx.data) + first * a.dx.ld, a.dx.ld};
     Drop d = drop;

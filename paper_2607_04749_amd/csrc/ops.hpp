@@ -40,16 +40,20 @@ typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // rows' loads in flight: a value that is widened where it is loaded, on one side
 // of a branch on n, is waited for right there.  Loads and stores are 16 bytes
 // wide at any element's address: rows of odd widths start anywhere, and the
-// hardware splits what crosses a line.
+// hardware splits what crosses a line.  kStream: non-temporal, for what is not
+// used again by this launch.
 template <typename T>
 struct Raw8;
 
 template <>
 struct Raw8<bf16> {
   u32x4_e2 w;
+  template <bool kStream = false>
   __device__ __forceinline__ void load(const bf16* p, uint32_t n) {
     if (n >= 8) {
-      w = *reinterpret_cast<const u32x4_e2*>(p);
+      const auto* q = reinterpret_cast<const u32x4_e2*>(p);
+      if constexpr (kStream) w = __builtin_nontemporal_load(q);
+      else w = *q;
     } else {  // elements past the end repeat the last one
       const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
@@ -70,10 +74,12 @@ struct Raw8<bf16> {
 template <>
 struct Raw8<float> {
   u32x4_e4 a, b;
+  template <bool kStream = false>
   __device__ __forceinline__ void load(const float* p, uint32_t n) {
     if (n >= 8) {
-      a = *reinterpret_cast<const u32x4_e4*>(p);
-      b = *reinterpret_cast<const u32x4_e4*>(p + 4);
+      const auto *q = reinterpret_cast<const u32x4_e4*>(p), *r = reinterpret_cast<const u32x4_e4*>(p + 4);
+      if constexpr (kStream) a = __builtin_nontemporal_load(q), b = __builtin_nontemporal_load(r);
+      else a = *q, b = *r;
     } else {
       const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
 #pragma unroll
@@ -94,19 +100,23 @@ struct Raw8<float> {
 };
 
 // Rounds to nearest even, once: v holds the whole result in 32 bits.
+template <bool kStream = false>
 __device__ __forceinline__ void store8(bf16* p, uint32_t n, const float (&v)[8]) {
   if (n >= 8) {
     u32x4_e2 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
-    *reinterpret_cast<u32x4_e2*>(p) = w;
+    auto* q = reinterpret_cast<u32x4_e2*>(p);
+    if constexpr (kStream) __builtin_nontemporal_store(w, q);
+    else *q = w;
   } else {
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e)
       if (e < n) p[e] = bf16(v[e]);
   }
 }
+template <bool kStream = false>
 __device__ __forceinline__ void store8(float* p, uint32_t n, const float (&v)[8]) {
   if (n >= 8) {
     u32x4_e4 a, b;
@@ -115,8 +125,9 @@ __device__ __forceinline__ void store8(float* p, uint32_t n, const float (&v)[8]
       a[e] = __float_as_uint(v[e]);
       b[e] = __float_as_uint(v[e + 4]);
     }
-    *reinterpret_cast<u32x4_e4*>(p) = a;
-    *reinterpret_cast<u32x4_e4*>(p + 4) = b;
+    auto *q = reinterpret_cast<u32x4_e4*>(p), *r = reinterpret_cast<u32x4_e4*>(p + 4);
+    if constexpr (kStream) __builtin_nontemporal_store(a, q), __builtin_nontemporal_store(b, r);
+    else *q = a, *r = b;
   } else {
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e)
@@ -136,31 +147,31 @@ struct Divisor {
   __host__ __device__ uint32_t div(uint32_t n) const { return uint32_t((((uint64_t(n) * m) >> 32) + n) >> s); }
 };
 
-// An elementwise launch: one lane per eight-column block of a matrix, blocks
-// numbered row by row.
+inline uint32_t blocks_per_row(int64_t cols) { return uint32_t((cols + kBlockCols - 1) / kBlockCols); }
+
+// An elementwise launch: a lane has one eight-column block of `per` consecutive
+// rows.  Lanes are numbered along the row, then down the groups of rows.
 struct BlockGrid {
-  uint32_t n;      // blocks in this launch, < 2^31
-  uint32_t cols;
+  uint32_t n;  // lanes with work, < 2^31
+  uint32_t rows, cols;
   Divisor per_row;
-  // block `at`: its row, its number in the row, and how many columns it has
-  __device__ __forceinline__ void place(uint32_t at, uint32_t* row, uint32_t* block, uint32_t* width) const {
-    *row = per_row.div(at);
-    *block = at - *row * per_row.d;
+  // lane `at`: its group of rows, its block's number in the row, and how many columns that has
+  __device__ __forceinline__ void place(uint32_t at, uint32_t* group, uint32_t* block, uint32_t* width) const {
+    *group = per_row.div(at);
+    *block = at - *group * per_row.d;
     const uint32_t left = cols - *block * kBlockCols;
     *width = left < kBlockCols ? left : kBlockCols;
   }
 };
 
-inline uint32_t blocks_per_row(int64_t cols) { return uint32_t((cols + kBlockCols - 1) / kBlockCols); }
-
-// Calls launch(first row, grid) for runs of rows of fewer than 2^31 blocks, until one fails.
+// Calls launch(first row, grid) for runs of rows of fewer than 2^31 lanes, until one fails.
 template <typename F>
-hipError_t for_row_runs(int64_t rows, int64_t cols, F launch) {
+hipError_t for_row_runs(int64_t rows, int64_t cols, uint32_t per, F launch) {
   const uint32_t nb = blocks_per_row(cols);
-  const int64_t most = INT32_MAX / int64_t(nb);
+  const int64_t most = INT32_MAX / int64_t(nb) * per;
   for (int64_t at = 0; at < rows; at += most) {
     const int64_t n = rows - at < most ? rows - at : most;
-    const hipError_t e = launch(at, BlockGrid{uint32_t(n) * nb, uint32_t(cols), Divisor(nb)});
+    const hipError_t e = launch(at, BlockGrid{uint32_t((n + per - 1) / per) * nb, uint32_t(n), uint32_t(cols), Divisor(nb)});
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -74,15 +74,17 @@ def test_division(host):
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1000, 8), (1, (1 << 31) - 1), ((1 << 31) - 1, 8), ((1 << 31) - 1, 4097),
                                        (3, (1 << 31) - 1)])
-def test_launches_cover_the_rows(host, rows, cols):
-    nb = -(-cols // 8)
-    most, at = (2 ** 31 - 1) // nb, 0
-    lines = host("runs", rows, cols).splitlines()
-    for line in lines:
-        first, n, c, d = map(int, line.split())
-        assert first == at and c == cols and d == nb and n % nb == 0 and 0 < n < 2 ** 31
-        at += n // nb
-    assert at == rows and len(lines) == -(-rows // most)
+@pytest.mark.parametrize("per", (1, 2))
+def test_launches_cover_the_rows(host, rows, cols, per):
+    nb, at = -(-cols // 8), 0
+    for line in host("runs", rows, cols, per).splitlines():
+        first, n, run, c, d = map(int, line.split())
+        assert first == at and c == cols and d == nb
+        assert n == -(-run // per) * nb and 0 < n < 2 ** 31
+        at += run
+        # only the last run ends inside a lane's rows or leaves room for more
+        assert at == rows or (run % per == 0 and n + nb >= 2 ** 31)
+    assert at == rows
 
 
 def test_layout(host):
