@@ -3,13 +3,15 @@
 //
 //   dtable[r, :] (+)= scale * sum over i with id_i - row0 = r of drop'(grad[i, :])
 //
-// The tokens are put in the order (row, token): few by counting who comes
-// before whom, many by a radix sort.  The ordered list is then cut into chunks
-// of equal length, whatever the runs of equal rows are, so that a frequent id
-// keeps no wavefront longer than a rare one: a wavefront sums one chunk over
-// 512 columns and writes the rows whose runs lie inside it.  The parts of a
-// run that crosses chunks go to the workspace and are joined afterwards.  All
-// sums are in 32 bits and in a fixed order.
+// Few tokens: one launch.  The first token of each row finds the others in the
+// list and sums them.
+// Many: the tokens are put in the order (row, token) by sorting tiles and merging
+// them.  The ordered list is cut into chunks of equal length, whatever the runs
+// of equal rows are, so that a frequent id keeps no wavefront longer than a rare
+// one: a wavefront sums one chunk over 512 columns and writes the rows whose
+// runs lie inside it.  The parts of a run that crosses chunks go to the
+// workspace and are joined afterwards.
+// All sums are in 32 bits and in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -45,148 +47,103 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // ---------------------------------------------------------------------------
-// Order, few tokens: a token's place is the number of tokens before it, smaller
-// keys and equal ones of earlier tokens.  A workgroup places 64 tokens; its 16
-// wavefronts share the keys that they are compared with, 64 at a time.
+// Order.  A token's place in a sorted list is the number of tokens before it:
+// smaller keys, and equal ones of earlier tokens.  A tile's are found by
+// comparing each with all; then, level by level, runs of sorted tokens become one, a
+// token's place being its own in its run plus what a binary search finds
+// before it in each of the other runs.  No counters, so no order of arrival.
 
-constexpr uint32_t kRankWaves = 16;
+constexpr uint32_t kTile = 256;
+constexpr uint32_t kTileWaves = kTile / kWave;
 
-__global__ __launch_bounds__(kRankWaves* kWave) void rank_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
-  __shared__ __attribute__((aligned(16))) uint32_t other[kRankWaves][kWave];
-  __shared__ uint32_t count[kRankWaves][kWave];
-  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, mine = blockIdx.x;
-  const uint32_t i = mine * kWave + lane, blocks = (t.n + kWave - 1) / kWave;
-  const uint32_t key = i < t.n ? t.key(i) : 0;
+__global__ __launch_bounds__(kTile) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
+  __shared__ __attribute__((aligned(16))) uint32_t all[kTile];
+  const uint32_t lane = threadIdx.x % kWave, mine = threadIdx.x / kWave;
+  const uint32_t first = blockIdx.x * kTile, i = first + threadIdx.x;
+  const uint32_t key = i < t.n ? t.key(i) : kNone;
+  all[threadIdx.x] = key;
+  __syncthreads();
   uint32_t place = 0;
-  for (uint32_t b = wave; b < blocks; b += kRankWaves) {
-    const uint32_t j = b * kWave + lane;
-    other[wave][lane] = j < t.n ? t.key(j) : kNone;
-    wave_sync();
-    const uint32_t below = key + (b < mine);  // equal keys of earlier blocks come before
-    if (b != mine) {
+  for (uint32_t w = 0; w < kTileWaves; ++w) {
+    if (w != mine) {
+      const uint32_t below = key + (w < mine);  // equal keys of earlier wavefronts come before
 #pragma unroll
-      for (uint32_t e = 0; e < kWave; ++e) place += other[wave][e] < below;
+      for (uint32_t e = 0; e < kWave; ++e) place += all[w * kWave + e] < below;
     } else {
 #pragma unroll
-      for (uint32_t e = 0; e < kWave; ++e) place += other[wave][e] < key + (e < lane);
+      for (uint32_t e = 0; e < kWave; ++e) place += all[w * kWave + e] < key + (e < lane);
     }
+  }
+  if (i < t.n) {
+    keys[first + place] = key;
+    order[first + place] = i;
+  }
+}
+
+constexpr uint32_t kMergeRuns = 64;   // runs that become one
+constexpr uint32_t kMergeWaves = 16;  // a workgroup places 64 tokens; its wavefronts share the runs
+constexpr uint32_t kMergeEach = kMergeRuns / kMergeWaves;
+
+// How many of keys[0 .. n) are below `key`; n <= length, a power of two.
+__device__ __forceinline__ uint32_t count_below(const uint32_t* keys, uint32_t n, uint32_t length, uint32_t key) {
+  uint32_t at = 0;
+  for (uint32_t step = length; step; step /= 2) {
+    const uint32_t to = at + step;
+    if (to <= n && keys[to - 1] < key) at = to;
+  }
+  return at;
+}
+
+// kTiles: the runs are tiles, which fit into LDS.
+template <bool kTiles>
+__global__ __launch_bounds__(kMergeWaves* kWave) void merge_kernel(uint32_t n, uint32_t length, const uint32_t* keys,
+                                                                   const uint32_t* order, uint32_t* to_keys,
+                                                                   uint32_t* to_order) {
+  __shared__ uint32_t staged[kTiles ? kMergeWaves : 1][kMergeEach][kTiles ? kTile : 1];
+  __shared__ uint32_t count[kMergeWaves][kWave];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t from = blockIdx.x * kWave, i = from + lane;  // one run's: lengths are multiples of 64
+  const uint32_t run = from / length, group = run / kMergeRuns * kMergeRuns;
+  const uint32_t key = i < n ? keys[i] : 0;
+  uint32_t first[kMergeEach], size[kMergeEach];
+#pragma unroll
+  for (uint32_t k = 0; k < kMergeEach; ++k) {
+    const uint64_t start = uint64_t(group + wave + k * kMergeWaves) * length;
+    first[k] = uint32_t(start < n ? start : 0);
+    size[k] = start < n ? min(length, n - uint32_t(start)) : 0;
+  }
+  if constexpr (kTiles) {
+    uint32_t v[kMergeEach][kTile / kWave];
+#pragma unroll
+    for (uint32_t k = 0; k < kMergeEach; ++k)
+#pragma unroll
+      for (uint32_t e = 0; e < kTile / kWave; ++e) {
+        const uint32_t x = e * kWave + lane;
+        v[k][e] = x < size[k] ? keys[first[k] + x] : kNone;
+      }
+#pragma unroll
+    for (uint32_t k = 0; k < kMergeEach; ++k)
+#pragma unroll
+      for (uint32_t e = 0; e < kTile / kWave; ++e) staged[wave][k][e * kWave + lane] = v[k][e];
     wave_sync();
+  }
+  uint32_t place = 0;
+#pragma unroll
+  for (uint32_t k = 0; k < kMergeEach; ++k) {
+    const uint32_t other = group + wave + k * kMergeWaves;
+    const uint32_t* list = kTiles ? staged[wave][k] : keys + first[k];
+    if (other == run) place += i - run * length;
+    else place += count_below(list, size[k], length, key + (other < run));  // equal keys of earlier runs come before
   }
   count[wave][lane] = place;
   __syncthreads();
-  if (wave == 0 && i < t.n) {
+  if (wave == 0 && i < n) {
     place = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < kRankWaves; ++w) place += count[w][lane];
-    keys[place] = key;
-    order[place] = i;
-  }
-}
-
-// ---------------------------------------------------------------------------
-// Order, many tokens: a radix sort from the low digits up, each pass stable.
-// A pass counts the digits of every tile (one workgroup each), and then every
-// tile moves its keys: to the keys of smaller digits, and of its own digit in
-// earlier tiles, it adds the rank inside the tile.
-
-constexpr uint32_t kSortThreads = 256;
-constexpr uint32_t kSortWaves = kSortThreads / kWave;
-constexpr uint32_t kMaxDigitBits = 9;
-constexpr uint32_t kMaxTiles = 64;  // every tile sums the counts of all
-
-struct SortPass {
-  uint32_t tile;   // keys per tile, a multiple of kSortThreads
-  uint32_t tiles;  // at most kMaxTiles
-  uint32_t shift, bits;
-  const uint32_t *keys, *order;  // keys NULL: the first pass, from the ids
-  __device__ __forceinline__ uint32_t digit(uint32_t key) const { return (key >> shift) & ((1u << bits) - 1); }
-};
-
-__global__ __launch_bounds__(kSortThreads) void digit_kernel(Tokens t, SortPass p, uint32_t* counts) {
-  __shared__ uint32_t count[1 << kMaxDigitBits];
-  const uint32_t bins = 1u << p.bits;
-  for (uint32_t d = threadIdx.x; d < bins; d += kSortThreads) count[d] = 0;
-  __syncthreads();
-  const uint32_t end = min(t.n, (blockIdx.x + 1) * p.tile);
-  for (uint32_t i = blockIdx.x * p.tile + threadIdx.x; i < end; i += kSortThreads)
-    atomicAdd(&count[p.digit(p.keys ? p.keys[i] : t.key(i))], 1u);
-  __syncthreads();
-  for (uint32_t d = threadIdx.x; d < bins; d += kSortThreads) counts[blockIdx.x * bins + d] = count[d];
-}
-
-__global__ __launch_bounds__(kSortThreads) void move_kernel(Tokens t, SortPass p, const uint32_t* counts,
-                                                            uint32_t* keys, uint32_t* order) {
-  __shared__ uint32_t at[kSortWaves][1 << kMaxDigitBits];  // where each wavefront's next key of a digit goes
-  __shared__ uint32_t sums[kSortWaves];
-  const uint32_t bins = 1u << p.bits, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (uint32_t d = threadIdx.x; d < bins; d += kSortThreads)
-#pragma unroll
-    for (uint32_t w = 0; w < kSortWaves; ++w) at[w][d] = 0;
-  __syncthreads();
-  // each wavefront has a quarter of the tile, so earlier wavefronts' keys come first
-  const uint32_t quarter = p.tile / kSortWaves, first = blockIdx.x * p.tile + wave * quarter;
-  const uint32_t end = min(t.n, first + quarter);
-  for (uint32_t i = first + lane; i < end; i += kWave)
-    atomicAdd(&at[wave][p.digit(p.keys ? p.keys[i] : t.key(i))], 1u);
-  __syncthreads();
-  // starts: digits in order (two per thread at most), then tiles, then wavefronts
-  uint32_t total[2] = {}, before[2] = {};
-#pragma unroll
-  for (uint32_t h = 0; h < 2; ++h) {
-    const uint32_t d = threadIdx.x * 2 + h;
-    if (d < bins)
-      for (uint32_t b = 0; b < p.tiles; ++b) {
-        const uint32_t c = counts[b * bins + d];
-        total[h] += c;
-        before[h] += b < blockIdx.x ? c : 0;
-      }
-  }
-  uint32_t scan = total[0] + total[1];
-#pragma unroll
-  for (uint32_t step = 1; step < kWave; step *= 2) {
-    const uint32_t v = __shfl_up(scan, step);
-    if (lane >= step) scan += v;
-  }
-  if (lane == kWave - 1) sums[wave] = scan;
-  __syncthreads();
-  uint32_t base = scan - total[0] - total[1];
-  for (uint32_t w = 0; w < wave; ++w) base += sums[w];
-#pragma unroll
-  for (uint32_t h = 0; h < 2; ++h) {
-    const uint32_t d = threadIdx.x * 2 + h;
-    if (d < bins) {
-      uint32_t to = base + before[h];
-#pragma unroll
-      for (uint32_t w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = at[w][d];
-        at[w][d] = to;
-        to += c;
-      }
-    }
-    base += total[h];
-  }
-  __syncthreads();
-  for (uint32_t i0 = first; i0 < end; i0 += kWave) {  // the same for all lanes of a wavefront
-    const uint32_t i = i0 + lane;
-    const bool has = i < end;
-    const uint32_t key = has ? (p.keys ? p.keys[i] : t.key(i)) : 0, d = p.digit(key);
-    // the lanes of the same digit
-    uint64_t same = __ballot(has);
-    for (uint32_t b = 0; b < p.bits; ++b) {
-      const bool one = (d >> b) & 1;
-      const uint64_t ones = __ballot(one);
-      same &= one ? ones : ~ones;
-    }
-    const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1)));
-    uint32_t to = 0;
-    if (has) to = at[wave][d] + rank;
-    wave_sync();
-    if (has && rank == 0) at[wave][d] = to + uint32_t(__popcll(same));
-    wave_sync();
-    if (has) {
-      keys[to] = key;
-      order[to] = p.keys ? p.order[i] : i;
-    }
+    for (uint32_t w = 0; w < kMergeWaves; ++w) place += count[w][lane];
+    const uint32_t to = group * length + place;
+    to_keys[to] = key;
+    to_order[to] = order[i];
   }
 }
 
@@ -207,17 +164,20 @@ struct SumArgs {
   Drop drop;
 };
 
-__device__ __forceinline__ void write_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
-                                          uint32_t width, const float (&sum)[8]) {
-  float* to = out.p + int64_t(row) * out.ld + col;
-  Raw8<float> before;
-  before.zero();
-  if (a.accumulate) before.load(to, width);
+// A row of the table that a run ends in: what it holds, read early, and then the whole of it.
+__device__ __forceinline__ void finish_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
+                                           uint32_t width, const float (&sum)[8], const Raw8<float>& before) {
   float v[8];
   before.widen(v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += sum[e] * a.scale;
-  store8(to, width, v);
+  store8<true>(out.p + int64_t(row) * out.ld + col, width, v);
+}
+
+__device__ __forceinline__ void read_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
+                                         uint32_t width, Raw8<float>& before) {
+  if (a.accumulate) before.load(out.p + int64_t(row) * out.ld + col, width);
+  else before.zero();
 }
 
 // The first place whose key is at least `key`, found by all lanes of a wavefront together, 64 places at a time.
@@ -235,16 +195,20 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n
   return lo;
 }
 
+__device__ __forceinline__ void zero_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint32_t lane) {
+  const float zero[8] = {};
+  for (uint64_t col = lane * kBlockCols; col < a.cols; col += kWave * kBlockCols)
+    store8<true>(out.p + int64_t(row) * out.ld + col, uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols),
+                 zero);
+}
+
 // Zeros in the rows of no token, a wavefront per row.
 __device__ __forceinline__ void fill_rows(const SumArgs& a, const Mat<float>& out) {
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t waves = (gridDim.x - a.sum_wgs) * kSumWaves;
   for (uint32_t r = (blockIdx.x - a.sum_wgs) * kSumWaves + threadIdx.x / kWave; r < a.rows; r += waves) {
     const uint32_t at = lower_bound(a.keys, a.n, r, lane);
-    if (at < a.n && a.keys[at] == r) continue;
-    const float zero[8] = {};
-    for (uint64_t col = lane * kBlockCols; col < a.cols; col += kWave * kBlockCols)
-      store8(out.p + int64_t(r) * out.ld + col, uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols), zero);
+    if (at == a.n || a.keys[at] != r) zero_row(a, out, r, lane);
   }
 }
 
@@ -258,50 +222,59 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   const uint32_t job = __builtin_amdgcn_readfirstlane(blockIdx.x * kSumWaves + threadIdx.x / kWave);
   const uint32_t chunk = job / a.slabs;
   if (chunk >= a.chunks) return;
+  // the chunk's keys and tokens, one per lane
+  const uint32_t lo = chunk * a.chunk, size = min(a.chunk, a.n - lo);
+  const uint32_t key = lane < size ? a.keys[lo + lane] : kNone, token = lane < size ? a.order[lo + lane] : 0;
+  const uint32_t prev = lo > 0 ? a.keys[lo - 1] : kNone, next = lo + size < a.n ? a.keys[lo + size] : kNone;
+  const uint32_t inside = uint32_t(__popcll(__ballot(key < a.rows)));  // the others come last
+  if (inside == 0) return;
+  const uint32_t after = __shfl_down(key, 1);
+  const uint64_t ends = __ballot(lane < inside && (lane + 1 == size ? next : after) != key);
+  // the run that began in an earlier chunk: its end here goes to the parts, not to the table
+  uint32_t came = __builtin_amdgcn_readfirstlane(key) == prev ? (ends ? uint32_t(__builtin_ctzll(ends)) : inside) : kNone;
+
   const uint32_t block = (job - chunk * a.slabs) * kWave + lane;
   const uint64_t col = uint64_t(block) * kBlockCols;
-  if (col >= a.cols) return;
-  const uint32_t width = uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
-  const uint32_t lo = chunk * a.chunk, hi = min(a.n, lo + a.chunk);
-  uint32_t run = a.keys[lo];
-  bool came = lo > 0 && a.keys[lo - 1] == run;  // the run began in an earlier chunk
+  const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
   float* parts = a.parts + uint64_t(chunk) * 2 * a.cols + col;
   float sum[8] = {};
-  for (uint32_t at = lo; at < hi && run < a.rows; at += kBatch) {
-    uint32_t key[kBatch], i[kBatch];
+  for (uint32_t e0 = 0; e0 < inside; e0 += kBatch) {
+    uint32_t i[kBatch], row[kBatch];
     Raw8<T> raw[kBatch];
+    Raw8<float> before[kBatch];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
-      const uint32_t x = min(at + b, hi - 1);
-      key[b] = at + b < hi ? a.keys[x] : kNone;
-      i[b] = a.order[x];
-      raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
+      const uint32_t e = min(e0 + b, inside - 1);
+      i[b] = __builtin_amdgcn_readlane(token, e);
+      row[b] = __builtin_amdgcn_readlane(key, e);
+      if (width) raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
     }
 #pragma unroll
-    for (uint32_t b = 0; b < kBatch; ++b) {
-      if (key[b] == kNone) break;
-      if (key[b] != run) {
-        if (came) store8(parts, width, sum);
-        else write_row(a, out, run, col, width, sum);
-        came = false;
-        run = key[b];
+    for (uint32_t b = 0; b < kBatch; ++b)
+      if (width && e0 + b < inside && (ends >> (e0 + b) & 1) && e0 + b != came) read_row(a, out, row[b], col, width, before[b]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
-        if (run >= a.rows) break;  // from here on, ids outside the table
-      }
+    for (uint32_t b = 0; b < kBatch; ++b) {
+      const uint32_t e = e0 + b;
+      if (e >= inside) break;
       uint32_t bits[4];
       if (kDrop) a.drop.bits(i[b], block, bits);
       float v[8];
       raw[b].widen(v);
       if (kDrop) a.drop.apply(bits, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      for (int x = 0; x < 8; ++x) sum[x] += v[x];
+      if (ends >> e & 1) {
+        if (width) {
+          if (e == came) store8(parts, width, sum);
+          else finish_row(a, out, row[b], col, width, sum, before[b]);
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum[x] = 0.0f;
+      }
     }
   }
-  if (run >= a.rows) return;
-  if (came) store8(parts, width, sum);
-  else if (hi < a.n && a.keys[hi] == run) store8(parts + a.cols, width, sum);
-  else write_row(a, out, run, col, width, sum);
+  // a run that goes on: part 0 where it fills the chunk and came in, else part 1
+  if (!(ends >> (inside - 1) & 1) && width) store8(parts + (came == inside ? 0 : a.cols), width, sum);
 }
 
 // Joins the parts of the run that begins in this chunk and goes on in the next
@@ -327,34 +300,130 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   float sum[8] = {};
   if (width) {
     // part 0 is this chunk's own
-    for (uint32_t k = wave; k <= parts; k += kSumWaves) {
-      Raw8<float> part;
-      part.load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width);
-      float v[8];
-      part.widen(v);
+    for (uint32_t k0 = wave; k0 <= parts; k0 += kSumWaves * kBatch) {
+      Raw8<float> part[kBatch];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint32_t k = min(k0 + b * kSumWaves, parts);
+        part[b].load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width);
+      }
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        if (k0 + b * kSumWaves > parts) break;
+        float v[8];
+        part[b].widen(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      }
     }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) shared[wave][lane][e] = sum[e];
   __syncthreads();
   if (wave != 0 || !width) return;
+  Raw8<float> before;
+  read_row(a, out, run, col, width, before);
 #pragma unroll
   for (uint32_t w = 1; w < kSumWaves; ++w)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += shared[w][lane][e];
-  write_row(a, out, run, col, width, sum);
+  finish_row(a, out, run, col, width, sum, before);
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens, in one launch: a workgroup per token and slab, each lane with one
+// token's key.  The first token of a row adds up all of the row's, every
+// wavefront those among its 64 tokens.  Further workgroups write the rows of no
+// token, kFillRows each.
+
+constexpr uint32_t kFewMost = kSumThreads;  // a token per lane
+constexpr uint32_t kFillRows = 16;
+
+template <typename T, bool kDrop>
+__global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, Mat<const T> grad, Mat<float> out) {
+  __shared__ uint64_t masks[kSumWaves];
+  __shared__ float shared[kSumWaves][kWave][8];
+  __shared__ uint32_t seen[kFillRows];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t key = threadIdx.x < t.n ? t.key(threadIdx.x) : kNone;
+  if (blockIdx.x >= a.sum_wgs) {
+    for (uint64_t first = uint64_t(blockIdx.x - a.sum_wgs) * kFillRows; first < a.rows;
+         first += uint64_t(gridDim.x - a.sum_wgs) * kFillRows) {
+      if (threadIdx.x < kFillRows) seen[threadIdx.x] = 0;
+      __syncthreads();
+      if (key < a.rows && key >= first && key - first < kFillRows) seen[key - first] = 1;
+      __syncthreads();
+      for (uint32_t r = wave; r < kFillRows && first + r < a.rows; r += kSumWaves)
+        if (!seen[r]) zero_row(a, out, uint32_t(first) + r, lane);
+      __syncthreads();
+    }
+    return;
+  }
+  const uint32_t mine = blockIdx.x / a.slabs, row = t.key(mine);
+  if (row >= a.rows) return;
+  const uint64_t same = __ballot(key == row);
+  if (lane == 0) masks[wave] = same;
+  __syncthreads();
+  uint32_t holders = 0;  // wavefronts with tokens of the row
+#pragma unroll
+  for (uint32_t w = 0; w < kSumWaves; ++w) {
+    const uint64_t m = masks[w];
+    if (w * kWave <= mine && (mine - w * kWave >= kWave ? m : m & ((uint64_t(1) << (mine - w * kWave)) - 1))) return;
+    holders += m != 0;
+  }
+  const uint32_t block = (blockIdx.x - mine * a.slabs) * kWave + lane;
+  const uint64_t col = uint64_t(block) * kBlockCols;
+  const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
+  const bool last = masks[wave] != 0 && wave == mine / kWave;  // the wavefront of the first token finishes the row
+  Raw8<float> before;
+  before.zero();
+  if (width && last) read_row(a, out, row, col, width, before);
+  float sum[8] = {};
+  uint64_t left = same;
+  while (left) {
+    const uint32_t most = uint32_t(__popcll(left));
+    uint32_t i[kBatch];
+    Raw8<T> raw[kBatch];
+#pragma unroll
+    for (uint32_t b = 0; b < kBatch; ++b) {
+      if (left) {
+        i[b] = wave * kWave + uint32_t(__builtin_ctzll(left));
+        left &= left - 1;
+      } else {
+        i[b] = b ? i[b - 1] : 0;
+      }
+      if (width) raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
+    }
+#pragma unroll
+    for (uint32_t b = 0; b < kBatch; ++b) {
+      if (b >= most) break;
+      uint32_t bits[4];
+      if (kDrop) a.drop.bits(i[b], block, bits);
+      float v[8];
+      raw[b].widen(v);
+      if (kDrop) a.drop.apply(bits, v);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) sum[x] += v[x];
+    }
+  }
+  if (holders > 1) {  // the same for the whole workgroup
+#pragma unroll
+    for (int x = 0; x < 8; ++x) shared[wave][lane][x] = sum[x];
+    __syncthreads();
+    if (last)
+      for (uint32_t w = wave + 1; w < kSumWaves; ++w)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum[x] += shared[w][lane][x];
+  }
+  if (last && width) finish_row(a, out, row, col, width, sum, before);
 }
 
 // ---------------------------------------------------------------------------
 
-constexpr uint32_t kRankMost = 8192;  // tokens that are ordered by counting
-
 uint32_t slabs_of(uint64_t cols) { return uint32_t((cols + kWave * kBlockCols - 1) / (kWave * kBlockCols)); }
 
-// Tokens per chunk: at most kJobs wavefronts in all, but 4 to 128 tokens each.
-constexpr uint64_t kJobs = 4096, kChunkLeast = 4, kChunkMost = 128;
+// Tokens per chunk: at most kJobs wavefronts in all, but 4 to 64 (one per lane) tokens each.
+constexpr uint64_t kJobs = 4096, kChunkLeast = 4, kChunkMost = kWave;
 
 uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
@@ -372,32 +441,19 @@ uint64_t part_cols(uint64_t n, uint64_t cols) {
 hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, const uint32_t** keys,
                        const uint32_t** order, hipStream_t stream) {
   auto at = [&](uint64_t byte) { return reinterpret_cast<uint32_t*>(work + byte); };
-  *keys = at(w.keys[0]);
-  *order = at(w.order[0]);
-  if (t.n <= kRankMost) {
-    hipLaunchKernelGGL(rank_kernel, dim3((t.n + kWave - 1) / kWave), dim3(kRankWaves * kWave), 0, stream, t,
-                       at(w.keys[0]), at(w.order[0]));
-    return hipGetLastError();
-  }
-  uint32_t bits = 1;
-  while (bits < 32 && t.rows >> bits) ++bits;  // of the largest key, `rows`
-  const uint32_t passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
-  SortPass p{};
-  p.tile = (t.n + kMaxTiles - 1) / kMaxTiles;
-  p.tile = std::max(1024u, (p.tile + kSortThreads - 1) / kSortThreads * kSortThreads);
-  p.tiles = (t.n + p.tile - 1) / p.tile;
-  for (uint32_t k = 0; k < passes; ++k) {
-    p.shift = bits * k / passes;
-    p.bits = bits * (k + 1) / passes - p.shift;
-    uint32_t *to_keys = at(w.keys[k % 2]), *to_order = at(w.order[k % 2]);
-    hipLaunchKernelGGL(digit_kernel, dim3(p.tiles), dim3(kSortThreads), 0, stream, t, p, at(w.counts));
-    hipLaunchKernelGGL(move_kernel, dim3(p.tiles), dim3(kSortThreads), 0, stream, t, p, at(w.counts), to_keys, to_order);
+  hipLaunchKernelGGL(tile_kernel, dim3((t.n + kTile - 1) / kTile), dim3(kTile), 0, stream, t, at(w.keys[0]), at(w.order[0]));
+  uint32_t in = 0;  // the pair of lists that holds the runs
+  for (uint64_t length = kTile; length < t.n; length *= kMergeRuns, in ^= 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    *keys = p.keys = to_keys;
-    *order = p.order = to_order;
+    const dim3 wgs((t.n + kWave - 1) / kWave), block(kMergeWaves * kWave);
+    auto merge = length == kTile ? merge_kernel<true> : merge_kernel<false>;
+    hipLaunchKernelGGL(merge, wgs, block, 0, stream, t.n, uint32_t(length), at(w.keys[in]), at(w.order[in]),
+                       at(w.keys[in ^ 1]), at(w.order[in ^ 1]));
   }
-  return hipSuccess;
+  *keys = at(w.keys[in]);
+  *order = at(w.order[in]);
+  return hipGetLastError();
 }
 
 template <typename T>
@@ -405,30 +461,35 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   const uint32_t n = uint32_t(x.tokens.count), rows = uint32_t(x.dtable.rows), cols = uint32_t(x.dtable.cols);
   const EmbedGradSizes w = embed_grad_sizes(n, rows, cols);
   char* work = static_cast<char*>(x.workspace);
+  const Tokens t{Ids{x.tokens.data, x.tokens.dtype == ETC_IDS_I64}, x.row0, rows, n};
+  const Mat<const T> grad{static_cast<const T*>(x.grad.data), x.grad.ld};
+  const Mat<float> out{static_cast<float*>(x.dtable.data), x.dtable.ld};
+  const dim3 block(kSumThreads);
   SumArgs a{};
-  if (n) {
-    const Tokens t{Ids{x.tokens.data, x.tokens.dtype == ETC_IDS_I64}, x.row0, rows, n};
-    const hipError_t e = sort_tokens(t, work, w, &a.keys, &a.order, stream);
-    if (e != hipSuccess) return e;
-  }
-  a.parts = reinterpret_cast<float*>(work + w.parts);
   a.n = n;
   a.rows = rows;
   a.cols = cols;
   a.accumulate = x.accumulate != 0;
-  a.chunk = chunk_of(n, cols);
-  a.chunks = (n + a.chunk - 1) / a.chunk;
   a.slabs = slabs_of(cols);
-  a.sum_wgs = uint32_t((uint64_t(a.chunks) * a.slabs + kSumWaves - 1) / kSumWaves);
   a.scale = float(x.scale);
   a.drop = drop;
-  const Mat<const T> grad{static_cast<const T*>(x.grad.data), x.grad.ld};
-  const Mat<float> out{static_cast<float*>(x.dtable.data), x.dtable.ld};
-  const uint32_t fill_wgs = a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20);
-  const dim3 wgs(a.sum_wgs + fill_wgs), block(kSumThreads);
+  if (n <= kFewMost) {
+    a.sum_wgs = n * a.slabs;
+    const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kFillRows - 1) / kFillRows, 1u << 20)));
+    if (drop.limit) hipLaunchKernelGGL((few_kernel<T, true>), wgs, block, 0, stream, t, a, grad, out);
+    else hipLaunchKernelGGL((few_kernel<T, false>), wgs, block, 0, stream, t, a, grad, out);
+    return hipGetLastError();
+  }
+  const hipError_t e = sort_tokens(t, work, w, &a.keys, &a.order, stream);
+  if (e != hipSuccess) return e;
+  a.parts = reinterpret_cast<float*>(work + w.parts);
+  a.chunk = chunk_of(n, cols);
+  a.chunks = (n + a.chunk - 1) / a.chunk;
+  a.sum_wgs = uint32_t((uint64_t(a.chunks) * a.slabs + kSumWaves - 1) / kSumWaves);
+  const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20)));
   if (drop.limit) hipLaunchKernelGGL((sum_kernel<T, true>), wgs, block, 0, stream, a, grad, out);
   else hipLaunchKernelGGL((sum_kernel<T, false>), wgs, block, 0, stream, a, grad, out);
-  if (a.chunks > 1) hipLaunchKernelGGL(join_kernel, dim3((a.chunks - 1) * a.slabs), block, 0, stream, a, out);
+  hipLaunchKernelGGL(join_kernel, dim3((a.chunks - 1) * a.slabs), block, 0, stream, a, out);
   return hipGetLastError();
 }
 
@@ -441,20 +502,17 @@ EmbedGradSizes embed_grad_sizes(uint64_t n, uint64_t, uint64_t cols) {
     w.total += (bytes + 255) / 256 * 256;
     return at;
   };
-  w.keys[0] = take(4 * n);
-  w.order[0] = take(4 * n);
-  if (n > kRankMost) {
-    w.keys[1] = take(4 * n);
-    w.order[1] = take(4 * n);
-    w.counts = take((uint64_t(4) << kMaxDigitBits) * kMaxTiles);
+  for (int k = 0; k < 2; ++k) {
+    w.keys[k] = take(4 * n);
+    w.order[k] = take(4 * n);
   }
   w.parts = take(part_cols(n, cols) * 2 * sizeof(float));
   return w;
 }
 
 bool embed_grad_fits(uint64_t n, uint64_t cols) {
-  // a workgroup per chunk and slab in the largest launch, of kSumThreads each
-  return up(n, chunk_of(n, cols)) * slabs_of(cols) <= (uint64_t(1) << 32) / kSumThreads / 2;
+  // a workgroup per chunk (or token) and slab in the largest launch, of kSumThreads each
+  return (n <= kFewMost ? n : up(n, chunk_of(n, cols))) * slabs_of(cols) <= (uint64_t(1) << 32) / kSumThreads / 2;
 }
 
 hipError_t launch_embed_grad(const etc_embed_grad_args& a, const Drop& drop, hipStream_t stream) {

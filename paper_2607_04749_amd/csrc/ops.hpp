@@ -179,7 +179,7 @@ hipError_t for_row_runs(int64_t rows, int64_t cols, uint32_t per, F launch) {
 
 // The launchers take checked arguments: types, sizes and strides fit.
 struct EmbedGradSizes {
-  uint64_t keys[2], order[2], counts, parts;  // byte offsets in the workspace
+  uint64_t keys[2], order[2], parts;  // byte offsets in the workspace
   uint64_t total;                             // its length
 };
 EmbedGradSizes embed_grad_sizes(uint64_t ntokens, uint64_t rows, uint64_t cols);

@@ -76,12 +76,11 @@ def embed(ids, table, row0=0, scale=1.0, positions=None, pos_table=None, drop=No
 def embed_grad(ids, grad, before, row0=0, scale=1.0, drop=None, accumulate=False):
     g, _, _ = _drop(grad.astype(np.float64), drop)
     d, size, count = np.zeros(before.shape), np.zeros(before.shape), np.zeros(before.shape[0])
-    for i, v in enumerate(ids):
-        k = int(v) - row0
-        if 0 <= k < before.shape[0]:
-            d[k] += g[i]
-            size[k] += np.abs(g[i])
-            count[k] += 1
+    k = np.asarray(ids, np.int64) - row0
+    held = (k >= 0) & (k < before.shape[0])
+    np.add.at(d, k[held], g[held])
+    np.add.at(size, k[held], np.abs(g[held]))
+    np.add.at(count, k[held], 1)
     d *= scale
     size *= abs(scale)
     out = d + before if accumulate else d

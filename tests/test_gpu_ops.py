@@ -195,6 +195,18 @@ GRAD = [
     (20011, 8, 140000, 140000, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (33000, 12, 9, 9, 0, 0.0, "f32", "int64", "same", 0, 0),
     (50, 9000, 40, 40, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    # around the sizes where the way of ordering changes
+    (255, 40, 33, 33, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (256, 1032, 17, 17, 0, 0.0, "f32", "int32", "log", 0, 0),
+    (256, 24, 5, 5, 0, 0.0, "bf16", "int64", "same", 0, 0),
+    (257, 40, 33, 33, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (511, 24, 5000, 5000, 0, 0.0, "bf16", "int64", "distinct", 0, 0),
+    (16384, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (16385, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (40000, 9, 50000, 50000, 0, 0.1, "f32", "int32", "distinct", 0, 0),
+    # three levels of merging
+    (1100003, 3, 60000, 50000, 100, 0.0, "f32", "int64", "log", 0, 0),
+    (1048577, 1, 3, 3, 0, 0.0, "f32", "int64", "log", 0, 0),
 ]
 
 
