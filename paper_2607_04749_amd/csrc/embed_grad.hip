@@ -54,27 +54,33 @@ __device__ __forceinline__ void wave_sync() {
 // before it in each of the other runs.  No counters, so no order of arrival.
 
 constexpr uint32_t kTile = 256;
-constexpr uint32_t kTileWaves = kTile / kWave;
+constexpr uint32_t kTileParts = kTile / kWave;  // a token's keys to compare with are shared by so many lanes
+constexpr uint32_t kTileThreads = kTile * kTileParts;
 
-__global__ __launch_bounds__(kTile) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
+__global__ __launch_bounds__(kTileThreads) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
   __shared__ __attribute__((aligned(16))) uint32_t all[kTile];
-  const uint32_t lane = threadIdx.x % kWave, mine = threadIdx.x / kWave;
-  const uint32_t first = blockIdx.x * kTile, i = first + threadIdx.x;
+  __shared__ uint32_t count[kTileParts][kTile];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t mine = wave % kTileParts, part = wave / kTileParts;  // 64 tokens of the tile, against 64 keys of it
+  const uint32_t first = blockIdx.x * kTile, x = mine * kWave + lane, i = first + x;
   const uint32_t key = i < t.n ? t.key(i) : kNone;
-  all[threadIdx.x] = key;
+  if (part == 0) all[x] = key;
   __syncthreads();
   uint32_t place = 0;
-  for (uint32_t w = 0; w < kTileWaves; ++w) {
-    if (w != mine) {
-      const uint32_t below = key + (w < mine);  // equal keys of earlier wavefronts come before
+  if (part != mine) {
+    const uint32_t below = key + (part < mine);  // equal keys of earlier wavefronts come before
 #pragma unroll
-      for (uint32_t e = 0; e < kWave; ++e) place += all[w * kWave + e] < below;
-    } else {
+    for (uint32_t e = 0; e < kWave; ++e) place += all[part * kWave + e] < below;
+  } else {
 #pragma unroll
-      for (uint32_t e = 0; e < kWave; ++e) place += all[w * kWave + e] < key + (e < lane);
-    }
+    for (uint32_t e = 0; e < kWave; ++e) place += all[part * kWave + e] < key + (e < lane);
   }
-  if (i < t.n) {
+  count[part][x] = place;
+  __syncthreads();
+  if (part == 0 && i < t.n) {
+    place = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kTileParts; ++w) place += count[w][x];
     keys[first + place] = key;
     order[first + place] = i;
   }
@@ -83,16 +89,6 @@ __global__ __launch_bounds__(kTile) void tile_kernel(Tokens t, uint32_t* keys, u
 constexpr uint32_t kMergeRuns = 64;   // runs that become one
 constexpr uint32_t kMergeWaves = 16;  // a workgroup places 64 tokens; its wavefronts share the runs
 constexpr uint32_t kMergeEach = kMergeRuns / kMergeWaves;
-
-// How many of keys[0 .. n) are below `key`; n <= length, a power of two.
-__device__ __forceinline__ uint32_t count_below(const uint32_t* keys, uint32_t n, uint32_t length, uint32_t key) {
-  uint32_t at = 0;
-  for (uint32_t step = length; step; step /= 2) {
-    const uint32_t to = at + step;
-    if (to <= n && keys[to - 1] < key) at = to;
-  }
-  return at;
-}
 
 // kTiles: the runs are tiles, which fit into LDS.
 template <bool kTiles>
@@ -127,14 +123,22 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void merge_kernel(uint32_t n, u
       for (uint32_t e = 0; e < kTile / kWave; ++e) staged[wave][k][e * kWave + lane] = v[k][e];
     wave_sync();
   }
+  // how many keys of each run come before, all of its runs' searches side by side
+  uint32_t below[kMergeEach], at[kMergeEach] = {};
+#pragma unroll
+  for (uint32_t k = 0; k < kMergeEach; ++k)
+    below[k] = key + (group + wave + k * kMergeWaves < run);  // equal keys of earlier runs come before
+  for (uint32_t step = length; step; step /= 2) {
+#pragma unroll
+    for (uint32_t k = 0; k < kMergeEach; ++k) {
+      const uint32_t to = at[k] + step;
+      const uint32_t* list = kTiles ? staged[wave][k] : keys + first[k];
+      if (to <= size[k] && list[to - 1] < below[k]) at[k] = to;
+    }
+  }
   uint32_t place = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < kMergeEach; ++k) {
-    const uint32_t other = group + wave + k * kMergeWaves;
-    const uint32_t* list = kTiles ? staged[wave][k] : keys + first[k];
-    if (other == run) place += i - run * length;
-    else place += count_below(list, size[k], length, key + (other < run));  // equal keys of earlier runs come before
-  }
+  for (uint32_t k = 0; k < kMergeEach; ++k) place += group + wave + k * kMergeWaves == run ? i - run * length : at[k];
   count[wave][lane] = place;
   __syncthreads();
   if (wave == 0 && i < n) {
@@ -171,7 +175,7 @@ __device__ __forceinline__ void finish_row(const SumArgs& a, const Mat<float>& o
   before.widen(v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += sum[e] * a.scale;
-  store8<true>(out.p + int64_t(row) * out.ld + col, width, v);
+  store8(out.p + int64_t(row) * out.ld + col, width, v);
 }
 
 __device__ __forceinline__ void read_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
@@ -198,8 +202,7 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n
 __device__ __forceinline__ void zero_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint32_t lane) {
   const float zero[8] = {};
   for (uint64_t col = lane * kBlockCols; col < a.cols; col += kWave * kBlockCols)
-    store8<true>(out.p + int64_t(row) * out.ld + col, uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols),
-                 zero);
+    store8(out.p + int64_t(row) * out.ld + col, uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols), zero);
 }
 
 // Zeros in the rows of no token, a wavefront per row.
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
       const uint32_t e = min(e0 + b, inside - 1);
       i[b] = __builtin_amdgcn_readlane(token, e);
       row[b] = __builtin_amdgcn_readlane(key, e);
-      if (width) raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
+      if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b)
@@ -283,22 +286,28 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   __shared__ float shared[kSumWaves][kWave][8];
   const uint32_t chunk = blockIdx.x / a.slabs, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t lo = chunk * a.chunk, hi = lo + a.chunk;  // not the last chunk
-  const uint32_t run = a.keys[hi - 1];
-  if (run >= a.rows || a.keys[hi] != run) return;
-  if (a.keys[lo] == run && lo > 0 && a.keys[lo - 1] == run) return;  // it began before this chunk
+  // the keys that decide, in one wait: around both ends, and the first ones of the next 64 chunks
+  const uint32_t run = a.keys[hi - 1], prev = lo > 0 ? a.keys[lo - 1] : kNone, head = a.keys[lo];
+  uint32_t next = chunk + 1 + lane;
+  uint32_t key = next < a.chunks ? a.keys[next * a.chunk] : kNone;
+  if (run >= a.rows || __builtin_amdgcn_readfirstlane(key) != run) return;
+  if (head == run && prev == run) return;  // it began before this chunk
   // the chunks that the run reaches: those whose first key is the run's
   uint32_t parts = 0;
   for (;;) {
-    const uint32_t next = chunk + 1 + parts + lane;
-    const bool on = next < a.chunks && a.keys[next * a.chunk] == run;
-    const uint32_t more = uint32_t(__popcll(__ballot(on)));
+    const uint32_t more = uint32_t(__popcll(__ballot(key == run)));
     parts += more;
     if (more < kWave) break;
+    next += kWave;
+    key = next < a.chunks ? a.keys[next * a.chunk] : kNone;
   }
   const uint64_t col = (uint64_t(blockIdx.x - chunk * a.slabs) * kWave + lane) * kBlockCols;
   const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
   float sum[8] = {};
+  Raw8<float> before;
+  before.zero();
   if (width) {
+    if (wave == 0) read_row(a, out, run, col, width, before);
     // part 0 is this chunk's own
     for (uint32_t k0 = wave; k0 <= parts; k0 += kSumWaves * kBatch) {
       Raw8<float> part[kBatch];
@@ -321,8 +330,6 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   for (int e = 0; e < 8; ++e) shared[wave][lane][e] = sum[e];
   __syncthreads();
   if (wave != 0 || !width) return;
-  Raw8<float> before;
-  read_row(a, out, run, col, width, before);
 #pragma unroll
   for (uint32_t w = 1; w < kSumWaves; ++w)
 #pragma unroll
@@ -392,7 +399,7 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
       } else {
         i[b] = b ? i[b - 1] : 0;
       }
-      if (width) raw[b].load(grad.p + int64_t(i[b]) * grad.ld + col, width);
+      if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
@@ -441,7 +448,7 @@ uint64_t part_cols(uint64_t n, uint64_t cols) {
 hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, const uint32_t** keys,
                        const uint32_t** order, hipStream_t stream) {
   auto at = [&](uint64_t byte) { return reinterpret_cast<uint32_t*>(work + byte); };
-  hipLaunchKernelGGL(tile_kernel, dim3((t.n + kTile - 1) / kTile), dim3(kTile), 0, stream, t, at(w.keys[0]), at(w.order[0]));
+  hipLaunchKernelGGL(tile_kernel, dim3((t.n + kTile - 1) / kTile), dim3(kTileThreads), 0, stream, t, at(w.keys[0]), at(w.order[0]));
   uint32_t in = 0;  // the pair of lists that holds the runs
   for (uint64_t length = kTile; length < t.n; length *= kMergeRuns, in ^= 1) {
     const hipError_t e = hipGetLastError();
