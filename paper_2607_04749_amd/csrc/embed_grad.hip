@@ -280,10 +280,13 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   if (!(ends >> (inside - 1) & 1) && width) store8(parts + (came == inside ? 0 : a.cols), width, sum);
 }
 
+constexpr uint32_t kJoinWaves = 4;
+constexpr uint32_t kJoinBatch = 4;  // parts in flight per wavefront
+
 // Joins the parts of the run that begins in this chunk and goes on in the next
 // ones: a workgroup per chunk and slab, its wavefronts taking the parts in turn.
-__global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float> out) {
-  __shared__ float shared[kSumWaves][kWave][8];
+__global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<float> out) {
+  __shared__ float shared[kJoinWaves][kWave][8];
   const uint32_t chunk = blockIdx.x / a.slabs, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t lo = chunk * a.chunk, hi = lo + a.chunk;  // not the last chunk
   // the keys that decide, in one wait: around both ends, and the first ones of the next 64 chunks
@@ -309,16 +312,16 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   if (width) {
     if (wave == 0) read_row(a, out, run, col, width, before);
     // part 0 is this chunk's own
-    for (uint32_t k0 = wave; k0 <= parts; k0 += kSumWaves * kBatch) {
-      Raw8<float> part[kBatch];
+    for (uint32_t k0 = wave; k0 <= parts; k0 += kJoinWaves * kJoinBatch) {
+      Raw8<float> part[kJoinBatch];
 #pragma unroll
-      for (uint32_t b = 0; b < kBatch; ++b) {
-        const uint32_t k = min(k0 + b * kSumWaves, parts);
+      for (uint32_t b = 0; b < kJoinBatch; ++b) {
+        const uint32_t k = min(k0 + b * kJoinWaves, parts);
         part[b].load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width);
       }
 #pragma unroll
-      for (uint32_t b = 0; b < kBatch; ++b) {
-        if (k0 + b * kSumWaves > parts) break;
+      for (uint32_t b = 0; b < kJoinBatch; ++b) {
+        if (k0 + b * kJoinWaves > parts) break;
         float v[8];
         part[b].widen(v);
 #pragma unroll
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(kSumThreads) void join_kernel(SumArgs a, Mat<float>
   __syncthreads();
   if (wave != 0 || !width) return;
 #pragma unroll
-  for (uint32_t w = 1; w < kSumWaves; ++w)
+  for (uint32_t w = 1; w < kJoinWaves; ++w)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += shared[w][lane][e];
   finish_row(a, out, run, col, width, sum, before);
@@ -496,7 +499,7 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20)));
   if (drop.limit) hipLaunchKernelGGL((sum_kernel<T, true>), wgs, block, 0, stream, a, grad, out);
   else hipLaunchKernelGGL((sum_kernel<T, false>), wgs, block, 0, stream, a, grad, out);
-  hipLaunchKernelGGL(join_kernel, dim3((a.chunks - 1) * a.slabs), block, 0, stream, a, out);
+  hipLaunchKernelGGL(join_kernel, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
   return hipGetLastError();
 }
 
