@@ -163,7 +163,8 @@ struct SumArgs {
   float* parts;      // [chunk][2][cols]: 0 of the run that came in, 1 of the run that goes on
   uint32_t n, rows, cols, accumulate;
   uint32_t chunk, chunks, slabs;
-  uint32_t sum_wgs;  // workgroups that sum; the rest write the rows of no token
+  uint32_t sum_wgs;    // workgroups that sum; the rest write the rows of no token
+  uint32_t fill_rows;  // of few tokens: rows per workgroup of these
   float scale;
   Drop drop;
 };
@@ -341,29 +342,40 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
 }
 
 // ---------------------------------------------------------------------------
-// Few tokens, in one launch: a workgroup per token and slab, each lane with one
-// token's key.  The first token of a row adds up all of the row's, every
-// wavefront those among its 64 tokens.  Further workgroups write the rows of no
-// token, kFillRows each.
+// Few tokens, in one launch: a workgroup per token and slab, whose lanes look at
+// all tokens' keys, 64 tokens to a word of a mask.  The first token of a row
+// lists all of the row's and adds them up, its wavefronts a batch at a time in
+// turn.  Further workgroups write the rows of no token.
 
-constexpr uint32_t kFewMost = kSumThreads;  // a token per lane
-constexpr uint32_t kFillRows = 16;
+constexpr uint32_t kFewMost = 512;
+constexpr uint32_t kFewEach = kFewMost / kSumThreads;  // tokens per lane
+constexpr uint32_t kFewBatch = 8;                      // rows in flight per wavefront
+constexpr uint32_t kWords = kFewMost / kWave;
+constexpr uint32_t kFillMost = 16;                     // rows that a workgroup looks for
 
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, Mat<const T> grad, Mat<float> out) {
-  __shared__ uint64_t masks[kSumWaves];
+  __shared__ uint64_t masks[kWords];
+  __shared__ uint32_t list[kFewMost];
   __shared__ float shared[kSumWaves][kWave][8];
-  __shared__ uint32_t seen[kFillRows];
+  __shared__ uint32_t seen[kFillMost];
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const uint32_t key = threadIdx.x < t.n ? t.key(threadIdx.x) : kNone;
+  uint32_t key[kFewEach];
+#pragma unroll
+  for (uint32_t p = 0; p < kFewEach; ++p) {
+    const uint32_t i = p * kSumThreads + threadIdx.x;
+    key[p] = i < t.n ? t.key(i) : kNone;
+  }
   if (blockIdx.x >= a.sum_wgs) {
-    for (uint64_t first = uint64_t(blockIdx.x - a.sum_wgs) * kFillRows; first < a.rows;
-         first += uint64_t(gridDim.x - a.sum_wgs) * kFillRows) {
-      if (threadIdx.x < kFillRows) seen[threadIdx.x] = 0;
+    for (uint64_t first = uint64_t(blockIdx.x - a.sum_wgs) * a.fill_rows; first < a.rows;
+         first += uint64_t(gridDim.x - a.sum_wgs) * a.fill_rows) {
+      if (threadIdx.x < kFillMost) seen[threadIdx.x] = 0;
       __syncthreads();
-      if (key < a.rows && key >= first && key - first < kFillRows) seen[key - first] = 1;
+#pragma unroll
+      for (uint32_t p = 0; p < kFewEach; ++p)
+        if (key[p] < a.rows && key[p] >= first && key[p] - first < a.fill_rows) seen[key[p] - first] = 1;
       __syncthreads();
-      for (uint32_t r = wave; r < kFillRows && first + r < a.rows; r += kSumWaves)
+      for (uint32_t r = wave; r < a.fill_rows && first + r < a.rows; r += kSumWaves)
         if (!seen[r]) zero_row(a, out, uint32_t(first) + r, lane);
       __syncthreads();
     }
@@ -371,42 +383,46 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   }
   const uint32_t mine = blockIdx.x / a.slabs, row = t.key(mine);
   if (row >= a.rows) return;
-  const uint64_t same = __ballot(key == row);
-  if (lane == 0) masks[wave] = same;
-  __syncthreads();
-  uint32_t holders = 0;  // wavefronts with tokens of the row
 #pragma unroll
-  for (uint32_t w = 0; w < kSumWaves; ++w) {
-    const uint64_t m = masks[w];
-    if (w * kWave <= mine && (mine - w * kWave >= kWave ? m : m & ((uint64_t(1) << (mine - w * kWave)) - 1))) return;
-    holders += m != 0;
+  for (uint32_t p = 0; p < kFewEach; ++p) {
+    const uint64_t same = __ballot(key[p] == row);
+    if (lane == 0) masks[p * kSumWaves + wave] = same;
   }
+  __syncthreads();
+  // each of this lane's tokens has the tokens of its word and those before it in the list
+  uint32_t total = 0, before[kFewEach];
+#pragma unroll
+  for (uint32_t w = 0; w < kWords; ++w) {
+    const uint64_t m = masks[w];
+    const uint64_t earlier = mine >= (w + 1) * kWave ? ~uint64_t(0) : mine > w * kWave ? (uint64_t(1) << (mine - w * kWave)) - 1 : 0;
+    if (m & earlier) return;  // an earlier token's workgroup does it; the same for the whole workgroup
+    if (w % kSumWaves == wave) before[w / kSumWaves] = total + uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
+    total += uint32_t(__popcll(m));
+  }
+#pragma unroll
+  for (uint32_t p = 0; p < kFewEach; ++p)
+    if (key[p] == row) list[before[p]] = p * kSumThreads + threadIdx.x;
+  __syncthreads();
   const uint32_t block = (blockIdx.x - mine * a.slabs) * kWave + lane;
   const uint64_t col = uint64_t(block) * kBlockCols;
   const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
-  const bool last = masks[wave] != 0 && wave == mine / kWave;  // the wavefront of the first token finishes the row
-  Raw8<float> before;
-  before.zero();
-  if (width && last) read_row(a, out, row, col, width, before);
+  Raw8<float> held;
+  held.zero();
+  if (width && wave == 0) read_row(a, out, row, col, width, held);
   float sum[8] = {};
-  uint64_t left = same;
-  while (left) {
-    const uint32_t most = uint32_t(__popcll(left));
-    uint32_t i[kBatch];
-    Raw8<T> raw[kBatch];
+  for (uint32_t e0 = wave * kFewBatch; e0 < total; e0 += kSumWaves * kFewBatch) {
+    uint32_t i[kFewBatch];
+    Raw8<T> raw[kFewBatch];
 #pragma unroll
-    for (uint32_t b = 0; b < kBatch; ++b) {
-      if (left) {
-        i[b] = wave * kWave + uint32_t(__builtin_ctzll(left));
-        left &= left - 1;
-      } else {
-        i[b] = b ? i[b - 1] : 0;
+    for (uint32_t b = 0; b < kFewBatch; ++b) {
+      if (e0 + b < total) {
+        i[b] = __builtin_amdgcn_readfirstlane(list[e0 + b]);
+        if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
       }
-      if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
     }
 #pragma unroll
-    for (uint32_t b = 0; b < kBatch; ++b) {
-      if (b >= most) break;
+    for (uint32_t b = 0; b < kFewBatch; ++b) {
+      if (e0 + b >= total) break;
       uint32_t bits[4];
       if (kDrop) a.drop.bits(i[b], block, bits);
       float v[8];
@@ -416,21 +432,34 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
       for (int x = 0; x < 8; ++x) sum[x] += v[x];
     }
   }
-  if (holders > 1) {  // the same for the whole workgroup
+  if (total > kFewBatch) {  // other wavefronts have parts
 #pragma unroll
     for (int x = 0; x < 8; ++x) shared[wave][lane][x] = sum[x];
     __syncthreads();
-    if (last)
-      for (uint32_t w = wave + 1; w < kSumWaves; ++w)
+    if (wave == 0)
+#pragma unroll
+      for (uint32_t w = 1; w < kSumWaves; ++w)
 #pragma unroll
         for (int x = 0; x < 8; ++x) sum[x] += shared[w][lane][x];
   }
-  if (last && width) finish_row(a, out, row, col, width, sum, before);
+  if (wave == 0 && width) finish_row(a, out, row, col, width, sum, held);
 }
 
 // ---------------------------------------------------------------------------
 
+// Few tokens or many, at most so many tokens and workgroups that sum: few waits
+// less (one launch) but leaves a frequent id to four wavefronts.  MI355X, graph
+// replays, in us, few / many, gradients accumulated with dropout:
+//   columns        ids log-uniform                                  all ids alike
+//      256   256: 6.1 / 10.5   512: 8.1 / 14.4   1024: 12.2 / 15.1   512: 36 / 19   1024: 68 / 24
+//     2048   256: 6.2 / 10.6   512: 8.8 / 14.7   1024: 14.2 / 15.8   512: 36 / 19   1024: 68 / 25
+//     8192   128: 9.1 / 10.7   256: 13.5 / 11.3   512: 22.3 / 17.7
+// and each launch less saves the host 2.3 us.
+constexpr uint64_t kFewJobs = 2048;
+
 uint32_t slabs_of(uint64_t cols) { return uint32_t((cols + kWave * kBlockCols - 1) / (kWave * kBlockCols)); }
+
+bool is_few(uint64_t n, uint64_t cols) { return n <= kFewMost && n * slabs_of(cols) <= kFewJobs; }
 
 // Tokens per chunk: at most kJobs wavefronts in all, but 4 to 64 (one per lane) tokens each.
 constexpr uint64_t kJobs = 4096, kChunkLeast = 4, kChunkMost = kWave;
@@ -483,9 +512,10 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   a.slabs = slabs_of(cols);
   a.scale = float(x.scale);
   a.drop = drop;
-  if (n <= kFewMost) {
+  if (is_few(n, cols)) {
     a.sum_wgs = n * a.slabs;
-    const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kFillRows - 1) / kFillRows, 1u << 20)));
+    a.fill_rows = a.slabs == 1 ? kFillMost : kSumWaves;
+    const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + a.fill_rows - 1) / a.fill_rows, 1u << 20)));
     if (drop.limit) hipLaunchKernelGGL((few_kernel<T, true>), wgs, block, 0, stream, t, a, grad, out);
     else hipLaunchKernelGGL((few_kernel<T, false>), wgs, block, 0, stream, t, a, grad, out);
     return hipGetLastError();
@@ -522,7 +552,7 @@ EmbedGradSizes embed_grad_sizes(uint64_t n, uint64_t, uint64_t cols) {
 
 bool embed_grad_fits(uint64_t n, uint64_t cols) {
   // a workgroup per chunk (or token) and slab in the largest launch, of kSumThreads each
-  return (n <= kFewMost ? n : up(n, chunk_of(n, cols))) * slabs_of(cols) <= (uint64_t(1) << 32) / kSumThreads / 2;
+  return (is_few(n, cols) ? n : up(n, chunk_of(n, cols))) * slabs_of(cols) <= (uint64_t(1) << 32) / kSumThreads / 2;
 }
 
 hipError_t launch_embed_grad(const etc_embed_grad_args& a, const Drop& drop, hipStream_t stream) {

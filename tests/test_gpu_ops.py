@@ -201,6 +201,12 @@ GRAD = [
     (256, 24, 5, 5, 0, 0.0, "bf16", "int64", "same", 0, 0),
     (257, 40, 33, 33, 0, 0.1, "bf16", "int64", "log", 0, 0),
     (511, 24, 5000, 5000, 0, 0.0, "bf16", "int64", "distinct", 0, 0),
+    (512, 2048, 300, 300, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (512, 2056, 300, 300, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (512, 24, 5, 5, 0, 0.0, "bf16", "int64", "same", 0, 0),
+    (513, 24, 5000, 5000, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (128, 8192, 40, 40, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (129, 8192, 40, 40, 0, 0.1, "bf16", "int64", "log", 0, 0),
     (16384, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (16385, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (40000, 9, 50000, 50000, 0, 0.1, "f32", "int32", "distinct", 0, 0),
