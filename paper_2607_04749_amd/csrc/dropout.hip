@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_dx_kernel(BlockGrid grid
   store8<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 
-constexpr uint32_t kJoinCols = 32, kJoinRows = 32;
+constexpr uint32_t kJoinCols = 16, kJoinRows = 64, kJoinBatch = 8;
 
 __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float* partial, uint32_t n, uint32_t cols,
                                                                     float* dbias, uint32_t accumulate) {
@@ -150,14 +150,16 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float
   const uint64_t col = uint64_t(blockIdx.x) * kJoinCols + c;
   float sum = 0.0f;
   if (col < cols) {
-    uint32_t k = r;
-    for (; k + 3 * kJoinRows < n; k += 4 * kJoinRows) {
-      float v[4];
+    for (uint32_t k0 = r; k0 < n; k0 += kJoinBatch * kJoinRows) {
+      float v[kJoinBatch];
 #pragma unroll
-      for (uint32_t b = 0; b < 4; ++b) v[b] = partial[uint64_t(k + b * kJoinRows) * cols + col];
-      sum += (v[0] + v[1]) + (v[2] + v[3]);
+      for (uint32_t b = 0; b < kJoinBatch; ++b) {
+        const uint32_t k = k0 + b * kJoinRows;
+        v[b] = k < n ? partial[uint64_t(k) * cols + col] : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t b = 0; b < kJoinBatch; ++b) sum += v[b];
     }
-    for (; k < n; k += kJoinRows) sum += partial[uint64_t(k) * cols + col];
   }
   shared[r][c] = sum;
   __syncthreads();

@@ -49,88 +49,96 @@ __device__ __forceinline__ void wave_sync() {
 // ---------------------------------------------------------------------------
 // Order.  A token's place in a sorted list is the number of tokens before it:
 // smaller keys, and equal ones of earlier tokens.  A tile's are found by
-// comparing each with all; then, level by level, runs of sorted tokens become one, a
-// token's place being its own in its run plus what a binary search finds
-// before it in each of the other runs.  No counters, so no order of arrival.
+// comparing each with all; then, level by level, runs of sorted tokens become
+// one, a token's place being its own in its run plus what a binary search finds
+// before it in each of the other runs.  No counters, so no order of arrival.  Either
+// way a workgroup places 64 tokens, and its 16 wavefronts share what they are
+// compared with, so that a launch is a few waits long however many tokens there are.
 
-constexpr uint32_t kTile = 256;
-constexpr uint32_t kTileParts = kTile / kWave;  // a token's keys to compare with are shared by so many lanes
-constexpr uint32_t kTileThreads = kTile * kTileParts;
+constexpr uint32_t kPlaceWaves = 16;
+constexpr uint32_t kPlaceThreads = kPlaceWaves * kWave;
+constexpr uint32_t kTile = kPlaceWaves * kWave;  // a wavefront compares with 64 keys
 
-__global__ __launch_bounds__(kTileThreads) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
-  __shared__ __attribute__((aligned(16))) uint32_t all[kTile];
-  __shared__ uint32_t count[kTileParts][kTile];
+// The sum over the workgroup's wavefronts of what each counted, in the first of them.
+__device__ __forceinline__ uint32_t total_place(uint32_t (&count)[kPlaceWaves][kWave], uint32_t place) {
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const uint32_t mine = wave % kTileParts, part = wave / kTileParts;  // 64 tokens of the tile, against 64 keys of it
-  const uint32_t first = blockIdx.x * kTile, x = mine * kWave + lane, i = first + x;
-  const uint32_t key = i < t.n ? t.key(i) : kNone;
-  if (part == 0) all[x] = key;
+  count[wave][lane] = place;
   __syncthreads();
-  uint32_t place = 0;
-  if (part != mine) {
-    const uint32_t below = key + (part < mine);  // equal keys of earlier wavefronts come before
+  uint32_t total = 0;
+  if (wave == 0)
 #pragma unroll
-    for (uint32_t e = 0; e < kWave; ++e) place += all[part * kWave + e] < below;
+    for (uint32_t w = 0; w < kPlaceWaves; ++w) total += count[w][lane];
+  return total;
+}
+
+__global__ __launch_bounds__(kPlaceThreads) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
+  __shared__ __attribute__((aligned(16))) uint32_t all[kPlaceWaves][kWave];
+  __shared__ uint32_t count[kPlaceWaves][kWave];
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t mine = blockIdx.x, i = mine * kWave + lane;
+  const uint32_t first = mine / kPlaceWaves * kTile, other = mine / kPlaceWaves * kPlaceWaves + wave;
+  const uint32_t j = other * kWave + lane;
+  const uint32_t key = i < t.n ? t.key(i) : kNone;
+  all[wave][lane] = j < t.n ? t.key(j) : kNone;
+  wave_sync();
+  uint32_t place = 0;
+  if (other != mine) {
+    const uint32_t below = key + (other < mine);  // equal keys of earlier tokens come before
+#pragma unroll
+    for (uint32_t e = 0; e < kWave; ++e) place += all[wave][e] < below;
   } else {
 #pragma unroll
-    for (uint32_t e = 0; e < kWave; ++e) place += all[part * kWave + e] < key + (e < lane);
+    for (uint32_t e = 0; e < kWave; ++e) place += all[wave][e] < key + (e < lane);
   }
-  count[part][x] = place;
-  __syncthreads();
-  if (part == 0 && i < t.n) {
-    place = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kTileParts; ++w) place += count[w][x];
+  place = total_place(count, place);
+  if (wave == 0 && i < t.n) {
     keys[first + place] = key;
     order[first + place] = i;
   }
 }
 
-constexpr uint32_t kMergeRuns = 64;   // runs that become one
-constexpr uint32_t kMergeWaves = 16;  // a workgroup places 64 tokens; its wavefronts share the runs
-constexpr uint32_t kMergeEach = kMergeRuns / kMergeWaves;
-
-// kTiles: the runs are tiles, which fit into LDS.
-template <bool kTiles>
-__global__ __launch_bounds__(kMergeWaves* kWave) void merge_kernel(uint32_t n, uint32_t length, const uint32_t* keys,
-                                                                   const uint32_t* order, uint32_t* to_keys,
-                                                                   uint32_t* to_order) {
-  __shared__ uint32_t staged[kTiles ? kMergeWaves : 1][kMergeEach][kTiles ? kTile : 1];
-  __shared__ uint32_t count[kMergeWaves][kWave];
+// kEach runs per wavefront become one with those of the other wavefronts.
+// kTiles: the runs are tiles, which are staged in LDS.
+template <bool kTiles, uint32_t kEach>
+__global__ __launch_bounds__(kPlaceThreads) void merge_kernel(uint32_t n, uint32_t length, const uint32_t* keys,
+                                                              const uint32_t* order, uint32_t* to_keys,
+                                                              uint32_t* to_order) {
+  constexpr uint32_t kRuns = kEach * kPlaceWaves;
+  __shared__ uint32_t staged[kTiles ? kPlaceWaves : 1][kEach][kTiles ? kTile : 1];
+  __shared__ uint32_t count[kPlaceWaves][kWave];
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t from = blockIdx.x * kWave, i = from + lane;  // one run's: lengths are multiples of 64
-  const uint32_t run = from / length, group = run / kMergeRuns * kMergeRuns;
+  const uint32_t run = from / length, group = run / kRuns * kRuns;
   const uint32_t key = i < n ? keys[i] : 0;
-  uint32_t first[kMergeEach], size[kMergeEach];
+  uint32_t first[kEach], size[kEach];
 #pragma unroll
-  for (uint32_t k = 0; k < kMergeEach; ++k) {
-    const uint64_t start = uint64_t(group + wave + k * kMergeWaves) * length;
+  for (uint32_t k = 0; k < kEach; ++k) {
+    const uint64_t start = uint64_t(group + wave + k * kPlaceWaves) * length;
     first[k] = uint32_t(start < n ? start : 0);
     size[k] = start < n ? min(length, n - uint32_t(start)) : 0;
   }
   if constexpr (kTiles) {
-    uint32_t v[kMergeEach][kTile / kWave];
 #pragma unroll
-    for (uint32_t k = 0; k < kMergeEach; ++k)
+    for (uint32_t k = 0; k < kEach; ++k) {
+      uint32_t v[kTile / kWave];
 #pragma unroll
       for (uint32_t e = 0; e < kTile / kWave; ++e) {
         const uint32_t x = e * kWave + lane;
-        v[k][e] = x < size[k] ? keys[first[k] + x] : kNone;
+        v[e] = x < size[k] ? keys[first[k] + x] : kNone;
       }
 #pragma unroll
-    for (uint32_t k = 0; k < kMergeEach; ++k)
-#pragma unroll
-      for (uint32_t e = 0; e < kTile / kWave; ++e) staged[wave][k][e * kWave + lane] = v[k][e];
+      for (uint32_t e = 0; e < kTile / kWave; ++e) staged[wave][k][e * kWave + lane] = v[e];
+    }
     wave_sync();
   }
   // how many keys of each run come before, all of its runs' searches side by side
-  uint32_t below[kMergeEach], at[kMergeEach] = {};
+  uint32_t below[kEach], at[kEach] = {};
 #pragma unroll
-  for (uint32_t k = 0; k < kMergeEach; ++k)
-    below[k] = key + (group + wave + k * kMergeWaves < run);  // equal keys of earlier runs come before
+  for (uint32_t k = 0; k < kEach; ++k)
+    below[k] = key + (group + wave + k * kPlaceWaves < run);  // equal keys of earlier runs come before
   for (uint32_t step = length; step; step /= 2) {
 #pragma unroll
-    for (uint32_t k = 0; k < kMergeEach; ++k) {
+    for (uint32_t k = 0; k < kEach; ++k) {
       const uint32_t to = at[k] + step;
       const uint32_t* list = kTiles ? staged[wave][k] : keys + first[k];
       if (to <= size[k] && list[to - 1] < below[k]) at[k] = to;
@@ -138,13 +146,9 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void merge_kernel(uint32_t n, u
   }
   uint32_t place = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < kMergeEach; ++k) place += group + wave + k * kMergeWaves == run ? i - run * length : at[k];
-  count[wave][lane] = place;
-  __syncthreads();
+  for (uint32_t k = 0; k < kEach; ++k) place += group + wave + k * kPlaceWaves == run ? i - run * length : at[k];
+  place = total_place(count, place);
   if (wave == 0 && i < n) {
-    place = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kMergeWaves; ++w) place += count[w][lane];
     const uint32_t to = group * length + place;
     to_keys[to] = key;
     to_order[to] = order[i];
@@ -480,15 +484,16 @@ uint64_t part_cols(uint64_t n, uint64_t cols) {
 hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, const uint32_t** keys,
                        const uint32_t** order, hipStream_t stream) {
   auto at = [&](uint64_t byte) { return reinterpret_cast<uint32_t*>(work + byte); };
-  hipLaunchKernelGGL(tile_kernel, dim3((t.n + kTile - 1) / kTile), dim3(kTileThreads), 0, stream, t, at(w.keys[0]), at(w.order[0]));
+  const dim3 wgs((t.n + kWave - 1) / kWave), block(kPlaceThreads);
+  hipLaunchKernelGGL(tile_kernel, wgs, block, 0, stream, t, at(w.keys[0]), at(w.order[0]));
   uint32_t in = 0;  // the pair of lists that holds the runs
-  for (uint64_t length = kTile; length < t.n; length *= kMergeRuns, in ^= 1) {
+  for (uint64_t length = kTile, runs = kPlaceWaves; length < t.n; length *= runs, runs = 4 * kPlaceWaves) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 wgs((t.n + kWave - 1) / kWave), block(kMergeWaves * kWave);
-    auto merge = length == kTile ? merge_kernel<true> : merge_kernel<false>;
+    auto merge = length == kTile ? merge_kernel<true, 1> : merge_kernel<false, 4>;
     hipLaunchKernelGGL(merge, wgs, block, 0, stream, t.n, uint32_t(length), at(w.keys[in]), at(w.order[in]),
                        at(w.keys[in ^ 1]), at(w.order[in ^ 1]));
+    in ^= 1;
   }
   *keys = at(w.keys[in]);
   *order = at(w.order[in]);
@@ -551,8 +556,10 @@ EmbedGradSizes embed_grad_sizes(uint64_t n, uint64_t, uint64_t cols) {
 }
 
 bool embed_grad_fits(uint64_t n, uint64_t cols) {
-  // a workgroup per chunk (or token) and slab in the largest launch, of kSumThreads each
-  return (is_few(n, cols) ? n : up(n, chunk_of(n, cols))) * slabs_of(cols) <= (uint64_t(1) << 32) / kSumThreads / 2;
+  constexpr uint64_t lanes = uint64_t(1) << 31;  // of a launch
+  // ordering: a workgroup per 64 tokens; sums: one per chunk (or token) and slab in the largest launch
+  const uint64_t jobs = (is_few(n, cols) ? n : up(n, chunk_of(n, cols))) * slabs_of(cols);
+  return up(n, kWave) * kPlaceThreads <= lanes && jobs * kSumThreads <= lanes;
 }
 
 hipError_t launch_embed_grad(const etc_embed_grad_args& a, const Drop& drop, hipStream_t stream) {

@@ -542,11 +542,19 @@ def _drop(dropout):
     return _NO_DROP if dropout is None else dropout._fields
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device_of(x, what):
     """The current device's number; the operator's tensors have to be there."""
-    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
+    d = x.get_device()
+    if d < 0 or d != _current_device():
         raise ValueError(f"{what} must be a tensor on the current GPU")
-    return x.get_device()
+    return d
+
+
+def _stream_on(stream, device):
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 def _matrix(x, what, device):
@@ -595,7 +603,7 @@ def etc_embed(tokens, table, out, row0=0, scale=1.0, positions=None, pos_table=N
     q = _NO_IDS if positions is None else _ids(positions, "positions", d)
     p = _NO_MATRIX if pos_table is None else _matrix(pos_table, "pos_table", d)
     _check(_lib.etc_embed(_EMBED.pack(*t, *q, *_matrix(table, "table", d), *p, *_matrix(out, "out", d),
-                                      *_drop(dropout), row0, scale), _stream(stream)), "etc_embed")
+                                      *_drop(dropout), row0, scale), _stream_on(stream, d)), "etc_embed")
 
 
 def etc_embed_grad_bytes(ntokens, table_rows, cols):
@@ -612,7 +620,7 @@ def etc_embed_grad(tokens, grad, dtable, workspace, row0=0, scale=1.0, dropout=N
     _check(_lib.etc_embed_grad(_EMBED_GRAD.pack(*_ids(tokens, "tokens", d), *_matrix(grad, "grad", d),
                                                 *_matrix(dtable, "dtable", d), *_drop(dropout), row0, scale,
                                                 *_workspace(workspace, d), bool(accumulate), 0),
-                               _stream(stream)), "etc_embed_grad")
+                               _stream_on(stream, d)), "etc_embed_grad")
 
 
 def etc_dropout(x, out, dropout=None, bias=None, residual=None, stream=None):
@@ -621,7 +629,7 @@ def etc_dropout(x, out, dropout=None, bias=None, residual=None, stream=None):
     b = _NO_MATRIX if bias is None else _matrix(bias, "bias", d)
     r = _NO_MATRIX if residual is None else _matrix(residual, "residual", d)
     _check(_lib.etc_dropout(_DROPOUT.pack(*_matrix(x, "x", d), *b, *r, *_matrix(out, "out", d), *_drop(dropout)),
-                            _stream(stream)), "etc_dropout")
+                            _stream_on(stream, d)), "etc_dropout")
 
 
 def etc_dropout_grad_bytes(rows, cols):
@@ -637,7 +645,7 @@ def etc_dropout_grad(grad, dx, dropout=None, dbias=None, workspace=None, accumul
     b = _NO_MATRIX if dbias is None else _matrix(dbias, "dbias", d)
     _check(_lib.etc_dropout_grad(_DROPOUT_GRAD.pack(*_matrix(grad, "grad", d), *_matrix(dx, "dx", d), *b,
                                                     *_drop(dropout), *_workspace(workspace, d), bool(accumulate), 0),
-                                 _stream(stream)), "etc_dropout_grad")
+                                 _stream_on(stream, d)), "etc_dropout_grad")
 
 
 def etc_adam(arenas, grad, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, first=0,

@@ -177,6 +177,7 @@ REFUSED = [
     (lambda: embed_grad(nbytes=8), INVALID), (lambda: embed_grad(reserved=1), INVALID),
     (lambda: embed_grad(tokens=ids((1 << 31) - 1), grad=mat((1 << 31) - 1, (1 << 31) - 1, ld=0),
                         dtable=mat(1, (1 << 31) - 1, F32)), UNSUPPORTED),
+    (lambda: embed_grad(tokens=ids((1 << 27) + 1), grad=mat((1 << 27) + 1, 16)), UNSUPPORTED),
     (lambda: embed_grad(scale=NAN), INVALID), (lambda: embed_grad(d=drop(p=2.0)), INVALID),
     (lambda: dropout(out=mat(3, 16, F32)), INVALID), (lambda: dropout(out=mat(3, 17)), INVALID),
     (lambda: dropout(bias=mat(2, 16)), INVALID), (lambda: dropout(bias=mat(1, 8)), INVALID),
