@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
 
 constexpr uint32_t kFewMost = 512;
 constexpr uint32_t kFewEach = kFewMost / kSumThreads;  // tokens per lane
-constexpr uint32_t kFewBatch = 8;                      // rows in flight per wavefront
+constexpr uint32_t kFewBatch = 2;                      // rows in flight per wavefront: most rows have one or two tokens
 constexpr uint32_t kWords = kFewMost / kWave;
 constexpr uint32_t kFillMost = 16;                     // rows that a workgroup looks for
 
@@ -415,25 +415,22 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   if (width && wave == 0) read_row(a, out, row, col, width, held);
   float sum[8] = {};
   for (uint32_t e0 = wave * kFewBatch; e0 < total; e0 += kSumWaves * kFewBatch) {
-    uint32_t i[kFewBatch];
+    // all loads, then all of the arithmetic without branches, so that the rows' chains of products overlap
     Raw8<T> raw[kFewBatch];
+    uint32_t bits[kFewBatch][4];
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
-      if (e0 + b < total) {
-        i[b] = __builtin_amdgcn_readfirstlane(list[e0 + b]);
-        if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
-      }
+      const uint32_t i = __builtin_amdgcn_readfirstlane(list[min(e0 + b, total - 1)]);
+      if (width) raw[b].template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
+      if (kDrop) a.drop.bits(i, block, bits[b]);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
-      if (e0 + b >= total) break;
-      uint32_t bits[4];
-      if (kDrop) a.drop.bits(i[b], block, bits);
       float v[8];
       raw[b].widen(v);
-      if (kDrop) a.drop.apply(bits, v);
+      if (kDrop) a.drop.apply(bits[b], v);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) sum[x] += v[x];
+      for (int x = 0; x < 8; ++x) sum[x] += e0 + b < total ? v[x] : 0.0f;
     }
   }
   if (total > kFewBatch) {  // other wavefronts have parts
@@ -452,13 +449,13 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
 // ---------------------------------------------------------------------------
 
 // Few tokens or many, at most so many tokens and workgroups that sum: few waits
-// less (one launch) but leaves a frequent id to four wavefronts.  MI355X, graph
-// replays, in us, few / many, gradients accumulated with dropout:
-//   columns        ids log-uniform                                  all ids alike
-//      256   256: 6.1 / 10.5   512: 8.1 / 14.4   1024: 12.2 / 15.1   512: 36 / 19   1024: 68 / 24
-//     2048   256: 6.2 / 10.6   512: 8.8 / 14.7   1024: 14.2 / 15.8   512: 36 / 19   1024: 68 / 25
-//     8192   128: 9.1 / 10.7   256: 13.5 / 11.3   512: 22.3 / 17.7
-// and each launch less saves the host 2.3 us.
+// less (one launch, where many take three or four, at 2.3 us of the host's time
+// each) but leaves a frequent id to four wavefronts, whose arithmetic it then
+// waits for.  MI355X, graph replays, in us, few / many, accumulated, dropout:
+//   columns   ids log-uniform                     all ids alike
+//      256    256: 5.1 / 10.2   512: 7.4 / 10.5    256: 21 / 11.6   512: 39 / 14.6
+//     2048    256: 4.9 / 10.2   512: 6.5 / 10.6    256: 21 / 12.1   512: 39 / 15.1
+//     8192    128: 6.9 / 10.2   512: 22 / 13.4     128: 11.8 / 10.5
 constexpr uint64_t kFewJobs = 2048;
 
 uint32_t slabs_of(uint64_t cols) { return uint32_t((cols + kWave * kBlockCols - 1) / (kWave * kBlockCols)); }
