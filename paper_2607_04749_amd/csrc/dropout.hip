@@ -23,27 +23,29 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_kernel(BlockGrid grid, D
                                                            Mat<const T> residual, Mat<T> out) {
   const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
   if (at >= grid.n) return;
-  uint32_t i, block, width;
-  grid.place(at, &i, &block, &width);
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  Raw8<T> rx, rb, rr;
+  constexpr uint32_t kC = kLaneCols<T>;
+  uint32_t i, block;
+  grid.place(at, &i, &block);
+  const uint64_t col = uint64_t(block) * kC;
+  const uint32_t width = block_width<kC>(col, grid.cols);
+  Raw<T, kC> rx, rb, rr;
   rb.zero();
   rr.zero();
   rx.template load<true>(x.p + int64_t(i) * x.ld + col, width);
   if (residual.p) rr.template load<true>(residual.p + int64_t(i) * residual.ld + col, width);
   if (bias) rb.load(bias + col, width);
-  uint32_t bits[4];
-  if (kDrop) drop.bits(i, block, bits);  // while the loads are on their way
-  float v[8], w[8];
+  uint32_t bits[kC / 2];
+  if (kDrop) drop.template bits<kC>(i, col, bits);  // while the loads are on their way
+  float v[kC], w[kC];
   rx.widen(v);
   rb.widen(w);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += w[e];
-  if (kDrop) drop.apply(bits, v);
+  for (uint32_t e = 0; e < kC; ++e) v[e] += w[e];
+  if (kDrop) drop.template apply<kC>(bits, v);
   rr.widen(w);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += w[e];
-  store8<true>(out.p + int64_t(i) * out.ld + col, width, v);
+  for (uint32_t e = 0; e < kC; ++e) v[e] += w[e];
+  store_block<true>(out.p + int64_t(i) * out.ld + col, width, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -65,9 +67,9 @@ constexpr uint32_t kBatch = 2;     // rows in flight per lane
 constexpr uint64_t kWgs = 2048;    // workgroups wanted at most
 constexpr uint32_t kSlab = 64;     // blocks of a slab at most
 
-GradShape grad_shape(uint32_t rows, uint32_t cols) {
+GradShape grad_shape(uint32_t rows, uint32_t cols, uint32_t block) {
   GradShape g{rows, cols, 0, 0, 0, 0};
-  const uint32_t nb = blocks_per_row(cols);
+  const uint32_t nb = blocks_per_row(cols, block);
   while ((1u << g.lane_bits) < std::min(nb, kSlab)) ++g.lane_bits;
   g.slabs = (nb + kSlab - 1) / kSlab;
   const uint64_t least = g.down() * kBatch;  // at least 8
@@ -80,17 +82,17 @@ GradShape grad_shape(uint32_t rows, uint32_t cols) {
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Drop drop, Mat<const T> grad, Mat<T> dx,
                                                                 float* partial) {
-  __shared__ float shared[kThreads][kBlockCols + 1];
+  constexpr uint32_t kC = kLaneCols<T>;
+  __shared__ float shared[kThreads][kC + 1];
   const uint32_t part = blockIdx.x / g.slabs, across = threadIdx.x & ((1u << g.lane_bits) - 1);
-  const uint32_t block = (blockIdx.x - part * g.slabs) * kSlab + across;
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  const uint32_t width = col >= g.cols ? 0 : uint32_t(g.cols - col < kBlockCols ? g.cols - col : kBlockCols);
+  const uint64_t left = uint64_t(blockIdx.x - part * g.slabs) * kSlab * kC, col = left + across * kC;
+  const uint32_t width = block_width<kC>(col, g.cols);
   const uint32_t down = kThreads >> g.lane_bits;
   const uint32_t end = uint32_t(min(uint64_t(g.rows), (uint64_t(part) + 1) * g.step));
-  float sum[8] = {};
+  float sum[kC] = {};
   if (width) {
     for (uint64_t i0 = uint64_t(part) * g.step + (threadIdx.x >> g.lane_bits); i0 < end; i0 += down * kBatch) {
-      Raw8<T> raw[kBatch];
+      Raw<T, kC> raw[kBatch];
 #pragma unroll
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
@@ -100,26 +102,25 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
         if (i >= end) break;
-        uint32_t bits[4];
-        if (kDrop) drop.bits(i, block, bits);
-        float v[8];
+        uint32_t bits[kC / 2];
+        if (kDrop) drop.template bits<kC>(i, col, bits);
+        float v[kC];
         raw[b].widen(v);
-        if (kDrop) drop.apply(bits, v);
+        if (kDrop) drop.template apply<kC>(bits, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += v[e];
-        store8<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
+        for (uint32_t e = 0; e < kC; ++e) sum[e] += v[e];
+        store_block<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
       }
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) shared[threadIdx.x][e] = sum[e];
+  for (uint32_t e = 0; e < kC; ++e) shared[threadIdx.x][e] = sum[e];
   __syncthreads();
   // a column's sums lie `1 << lane_bits` lanes apart
-  for (uint32_t c = threadIdx.x; c < (kBlockCols << g.lane_bits); c += kThreads) {
+  for (uint32_t c = threadIdx.x; c < (kC << g.lane_bits); c += kThreads) {
     float total = 0.0f;
-    for (uint32_t k = 0; k < down; ++k) total += shared[(k << g.lane_bits) + c / kBlockCols][c % kBlockCols];
-    const uint64_t to = uint64_t(blockIdx.x - part * g.slabs) * kSlab * kBlockCols + c;
-    if (to < g.cols) partial[uint64_t(part) * g.cols + to] = total;
+    for (uint32_t k = 0; k < down; ++k) total += shared[(k << g.lane_bits) + c / kC][c % kC];
+    if (left + c < g.cols) partial[uint64_t(part) * g.cols + left + c] = total;
   }
 }
 
@@ -128,17 +129,19 @@ template <typename T, bool kDrop>
 __global__ __launch_bounds__(kFlatThreads) void dropout_dx_kernel(BlockGrid grid, Drop drop, Mat<const T> grad, Mat<T> dx) {
   const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
   if (at >= grid.n) return;
-  uint32_t i, block, width;
-  grid.place(at, &i, &block, &width);
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  Raw8<T> raw;
+  constexpr uint32_t kC = kLaneCols<T>;
+  uint32_t i, block;
+  grid.place(at, &i, &block);
+  const uint64_t col = uint64_t(block) * kC;
+  const uint32_t width = block_width<kC>(col, grid.cols);
+  Raw<T, kC> raw;
   raw.template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
-  uint32_t bits[4];
-  if (kDrop) drop.bits(i, block, bits);
-  float v[8];
+  uint32_t bits[kC / 2];
+  if (kDrop) drop.template bits<kC>(i, col, bits);
+  float v[kC];
   raw.widen(v);
-  if (kDrop) drop.apply(bits, v);
-  store8<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
+  if (kDrop) drop.template apply<kC>(bits, v);
+  store_block<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 
 constexpr uint32_t kJoinCols = 16, kJoinRows = 64, kJoinBatch = 8;
@@ -172,7 +175,7 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float
 
 template <typename T>
 hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {
-  return for_row_runs(a.x.rows, a.x.cols, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+  return for_row_runs(a.x.rows, a.x.cols, kLaneCols<T>, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto at = [&](const etc_matrix& m) {
       return Mat<T>{m.data ? static_cast<T*>(m.data) + first * m.ld : nullptr, m.ld};
     };
@@ -193,7 +196,7 @@ hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream
 
 template <typename T>
 hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
-  return for_row_runs(a.grad.rows, a.grad.cols, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+  return for_row_runs(a.grad.rows, a.grad.cols, kLaneCols<T>, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     const Mat<const T> grad{static_cast<const T*>(a.grad.data) + first * a.grad.ld, a.grad.ld};
     const Mat<T> dx{static_cast<T*>(a.dx.data) + first * a.dx.ld, a.dx.ld};
     Drop d = drop;
@@ -208,7 +211,7 @@ hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream
 template <typename T>
 hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
   if (!a.dbias.data) return launch_dx<T>(a, drop, stream);
-  const GradShape g = grad_shape(uint32_t(a.grad.rows), uint32_t(a.grad.cols));
+  const GradShape g = grad_shape(uint32_t(a.grad.rows), uint32_t(a.grad.cols), kLaneCols<T>);
   float* partial = static_cast<float*>(a.workspace);
   if (g.parts) {
     const dim3 wgs(g.parts * g.slabs), block(kThreads);
@@ -231,7 +234,7 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
 // At most rows / 8 parts, and kWgs / slabs of them where steps are longer: it
 // grows with rows and cols, so a workspace serves smaller calls.
 uint64_t dropout_grad_bytes(uint64_t rows, uint64_t cols) {
-  return std::min((rows + 7) / 8 * cols, kWgs * kSlab * kBlockCols + cols) * sizeof(float);
+  return std::min((rows + 7) / 8 * cols, kWgs * kSlab * kLaneCols<bf16> + cols) * sizeof(float);
 }
 
 hipError_t launch_dropout(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {

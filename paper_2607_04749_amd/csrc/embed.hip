@@ -4,7 +4,7 @@
 //   out[i, :] = drop(scale * table[id_i - row0, :] + pos_table[position_i, :])
 //
 // HBM bound: it reads the rows that occur and writes one row per token.  A
-// lane moves one block of eight columns.
+// lane moves one or two blocks of columns.
 #include <hip/hip_runtime.h>
 
 #include "ops.hpp"
@@ -31,10 +31,11 @@ template <typename T, typename O, bool kDrop, uint32_t kN>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> out) {
   const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
   if (at >= a.grid.n) return;
-  uint32_t group, block, width;
-  a.grid.place(at, &group, &block, &width);
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  const uint32_t i0 = group * kN, last = a.grid.rows - 1;
+  constexpr uint32_t kC = kLaneCols<O>;
+  uint32_t group, block;
+  a.grid.place(at, &group, &block);
+  const uint64_t col = uint64_t(block) * kC;
+  const uint32_t width = block_width<kC>(col, a.grid.cols), i0 = group * kN, last = a.grid.rows - 1;
   uint64_t k[kN], q[kN] = {};
 #pragma unroll
   for (uint32_t r = 0; r < kN; ++r) {
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> 
     k[r] = uint64_t(a.tokens.at(i)) - uint64_t(a.row0);  // unsigned: an id below row0 becomes a large row
     if (a.pos.p) q[r] = uint64_t(a.positions.at(i));
   }
-  Raw8<T> word[kN], place[kN];
+  Raw<T, kC> word[kN], place[kN];
 #pragma unroll
   for (uint32_t r = 0; r < kN; ++r) {
     word[r].zero();
@@ -54,15 +55,15 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> 
   for (uint32_t r = 0; r < kN; ++r) {
     const uint32_t i = i0 + r;
     if (i > last) break;
-    uint32_t bits[4];
-    if (kDrop) a.drop.bits(i, block, bits);  // while the loads are on their way
-    float v[8], w[8];
+    uint32_t bits[kC / 2];
+    if (kDrop) a.drop.template bits<kC>(i, col, bits);  // while the loads are on their way
+    float v[kC], w[kC];
     word[r].widen(v);
     place[r].widen(w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = v[e] * a.scale + w[e];
-    if (kDrop) a.drop.apply(bits, v);
-    store8<true>(out.p + int64_t(i) * out.ld + col, width, v);
+    for (uint32_t e = 0; e < kC; ++e) v[e] = v[e] * a.scale + w[e];
+    if (kDrop) a.drop.template apply<kC>(bits, v);
+    store_block<true>(out.p + int64_t(i) * out.ld + col, width, v);
   }
 }
 
@@ -78,8 +79,8 @@ hipError_t launch(const etc_embed_args& x, const Drop& drop, hipStream_t stream)
   // Two rows per lane where dropout's arithmetic can fill the wait for the
   // second row's loads: 16384 x 2048 with positions and dropout 20.5 us, with one
   // row 22.4; 8192 x 8192 without dropout 22.5 us, with one row 20.8.
-  const bool two = drop.limit && uint64_t(x.out.rows) * blocks_per_row(x.out.cols) >= kManyBlocks;
-  return for_row_runs(x.out.rows, x.out.cols, two ? 2 : 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+  const bool two = drop.limit && uint64_t(x.out.rows) * blocks_per_row(x.out.cols, kLaneCols<O>) >= kManyBlocks;
+  return for_row_runs(x.out.rows, x.out.cols, kLaneCols<O>, two ? 2 : 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto ids = [&](const etc_ids& v) {
       const bool wide = v.dtype == ETC_IDS_I64;
       return Ids{v.data ? static_cast<const char*>(v.data) + first * (wide ? 8 : 4) : nullptr, wide};

@@ -174,17 +174,19 @@ struct SumArgs {
 };
 
 // A row of the table that a run ends in: what it holds, read early, and then the whole of it.
+template <uint32_t kC>
 __device__ __forceinline__ void finish_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
-                                           uint32_t width, const float (&sum)[8], const Raw8<float>& before) {
-  float v[8];
+                                           uint32_t width, const float (&sum)[kC], const Raw<float, kC>& before) {
+  float v[kC];
   before.widen(v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += sum[e] * a.scale;
-  store8(out.p + int64_t(row) * out.ld + col, width, v);
+  for (uint32_t e = 0; e < kC; ++e) v[e] += sum[e] * a.scale;
+  store_block(out.p + int64_t(row) * out.ld + col, width, v);
 }
 
+template <uint32_t kC>
 __device__ __forceinline__ void read_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
-                                         uint32_t width, Raw8<float>& before) {
+                                         uint32_t width, Raw<float, kC>& before) {
   if (a.accumulate) before.load(out.p + int64_t(row) * out.ld + col, width);
   else before.zero();
 }
@@ -205,9 +207,10 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n
 }
 
 __device__ __forceinline__ void zero_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint32_t lane) {
-  const float zero[8] = {};
-  for (uint64_t col = lane * kBlockCols; col < a.cols; col += kWave * kBlockCols)
-    store8(out.p + int64_t(row) * out.ld + col, uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols), zero);
+  constexpr uint32_t kC = kLaneCols<float>;
+  const float zero[kC] = {};
+  for (uint64_t col = lane * kC; col < a.cols; col += kWave * kC)
+    store_block(out.p + int64_t(row) * out.ld + col, block_width<kC>(col, a.cols), zero);
 }
 
 // Zeros in the rows of no token, a wavefront per row.
@@ -222,6 +225,7 @@ __device__ __forceinline__ void fill_rows(const SumArgs& a, const Mat<float>& ou
 
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T> grad, Mat<float> out) {
+  constexpr uint32_t kC = kLaneCols<T>;
   if (blockIdx.x >= a.sum_wgs) {
     fill_rows(a, out);
     return;
@@ -241,15 +245,14 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   // the run that began in an earlier chunk: its end here goes to the parts, not to the table
   uint32_t came = __builtin_amdgcn_readfirstlane(key) == prev ? (ends ? uint32_t(__builtin_ctzll(ends)) : inside) : kNone;
 
-  const uint32_t block = (job - chunk * a.slabs) * kWave + lane;
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
+  const uint64_t col = (uint64_t(job - chunk * a.slabs) * kWave + lane) * kC;
+  const uint32_t width = block_width<kC>(col, a.cols);
   float* parts = a.parts + uint64_t(chunk) * 2 * a.cols + col;
-  float sum[8] = {};
+  float sum[kC] = {};
   for (uint32_t e0 = 0; e0 < inside; e0 += kBatch) {
     uint32_t i[kBatch], row[kBatch];
-    Raw8<T> raw[kBatch];
-    Raw8<float> before[kBatch];
+    Raw<T, kC> raw[kBatch];
+    Raw<float, kC> before[kBatch];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t e = min(e0 + b, inside - 1);
@@ -264,25 +267,25 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t e = e0 + b;
       if (e >= inside) break;
-      uint32_t bits[4];
-      if (kDrop) a.drop.bits(i[b], block, bits);
-      float v[8];
+      uint32_t bits[kC / 2];
+      if (kDrop) a.drop.template bits<kC>(i[b], col, bits);
+      float v[kC];
       raw[b].widen(v);
-      if (kDrop) a.drop.apply(bits, v);
+      if (kDrop) a.drop.template apply<kC>(bits, v);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) sum[x] += v[x];
+      for (uint32_t x = 0; x < kC; ++x) sum[x] += v[x];
       if (ends >> e & 1) {
         if (width) {
-          if (e == came) store8(parts, width, sum);
+          if (e == came) store_block(parts, width, sum);
           else finish_row(a, out, row[b], col, width, sum, before[b]);
         }
 #pragma unroll
-        for (int x = 0; x < 8; ++x) sum[x] = 0.0f;
+        for (uint32_t x = 0; x < kC; ++x) sum[x] = 0.0f;
       }
     }
   }
   // a run that goes on: part 0 where it fills the chunk and came in, else part 1
-  if (!(ends >> (inside - 1) & 1) && width) store8(parts + (came == inside ? 0 : a.cols), width, sum);
+  if (!(ends >> (inside - 1) & 1) && width) store_block(parts + (came == inside ? 0 : a.cols), width, sum);
 }
 
 constexpr uint32_t kJoinWaves = 4;
@@ -290,8 +293,9 @@ constexpr uint32_t kJoinBatch = 4;  // parts in flight per wavefront
 
 // Joins the parts of the run that begins in this chunk and goes on in the next
 // ones: a workgroup per chunk and slab, its wavefronts taking the parts in turn.
+template <uint32_t kC>
 __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<float> out) {
-  __shared__ float shared[kJoinWaves][kWave][8];
+  __shared__ float shared[kJoinWaves][kWave][kC];
   const uint32_t chunk = blockIdx.x / a.slabs, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t lo = chunk * a.chunk, hi = lo + a.chunk;  // not the last chunk
   // the keys that decide, in one wait: around both ends, and the first ones of the next 64 chunks
@@ -309,16 +313,16 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
     next += kWave;
     key = next < a.chunks ? a.keys[next * a.chunk] : kNone;
   }
-  const uint64_t col = (uint64_t(blockIdx.x - chunk * a.slabs) * kWave + lane) * kBlockCols;
-  const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
-  float sum[8] = {};
-  Raw8<float> before;
+  const uint64_t col = (uint64_t(blockIdx.x - chunk * a.slabs) * kWave + lane) * kC;
+  const uint32_t width = block_width<kC>(col, a.cols);
+  float sum[kC] = {};
+  Raw<float, kC> before;
   before.zero();
   if (width) {
     if (wave == 0) read_row(a, out, run, col, width, before);
     // part 0 is this chunk's own
     for (uint32_t k0 = wave; k0 <= parts; k0 += kJoinWaves * kJoinBatch) {
-      Raw8<float> part[kJoinBatch];
+      Raw<float, kC> part[kJoinBatch];
 #pragma unroll
       for (uint32_t b = 0; b < kJoinBatch; ++b) {
         const uint32_t k = min(k0 + b * kJoinWaves, parts);
@@ -327,21 +331,21 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
 #pragma unroll
       for (uint32_t b = 0; b < kJoinBatch; ++b) {
         if (k0 + b * kJoinWaves > parts) break;
-        float v[8];
+        float v[kC];
         part[b].widen(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        for (uint32_t e = 0; e < kC; ++e) sum[e] += v[e];
       }
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) shared[wave][lane][e] = sum[e];
+  for (uint32_t e = 0; e < kC; ++e) shared[wave][lane][e] = sum[e];
   __syncthreads();
   if (wave != 0 || !width) return;
 #pragma unroll
   for (uint32_t w = 1; w < kJoinWaves; ++w)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += shared[w][lane][e];
+    for (uint32_t e = 0; e < kC; ++e) sum[e] += shared[w][lane][e];
   finish_row(a, out, run, col, width, sum, before);
 }
 
@@ -359,9 +363,10 @@ constexpr uint32_t kFillMost = 16;                     // rows that a workgroup 
 
 template <typename T, bool kDrop>
 __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, Mat<const T> grad, Mat<float> out) {
+  constexpr uint32_t kC = kLaneCols<T>;
   __shared__ uint64_t masks[kWords];
   __shared__ uint32_t list[kFewMost];
-  __shared__ float shared[kSumWaves][kWave][8];
+  __shared__ float shared[kSumWaves][kWave][kC];
   __shared__ uint32_t seen[kFillMost];
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   uint32_t key[kFewEach];
@@ -407,41 +412,40 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   for (uint32_t p = 0; p < kFewEach; ++p)
     if (key[p] == row) list[before[p]] = p * kSumThreads + threadIdx.x;
   __syncthreads();
-  const uint32_t block = (blockIdx.x - mine * a.slabs) * kWave + lane;
-  const uint64_t col = uint64_t(block) * kBlockCols;
-  const uint32_t width = col >= a.cols ? 0 : uint32_t(a.cols - col < kBlockCols ? a.cols - col : kBlockCols);
-  Raw8<float> held;
+  const uint64_t col = (uint64_t(blockIdx.x - mine * a.slabs) * kWave + lane) * kC;
+  const uint32_t width = block_width<kC>(col, a.cols);
+  Raw<float, kC> held;
   held.zero();
   if (width && wave == 0) read_row(a, out, row, col, width, held);
-  float sum[8] = {};
+  float sum[kC] = {};
   for (uint32_t e0 = wave * kFewBatch; e0 < total; e0 += kSumWaves * kFewBatch) {
     // all loads, then all of the arithmetic without branches, so that the rows' chains of products overlap
-    Raw8<T> raw[kFewBatch];
-    uint32_t bits[kFewBatch][4];
+    Raw<T, kC> raw[kFewBatch];
+    uint32_t bits[kFewBatch][kC / 2];
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
       const uint32_t i = __builtin_amdgcn_readfirstlane(list[min(e0 + b, total - 1)]);
       if (width) raw[b].template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
-      if (kDrop) a.drop.bits(i, block, bits[b]);
+      if (kDrop) a.drop.template bits<kC>(i, col, bits[b]);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
-      float v[8];
+      float v[kC];
       raw[b].widen(v);
-      if (kDrop) a.drop.apply(bits[b], v);
+      if (kDrop) a.drop.template apply<kC>(bits[b], v);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) sum[x] += e0 + b < total ? v[x] : 0.0f;
+      for (uint32_t x = 0; x < kC; ++x) sum[x] += e0 + b < total ? v[x] : 0.0f;
     }
   }
   if (total > kFewBatch) {  // other wavefronts have parts
 #pragma unroll
-    for (int x = 0; x < 8; ++x) shared[wave][lane][x] = sum[x];
+    for (uint32_t x = 0; x < kC; ++x) shared[wave][lane][x] = sum[x];
     __syncthreads();
     if (wave == 0)
 #pragma unroll
       for (uint32_t w = 1; w < kSumWaves; ++w)
 #pragma unroll
-        for (int x = 0; x < 8; ++x) sum[x] += shared[w][lane][x];
+        for (uint32_t x = 0; x < kC; ++x) sum[x] += shared[w][lane][x];
   }
   if (wave == 0 && width) finish_row(a, out, row, col, width, sum, held);
 }
@@ -458,24 +462,25 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
 //     8192    128: 6.9 / 10.2   512: 22 / 13.4     128: 11.8 / 10.5
 constexpr uint64_t kFewJobs = 2048;
 
-uint32_t slabs_of(uint64_t cols) { return uint32_t((cols + kWave * kBlockCols - 1) / (kWave * kBlockCols)); }
+// Slabs of a row: a wavefront's 64 blocks of `block` columns.
+uint64_t slabs_of(uint64_t cols, uint32_t block) { return (cols + kWave * block - 1) / (kWave * block); }
 
-bool is_few(uint64_t n, uint64_t cols) { return n <= kFewMost && n * slabs_of(cols) <= kFewJobs; }
+bool is_few(uint64_t n, uint64_t slabs) { return n <= kFewMost && n * slabs <= kFewJobs; }
 
 // Tokens per chunk: at most kJobs wavefronts in all, but 4 to 64 (one per lane) tokens each.
 constexpr uint64_t kJobs = 4096, kChunkLeast = 4, kChunkMost = kWave;
 
 uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-uint32_t chunk_of(uint64_t n, uint64_t cols) {
-  return uint32_t(std::min(kChunkMost, std::max(kChunkLeast, up(n * slabs_of(cols), kJobs))));
+uint32_t chunk_of(uint64_t n, uint64_t slabs) {
+  return uint32_t(std::min(kChunkMost, std::max(kChunkLeast, up(n * slabs, kJobs))));
 }
 
 // Columns of parts, at most, over all chunks: n / kChunkLeast of them, or where
 // chunks are longer kJobs / slabs, or where those would pass kChunkMost tokens
 // n / kChunkMost.  It grows with n and cols, so a workspace serves smaller calls.
 uint64_t part_cols(uint64_t n, uint64_t cols) {
-  return std::min(up(n, kChunkLeast) * cols, std::max(kJobs * kWave * kBlockCols + cols, up(n, kChunkMost) * cols));
+  return std::min(up(n, kChunkLeast) * cols, std::max(kJobs * kWave * kLaneCols<bf16> + cols, up(n, kChunkMost) * cols));
 }
 
 hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, const uint32_t** keys,
@@ -511,10 +516,10 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   a.rows = rows;
   a.cols = cols;
   a.accumulate = x.accumulate != 0;
-  a.slabs = slabs_of(cols);
+  a.slabs = uint32_t(slabs_of(cols, kLaneCols<T>));
   a.scale = float(x.scale);
   a.drop = drop;
-  if (is_few(n, cols)) {
+  if (is_few(n, a.slabs)) {
     a.sum_wgs = n * a.slabs;
     a.fill_rows = a.slabs == 1 ? kFillMost : kSumWaves;
     const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + a.fill_rows - 1) / a.fill_rows, 1u << 20)));
@@ -525,13 +530,13 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   const hipError_t e = sort_tokens(t, work, w, &a.keys, &a.order, stream);
   if (e != hipSuccess) return e;
   a.parts = reinterpret_cast<float*>(work + w.parts);
-  a.chunk = chunk_of(n, cols);
+  a.chunk = chunk_of(n, a.slabs);
   a.chunks = (n + a.chunk - 1) / a.chunk;
   a.sum_wgs = uint32_t((uint64_t(a.chunks) * a.slabs + kSumWaves - 1) / kSumWaves);
   const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20)));
   if (drop.limit) hipLaunchKernelGGL((sum_kernel<T, true>), wgs, block, 0, stream, a, grad, out);
   else hipLaunchKernelGGL((sum_kernel<T, false>), wgs, block, 0, stream, a, grad, out);
-  hipLaunchKernelGGL(join_kernel, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
+  hipLaunchKernelGGL(join_kernel<kLaneCols<T>>, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
   return hipGetLastError();
 }
 
@@ -555,7 +560,7 @@ EmbedGradSizes embed_grad_sizes(uint64_t n, uint64_t, uint64_t cols) {
 bool embed_grad_fits(uint64_t n, uint64_t cols) {
   constexpr uint64_t lanes = uint64_t(1) << 31;  // of a launch
   // ordering: a workgroup per 64 tokens; sums: one per chunk (or token) and slab in the largest launch
-  const uint64_t jobs = (is_few(n, cols) ? n : up(n, chunk_of(n, cols))) * slabs_of(cols);
+  const uint64_t slabs = slabs_of(cols, kLaneCols<float>), jobs = (is_few(n, slabs) ? n : up(n, chunk_of(n, slabs))) * slabs;
   return up(n, kWave) * kPlaceThreads <= lanes && jobs * kSumThreads <= lanes;
 }
 

@@ -1,18 +1,23 @@
 // ops.hpp -- what the operators of a training step share: matrices as kernels
-// see them, eight-column blocks (the unit of dropout's generator and of a
-// lane's work), and the launchers.
+// see them, the blocks of columns that lanes work on, and the launchers.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "etc.h"
 #include "philox.hpp"
 
 namespace etc {
 
-constexpr uint32_t kBlockCols = 8;  // columns of a lane's block: 16 bytes of bf16, 32 of fp32
+// Columns of a lane's block: 16 bytes of the type that a kernel mostly moves,
+// so that a wavefront's accesses cover whole lines one after the other.  Lanes of
+// eight fp32 columns, two accesses 32 bytes apart each, reached 3.8 TB/s in the
+// dropout backward where bf16 reached 5.0.
+template <typename T>
+constexpr uint32_t kLaneCols = 16 / sizeof(T);
 
 // A matrix of T as a kernel sees it: row i starts at p + i * ld.
 template <typename T>
@@ -30,109 +35,175 @@ struct Ids {
 };
 
 typedef __bf16 bf16;
-typedef uint32_t u32x4_e2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any bf16's address
-typedef uint32_t u32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));  // at any fp32's
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Eight elements of a row as they are in memory, or the n < 8 that a row's last
-// block has.  Loading and widening are apart, so that a kernel can have several
-// rows' loads in flight: a value that is widened where it is loaded, on one side
-// of a branch on n, is waited for right there.  Loads and stores are 16 bytes
-// wide at any element's address: rows of odd widths start anywhere, and the
-// hardware splits what crosses a line.  kStream: non-temporal, for what is not
-// used again by this launch.
+// Words at any element's address: rows of odd widths start anywhere, and the
+// hardware splits what crosses a line.
 template <typename T>
-struct Raw8;
-
+struct Words;
 template <>
-struct Raw8<bf16> {
-  u32x4_e2 w;
+struct Words<bf16> {
+  typedef uint32_t x1 __attribute__((aligned(2)));
+  typedef uint32_t x2 __attribute__((ext_vector_type(2), aligned(2)));
+  typedef uint32_t x4 __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <>
+struct Words<float> {
+  typedef uint32_t x1;
+  typedef uint32_t x2 __attribute__((ext_vector_type(2), aligned(4)));
+  typedef uint32_t x4 __attribute__((ext_vector_type(4), aligned(4)));
+};
+
+// kC (4 or 8) elements of a row as they are in memory, or the n < kC that a row's
+// last block has.  Loading and widening are apart, so that a kernel can have
+// several rows' loads in flight: a value that is widened where it is loaded, on
+// one side of a branch on n, is waited for right there.  A last block moves in
+// pieces of 4, 2 and 1 elements.  kStream: non-temporal, for what is not used
+// again by this launch.
+template <typename T, uint32_t kC>
+struct Raw;
+
+template <uint32_t kC>
+struct Raw<bf16, kC> {
+  static constexpr uint32_t kWords = kC / 2;
+  uint32_t w[kWords];
   template <bool kStream = false>
   __device__ __forceinline__ void load(const bf16* p, uint32_t n) {
-    if (n >= 8) {
-      const auto* q = reinterpret_cast<const u32x4_e2*>(p);
-      if constexpr (kStream) w = __builtin_nontemporal_load(q);
-      else w = *q;
-    } else {  // elements past the end repeat the last one
-      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    using V = typename std::conditional<kC == 8, Words<bf16>::x4, Words<bf16>::x2>::type;
+    if (n >= kC) {
+      const V* q = reinterpret_cast<const V*>(p);
+      V v;
+      if constexpr (kStream) v = __builtin_nontemporal_load(q);
+      else v = *q;
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e)
-        w[e] = q[2 * e < n ? 2 * e : n - 1] | uint32_t(q[2 * e + 1 < n ? 2 * e + 1 : n - 1]) << 16;
+      for (uint32_t e = 0; e < kWords; ++e) w[e] = v[e];
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+      Words<bf16>::x2 four = 0;
+      uint32_t two = 0, one = 0;
+      if (kC == 8 && (n & 4)) four = *reinterpret_cast<const Words<bf16>::x2*>(q);
+      if (n & 2) two = *reinterpret_cast<const Words<bf16>::x1*>(q + (n & 4));
+      if (n & 1) one = q[n & 6];
+      const uint32_t low = n & 2 ? two : one, high = n & 2 ? one : 0;  // the last 1 to 3
+      const uint32_t f0 = four[0], f1 = four[1];
+      w[0] = n & 4 ? f0 : low;
+      w[1] = n & 4 ? f1 : high;
+      if constexpr (kC == 8) w[2] = low, w[3] = high;
     }
   }
-  __device__ __forceinline__ void zero() { w = 0; }
-  __device__ __forceinline__ void widen(float (&v)[8]) const {
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (uint32_t e = 0; e < kWords; ++e) w[e] = 0;
+  }
+  __device__ __forceinline__ void widen(float (&v)[kC]) const {
+#pragma unroll
+    for (uint32_t e = 0; e < kWords; ++e) {
       v[2 * e] = __uint_as_float(w[e] << 16);
       v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
     }
   }
+  // rounds to nearest even
+  __device__ __forceinline__ void narrow(const float (&v)[kC]) {
+#pragma unroll
+    for (uint32_t e = 0; e < kWords; ++e)
+      w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
+  }
+  template <bool kStream = false>
+  __device__ __forceinline__ void store(bf16* p, uint32_t n) const {
+    using V = typename std::conditional<kC == 8, Words<bf16>::x4, Words<bf16>::x2>::type;
+    if (n >= kC) {
+      V v;
+#pragma unroll
+      for (uint32_t e = 0; e < kWords; ++e) v[e] = w[e];
+      V* q = reinterpret_cast<V*>(p);
+      if constexpr (kStream) __builtin_nontemporal_store(v, q);
+      else *q = v;
+    } else {
+      uint16_t* q = reinterpret_cast<uint16_t*>(p);
+      if (kC == 8 && (n & 4)) *reinterpret_cast<Words<bf16>::x2*>(q) = Words<bf16>::x2{w[0], w[1]};
+      // copies: a choice between elements of an array would be one between their addresses
+      const uint32_t w0 = w[0], w1 = w[1], w2 = w[kWords - 2], w3 = w[kWords - 1];
+      const uint32_t low = n & 4 ? w2 : w0, high = n & 4 ? w3 : w1;
+      if (n & 2) *reinterpret_cast<Words<bf16>::x1*>(q + (n & 4)) = low;
+      if (n & 1) q[n & 6] = uint16_t(n & 2 ? high : low);
+    }
+  }
 };
 
-template <>
-struct Raw8<float> {
-  u32x4_e4 a, b;
+template <uint32_t kC>
+struct Raw<float, kC> {
+  uint32_t w[kC];
   template <bool kStream = false>
   __device__ __forceinline__ void load(const float* p, uint32_t n) {
-    if (n >= 8) {
-      const auto *q = reinterpret_cast<const u32x4_e4*>(p), *r = reinterpret_cast<const u32x4_e4*>(p + 4);
-      if constexpr (kStream) a = __builtin_nontemporal_load(q), b = __builtin_nontemporal_load(r);
-      else a = *q, b = *r;
+    using V = Words<float>::x4;
+    if (n >= kC) {
+#pragma unroll
+      for (uint32_t h = 0; h < kC / 4; ++h) {
+        const V* q = reinterpret_cast<const V*>(p + 4 * h);
+        V v;
+        if constexpr (kStream) v = __builtin_nontemporal_load(q);
+        else v = *q;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) w[4 * h + e] = v[e];
+      }
     } else {
       const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+      V four = 0;
+      Words<float>::x2 two = 0;
+      uint32_t one = 0;
+      if (kC == 8 && (n & 4)) four = *reinterpret_cast<const V*>(q);
+      if (n & 2) two = *reinterpret_cast<const Words<float>::x2*>(q + (n & 4));
+      if (n & 1) one = q[n & 6];
+      const uint32_t tail[4] = {n & 2 ? two[0] : one, two[1], one, 0};  // the last 1 to 3
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) {
-        a[e] = q[e < n ? e : n - 1];
-        b[e] = q[e + 4 < n ? e + 4 : n - 1];
+        const uint32_t f = four[e], t = tail[e];
+        w[e] = n & 4 ? f : t;
+        if constexpr (kC == 8) w[4 + e] = t;
       }
     }
   }
-  __device__ __forceinline__ void zero() { a = 0, b = 0; }
-  __device__ __forceinline__ void widen(float (&v)[8]) const {
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = __uint_as_float(a[e]);
-      v[e + 4] = __uint_as_float(b[e]);
+    for (uint32_t e = 0; e < kC; ++e) w[e] = 0;
+  }
+  __device__ __forceinline__ void widen(float (&v)[kC]) const {
+#pragma unroll
+    for (uint32_t e = 0; e < kC; ++e) v[e] = __uint_as_float(w[e]);
+  }
+  __device__ __forceinline__ void narrow(const float (&v)[kC]) {
+#pragma unroll
+    for (uint32_t e = 0; e < kC; ++e) w[e] = __float_as_uint(v[e]);
+  }
+  template <bool kStream = false>
+  __device__ __forceinline__ void store(float* p, uint32_t n) const {
+    using V = Words<float>::x4;
+    if (n >= kC) {
+#pragma unroll
+      for (uint32_t h = 0; h < kC / 4; ++h) {
+        const V v{w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
+        V* q = reinterpret_cast<V*>(p + 4 * h);
+        if constexpr (kStream) __builtin_nontemporal_store(v, q);
+        else *q = v;
+      }
+    } else {
+      uint32_t* q = reinterpret_cast<uint32_t*>(p);
+      if (kC == 8 && (n & 4)) *reinterpret_cast<V*>(q) = V{w[0], w[1], w[2], w[3]};
+      // copies: a choice between elements of an array would be one between their addresses
+      const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w4 = w[kC - 4], w5 = w[kC - 3], w6 = w[kC - 2];
+      const uint32_t t0 = n & 4 ? w4 : w0, t1 = n & 4 ? w5 : w1, t2 = n & 4 ? w6 : w2;
+      if (n & 2) *reinterpret_cast<Words<float>::x2*>(q + (n & 4)) = Words<float>::x2{t0, t1};
+      if (n & 1) q[n & 6] = n & 2 ? t2 : t0;
     }
   }
 };
 
-// Rounds to nearest even, once: v holds the whole result in 32 bits.
-template <bool kStream = false>
-__device__ __forceinline__ void store8(bf16* p, uint32_t n, const float (&v)[8]) {
-  if (n >= 8) {
-    u32x4_e2 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
-    auto* q = reinterpret_cast<u32x4_e2*>(p);
-    if constexpr (kStream) __builtin_nontemporal_store(w, q);
-    else *q = w;
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e)
-      if (e < n) p[e] = bf16(v[e]);
-  }
-}
-template <bool kStream = false>
-__device__ __forceinline__ void store8(float* p, uint32_t n, const float (&v)[8]) {
-  if (n >= 8) {
-    u32x4_e4 a, b;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      a[e] = __float_as_uint(v[e]);
-      b[e] = __float_as_uint(v[e + 4]);
-    }
-    auto *q = reinterpret_cast<u32x4_e4*>(p), *r = reinterpret_cast<u32x4_e4*>(p + 4);
-    if constexpr (kStream) __builtin_nontemporal_store(a, q), __builtin_nontemporal_store(b, r);
-    else *q = a, *r = b;
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e)
-      if (e < n) p[e] = v[e];
-  }
+template <bool kStream = false, typename T, uint32_t kC>
+__device__ __forceinline__ void store_block(T* p, uint32_t n, const float (&v)[kC]) {
+  Raw<T, kC> raw;
+  raw.narrow(v);
+  raw.template store<kStream>(p, n);
 }
 
 // Division of n < 2^31 by d >= 1 as a product (Granlund and Montgomery, "Division
@@ -147,27 +218,31 @@ struct Divisor {
   __host__ __device__ uint32_t div(uint32_t n) const { return uint32_t((((uint64_t(n) * m) >> 32) + n) >> s); }
 };
 
-inline uint32_t blocks_per_row(int64_t cols) { return uint32_t((cols + kBlockCols - 1) / kBlockCols); }
+inline uint32_t blocks_per_row(int64_t cols, uint32_t block) { return uint32_t((cols + block - 1) / block); }
 
-// An elementwise launch: a lane has one eight-column block of `per` consecutive
-// rows.  Lanes are numbered along the row, then down the groups of rows.
+// Columns of the block of kC that begins at `col`, 0 past the matrix.
+template <uint32_t kC>
+__device__ __forceinline__ uint32_t block_width(uint64_t col, uint32_t cols) {
+  return col >= cols ? 0 : cols - col < kC ? uint32_t(cols - col) : kC;
+}
+
+// An elementwise launch: a lane has one block of `per` consecutive rows.
+// Lanes are numbered along the row, then down the groups of rows.
 struct BlockGrid {
   uint32_t n;  // lanes with work, < 2^31
   uint32_t rows, cols;
   Divisor per_row;
-  // lane `at`: its group of rows, its block's number in the row, and how many columns that has
-  __device__ __forceinline__ void place(uint32_t at, uint32_t* group, uint32_t* block, uint32_t* width) const {
+  // lane `at`: its group of rows and its block's number in the row
+  __device__ __forceinline__ void place(uint32_t at, uint32_t* group, uint32_t* block) const {
     *group = per_row.div(at);
     *block = at - *group * per_row.d;
-    const uint32_t left = cols - *block * kBlockCols;
-    *width = left < kBlockCols ? left : kBlockCols;
   }
 };
 
 // Calls launch(first row, grid) for runs of rows of fewer than 2^31 lanes, until one fails.
 template <typename F>
-hipError_t for_row_runs(int64_t rows, int64_t cols, uint32_t per, F launch) {
-  const uint32_t nb = blocks_per_row(cols);
+hipError_t for_row_runs(int64_t rows, int64_t cols, uint32_t block, uint32_t per, F launch) {
+  const uint32_t nb = blocks_per_row(cols, block);
   const int64_t most = INT32_MAX / int64_t(nb) * per;
   for (int64_t at = 0; at < rows; at += most) {
     const int64_t n = rows - at < most ? rows - at : most;

@@ -40,23 +40,29 @@ struct Drop {
   uint64_t row0;
   float scale;  // of what is kept: 65536 / (65536 - limit)
 
-  // the eight 16-bit numbers of columns 8 * block .. 8 * block + 7 of row i, two to a word
-  __host__ __device__ void bits(uint64_t i, uint32_t block, uint32_t (&w)[4]) const {
+  // The 16-bit numbers of columns col .. col + kC - 1 (a multiple of kC) of row i, two to a word.
+  template <uint32_t kC>
+  __host__ __device__ void bits(uint64_t i, uint64_t col, uint32_t (&w)[kC / 2]) const {
     const uint64_t r = row0 + i;
-    w[0] = block;
-    w[1] = uint32_t(r);
-    w[2] = uint32_t(r >> 32);
-    w[3] = call;
-    philox4x32_10(w, k0, k1);
+    uint32_t c[4] = {uint32_t(col / 8), uint32_t(r), uint32_t(r >> 32), call};
+    philox4x32_10(c, k0, k1);
+    const uint32_t c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+    if constexpr (kC == 8) {
+      w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+    } else {
+      w[0] = col & 4 ? c2 : c0;
+      w[1] = col & 4 ? c3 : c1;
+    }
   }
   // v scaled where kept and 0 where dropped, whatever it is (a product with 0
   // would keep NaN); limit >= 1.  A number is in the upper half of a word for the
   // comparison: below the limit where the word is at most (limit << 16) - 1,
   // which for 65536 is any word, whatever the lower half holds.
-  __device__ __forceinline__ void apply(const uint32_t (&w)[4], float (&v)[8]) const {
+  template <uint32_t kC>
+  __device__ __forceinline__ void apply(const uint32_t (&w)[kC / 2], float (&v)[kC]) const {
     const uint32_t top = (limit << 16) - 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (e % 2 ? w[e / 2] : w[e / 2] << 16) > top ? v[e] * scale : 0.0f;
+    for (uint32_t e = 0; e < kC; ++e) v[e] = (e % 2 ? w[e / 2] : w[e / 2] << 16) > top ? v[e] * scale : 0.0f;
   }
 };
 

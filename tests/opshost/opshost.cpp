@@ -41,9 +41,9 @@ int main(int argc, char** argv) {
         if (n <= 0x7FFFFFFFu && by.div(n) != n / d) ++bad;
     }
     printf("%llu\n", (unsigned long long)bad);
-  } else if (!strcmp(argv[1], "runs") && argc == 5) {
+  } else if (!strcmp(argv[1], "runs") && argc == 6) {
     const int64_t rows = atoll(argv[2]), cols = atoll(argv[3]);
-    (void)etc::for_row_runs(rows, cols, uint32_t(atoi(argv[4])), [&](int64_t first, const etc::BlockGrid& g) -> hipError_t {
+    (void)etc::for_row_runs(rows, cols, uint32_t(atoi(argv[4])), uint32_t(atoi(argv[5])), [&](int64_t first, const etc::BlockGrid& g) -> hipError_t {
       printf("%lld %u %u %u %u\n", (long long)first, g.n, g.rows, g.cols, g.per_row.d);
       return hipSuccess;
     });

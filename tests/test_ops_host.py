@@ -74,10 +74,10 @@ def test_division(host):
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1000, 8), (1, (1 << 31) - 1), ((1 << 31) - 1, 8), ((1 << 31) - 1, 4097),
                                        (3, (1 << 31) - 1)])
-@pytest.mark.parametrize("per", (1, 2))
-def test_launches_cover_the_rows(host, rows, cols, per):
-    nb, at = -(-cols // 8), 0
-    for line in host("runs", rows, cols, per).splitlines():
+@pytest.mark.parametrize("block,per", ((8, 1), (8, 2), (4, 1)))
+def test_launches_cover_the_rows(host, rows, cols, block, per):
+    nb, at = -(-cols // block), 0
+    for line in host("runs", rows, cols, block, per).splitlines():
         first, n, run, c, d = map(int, line.split())
         assert first == at and c == cols and d == nb
         assert n == -(-run // per) * nb and 0 < n < 2 ** 31
