@@ -18,7 +18,7 @@ namespace {
 constexpr uint32_t kFlatThreads = 64;  // elementwise launches: 31.3 us where 256 took 32.0 (16384 x 2048, bf16)
 constexpr uint32_t kThreads = 256;     // launches that sum
 
-template <typename T, bool kDrop>
+template <typename T, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kFlatThreads) void dropout_kernel(BlockGrid grid, Drop drop, Mat<const T> x, const T* bias,
                                                            Mat<const T> residual, Mat<T> out) {
   const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
@@ -28,24 +28,26 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_kernel(BlockGrid grid, D
   grid.place(at, &i, &block);
   const uint64_t col = uint64_t(block) * kC;
   const uint32_t width = block_width<kC>(col, grid.cols);
-  Raw<T, kC> rx, rb, rr;
+  const bool shorter = grid.cols < kC;
+  Raw<T, kC, kWhole> rx, rb, rr;
   rb.zero();
   rr.zero();
-  rx.template load<true>(x.p + int64_t(i) * x.ld + col, width);
-  if (residual.p) rr.template load<true>(residual.p + int64_t(i) * residual.ld + col, width);
-  if (bias) rb.load(bias + col, width);
+  rx.template load<true>(x.p + int64_t(i) * x.ld + col, width, shorter);
+  if (residual.p) rr.template load<true>(residual.p + int64_t(i) * residual.ld + col, width, shorter);
+  if (bias) rb.load(bias + col, width, shorter);
+  compiler_fence();
   uint32_t bits[kC / 2];
   if (kDrop) drop.template bits<kC>(i, col, bits);  // while the loads are on their way
   float v[kC], w[kC];
-  rx.widen(v);
-  rb.widen(w);
+  rx.widen(v, width);
+  rb.widen(w, width);
 #pragma unroll
   for (uint32_t e = 0; e < kC; ++e) v[e] += w[e];
   if (kDrop) drop.template apply<kC>(bits, v);
-  rr.widen(w);
+  rr.widen(w, width);
 #pragma unroll
   for (uint32_t e = 0; e < kC; ++e) v[e] += w[e];
-  store_block<true>(out.p + int64_t(i) * out.ld + col, width, v);
+  store_block<kWhole, true>(out.p + int64_t(i) * out.ld + col, width, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -79,7 +81,7 @@ GradShape grad_shape(uint32_t rows, uint32_t cols, uint32_t block) {
   return g;
 }
 
-template <typename T, bool kDrop>
+template <typename T, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Drop drop, Mat<const T> grad, Mat<T> dx,
                                                                 float* partial) {
   constexpr uint32_t kC = kLaneCols<T>;
@@ -89,15 +91,17 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
   const uint32_t width = block_width<kC>(col, g.cols);
   const uint32_t down = kThreads >> g.lane_bits;
   const uint32_t end = uint32_t(min(uint64_t(g.rows), (uint64_t(part) + 1) * g.step));
+  const bool shorter = g.cols < kC;
   float sum[kC] = {};
   if (width) {
     for (uint64_t i0 = uint64_t(part) * g.step + (threadIdx.x >> g.lane_bits); i0 < end; i0 += down * kBatch) {
-      Raw<T, kC> raw[kBatch];
+      Raw<T, kC, kWhole> raw[kBatch];
 #pragma unroll
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
-        raw[b].load(grad.p + int64_t(i < end ? i : i0) * grad.ld + col, width);
+        raw[b].load(grad.p + int64_t(i < end ? i : i0) * grad.ld + col, width, shorter);
       }
+      compiler_fence();
 #pragma unroll
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
@@ -105,11 +109,11 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
         uint32_t bits[kC / 2];
         if (kDrop) drop.template bits<kC>(i, col, bits);
         float v[kC];
-        raw[b].widen(v);
+        raw[b].widen(v, width);
         if (kDrop) drop.template apply<kC>(bits, v);
 #pragma unroll
         for (uint32_t e = 0; e < kC; ++e) sum[e] += v[e];
-        store_block<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
+        store_block<kWhole, true>(dx.p + int64_t(i) * dx.ld + col, width, v);
       }
     }
   }
@@ -125,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
 }
 
 // dx alone
-template <typename T, bool kDrop>
+template <typename T, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kFlatThreads) void dropout_dx_kernel(BlockGrid grid, Drop drop, Mat<const T> grad, Mat<T> dx) {
   const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
   if (at >= grid.n) return;
@@ -134,14 +138,16 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_dx_kernel(BlockGrid grid
   grid.place(at, &i, &block);
   const uint64_t col = uint64_t(block) * kC;
   const uint32_t width = block_width<kC>(col, grid.cols);
-  Raw<T, kC> raw;
-  raw.template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
+  const bool shorter = grid.cols < kC;
+  Raw<T, kC, kWhole> raw;
+  raw.template load<true>(grad.p + int64_t(i) * grad.ld + col, width, shorter);
+  compiler_fence();
   uint32_t bits[kC / 2];
   if (kDrop) drop.template bits<kC>(i, col, bits);
   float v[kC];
-  raw.widen(v);
+  raw.widen(v, width);
   if (kDrop) drop.template apply<kC>(bits, v);
-  store_block<true>(dx.p + int64_t(i) * dx.ld + col, width, v);
+  store_block<kWhole, true>(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 
 constexpr uint32_t kJoinCols = 16, kJoinRows = 64, kJoinBatch = 8;
@@ -175,6 +181,9 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float
 
 template <typename T>
 hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream_t stream) {
+  const bool whole = whole_blocks(a.x.cols, kLaneCols<T>);
+  const auto kernel = drop.limit ? whole ? dropout_kernel<T, true, true> : dropout_kernel<T, false, true>
+                                 : whole ? dropout_kernel<T, true, false> : dropout_kernel<T, false, false>;
   return for_row_runs(a.x.rows, a.x.cols, kLaneCols<T>, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto at = [&](const etc_matrix& m) {
       return Mat<T>{m.data ? static_cast<T*>(m.data) + first * m.ld : nullptr, m.ld};
@@ -184,26 +193,23 @@ hipError_t launch_forward(const etc_dropout_args& a, const Drop& drop, hipStream
     Drop d = drop;
     d.row0 += uint64_t(first);
     const dim3 wgs((grid.n + kFlatThreads - 1) / kFlatThreads), block(kFlatThreads);
-#define ETC_DROPOUT(...)                                                                                          \
-  hipLaunchKernelGGL((dropout_kernel<T, __VA_ARGS__>), wgs, block, 0, stream, grid, d, Mat<const T>{x.p, x.ld}, bias, \
-                     Mat<const T>{r.p, r.ld}, out)
-    if (drop.limit) ETC_DROPOUT(true);
-    else ETC_DROPOUT(false);
-#undef ETC_DROPOUT
+    hipLaunchKernelGGL(kernel, wgs, block, 0, stream, grid, d, Mat<const T>{x.p, x.ld}, bias, Mat<const T>{r.p, r.ld}, out);
     return hipGetLastError();
   });
 }
 
 template <typename T>
 hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
+  const bool whole = whole_blocks(a.grad.cols, kLaneCols<T>);
+  const auto kernel = drop.limit ? whole ? dropout_dx_kernel<T, true, true> : dropout_dx_kernel<T, false, true>
+                                 : whole ? dropout_dx_kernel<T, true, false> : dropout_dx_kernel<T, false, false>;
   return for_row_runs(a.grad.rows, a.grad.cols, kLaneCols<T>, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     const Mat<const T> grad{static_cast<const T*>(a.grad.data) + first * a.grad.ld, a.grad.ld};
     const Mat<T> dx{static_cast<T*>(a.dx.data) + first * a.dx.ld, a.dx.ld};
     Drop d = drop;
     d.row0 += uint64_t(first);
     const dim3 wgs((grid.n + kFlatThreads - 1) / kFlatThreads), block(kFlatThreads);
-    if (drop.limit) hipLaunchKernelGGL((dropout_dx_kernel<T, true>), wgs, block, 0, stream, grid, d, grad, dx);
-    else hipLaunchKernelGGL((dropout_dx_kernel<T, false>), wgs, block, 0, stream, grid, d, grad, dx);
+    hipLaunchKernelGGL(kernel, wgs, block, 0, stream, grid, d, grad, dx);
     return hipGetLastError();
   });
 }
@@ -217,10 +223,10 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
     const dim3 wgs(g.parts * g.slabs), block(kThreads);
     const Mat<const T> grad{static_cast<const T*>(a.grad.data), a.grad.ld};
     const Mat<T> dx{static_cast<T*>(a.dx.data), a.dx.ld};
-    if (drop.limit)
-      hipLaunchKernelGGL((dropout_grad_kernel<T, true>), wgs, block, 0, stream, g, drop, grad, dx, partial);
-    else
-      hipLaunchKernelGGL((dropout_grad_kernel<T, false>), wgs, block, 0, stream, g, drop, grad, dx, partial);
+    const bool whole = whole_blocks(g.cols, kLaneCols<T>);
+    const auto kernel = drop.limit ? whole ? dropout_grad_kernel<T, true, true> : dropout_grad_kernel<T, false, true>
+                                   : whole ? dropout_grad_kernel<T, true, false> : dropout_grad_kernel<T, false, false>;
+    hipLaunchKernelGGL(kernel, wgs, block, 0, stream, g, drop, grad, dx, partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -27,7 +27,7 @@ struct EmbedArgs {
   BlockGrid grid;
 };
 
-template <typename T, typename O, bool kDrop, uint32_t kN>
+template <typename T, typename O, bool kWhole, bool kDrop, uint32_t kN>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> out) {
   const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
   if (at >= a.grid.n) return;
@@ -36,35 +36,43 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs<T> a, Mat<O> 
   a.grid.place(at, &group, &block);
   const uint64_t col = uint64_t(block) * kC;
   const uint32_t width = block_width<kC>(col, a.grid.cols), i0 = group * kN, last = a.grid.rows - 1;
+  const bool shorter = a.grid.cols < kC;
   uint64_t k[kN], q[kN] = {};
 #pragma unroll
   for (uint32_t r = 0; r < kN; ++r) {
-    const uint32_t i = min(i0 + r, last);
+    const uint32_t i = kN == 1 ? i0 : min(i0 + r, last);
     k[r] = uint64_t(a.tokens.at(i)) - uint64_t(a.row0);  // unsigned: an id below row0 becomes a large row
     if (a.pos.p) q[r] = uint64_t(a.positions.at(i));
   }
-  Raw<T, kC> word[kN], place[kN];
+  Raw<T, kC, kWhole> word[kN], place[kN];
 #pragma unroll
   for (uint32_t r = 0; r < kN; ++r) {
     word[r].zero();
     place[r].zero();
-    if (k[r] < a.rows) word[r].load(a.table.p + int64_t(k[r]) * a.table.ld + col, width);
-    if (q[r] < a.pos_rows) place[r].load(a.pos.p + int64_t(q[r]) * a.pos.ld + col, width);
+    if (k[r] < a.rows) word[r].load(a.table.p + int64_t(k[r]) * a.table.ld + col, width, shorter);
+    if (q[r] < a.pos_rows) place[r].load(a.pos.p + int64_t(q[r]) * a.pos.ld + col, width, shorter);
   }
+  compiler_fence();
 #pragma unroll
   for (uint32_t r = 0; r < kN; ++r) {
     const uint32_t i = i0 + r;
-    if (i > last) break;
+    if (kN > 1 && i > last) break;
     uint32_t bits[kC / 2];
     if (kDrop) a.drop.template bits<kC>(i, col, bits);  // while the loads are on their way
     float v[kC], w[kC];
-    word[r].widen(v);
-    place[r].widen(w);
+    word[r].widen(v, width);
+    place[r].widen(w, width);
 #pragma unroll
     for (uint32_t e = 0; e < kC; ++e) v[e] = v[e] * a.scale + w[e];
     if (kDrop) a.drop.template apply<kC>(bits, v);
-    store_block<true>(out.p + int64_t(i) * out.ld + col, width, v);
+    compiler_fence();
+    store_block<kWhole, true>(out.p + int64_t(i) * out.ld + col, width, v);
   }
+}
+
+template <typename T, typename O, bool kWhole>
+auto kernel_for(bool drop, bool two) {
+  return two ? embed_kernel<T, O, kWhole, true, 2> : drop ? embed_kernel<T, O, kWhole, true, 1> : embed_kernel<T, O, kWhole, false, 1>;
 }
 
 template <typename T, typename O>
@@ -80,6 +88,8 @@ hipError_t launch(const etc_embed_args& x, const Drop& drop, hipStream_t stream)
   // second row's loads: 16384 x 2048 with positions and dropout 20.5 us, with one
   // row 22.4; 8192 x 8192 without dropout 22.5 us, with one row 20.8.
   const bool two = drop.limit && uint64_t(x.out.rows) * blocks_per_row(x.out.cols, kLaneCols<O>) >= kManyBlocks;
+  const auto kernel = whole_blocks(x.out.cols, kLaneCols<O>) ? kernel_for<T, O, true>(drop.limit, two)
+                                                             : kernel_for<T, O, false>(drop.limit, two);
   return for_row_runs(x.out.rows, x.out.cols, kLaneCols<O>, two ? 2 : 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
     auto ids = [&](const etc_ids& v) {
       const bool wide = v.dtype == ETC_IDS_I64;
@@ -92,11 +102,7 @@ hipError_t launch(const etc_embed_args& x, const Drop& drop, hipStream_t stream)
     a.grid = grid;
     const Mat<O> out{static_cast<O*>(x.out.data) + first * x.out.ld, x.out.ld};
     const dim3 wgs((grid.n + kThreads - 1) / kThreads), block(kThreads);
-#define ETC_EMBED(...) hipLaunchKernelGGL((embed_kernel<T, O, __VA_ARGS__>), wgs, block, 0, stream, a, out)
-    if (two) ETC_EMBED(true, 2);
-    else if (drop.limit) ETC_EMBED(true, 1);
-    else ETC_EMBED(false, 1);
-#undef ETC_EMBED
+    hipLaunchKernelGGL(kernel, wgs, block, 0, stream, a, out);
     return hipGetLastError();
   });
 }

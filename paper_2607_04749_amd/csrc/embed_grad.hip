@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kPlaceThreads) void merge_kernel(uint32_t n, uint32
 
 constexpr uint32_t kSumThreads = 256;
 constexpr uint32_t kSumWaves = kSumThreads / kWave;
-constexpr uint32_t kBatch = 4;  // rows in flight per wavefront
+constexpr uint32_t kAddBatch = 4, kSetBatch = 8;  // rows in flight per wavefront
 
 struct SumArgs {
   const uint32_t *keys, *order;
@@ -173,21 +173,21 @@ struct SumArgs {
   Drop drop;
 };
 
-// A row of the table that a run ends in: what it holds, read early, and then the whole of it.
-template <uint32_t kC>
+// A row of the table that a run ends in: what it holds (kAdd; read early) and the sum.
+template <bool kAdd, bool kWhole, uint32_t kC>
 __device__ __forceinline__ void finish_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
-                                           uint32_t width, const float (&sum)[kC], const Raw<float, kC>& before) {
-  float v[kC];
-  before.widen(v);
+                                           uint32_t width, const float (&sum)[kC], const Raw<float, kC, kWhole>& before) {
+  float v[kC] = {};
+  if (kAdd) before.widen(v, width);
 #pragma unroll
   for (uint32_t e = 0; e < kC; ++e) v[e] += sum[e] * a.scale;
-  store_block(out.p + int64_t(row) * out.ld + col, width, v);
+  store_block<kWhole>(out.p + int64_t(row) * out.ld + col, width, v);
 }
 
-template <uint32_t kC>
+template <bool kWhole, uint32_t kC>
 __device__ __forceinline__ void read_row(const SumArgs& a, const Mat<float>& out, uint32_t row, uint64_t col,
-                                         uint32_t width, Raw<float, kC>& before) {
-  if (a.accumulate) before.load(out.p + int64_t(row) * out.ld + col, width);
+                                         uint32_t width, Raw<float, kC, kWhole>& before) {
+  if (a.accumulate) before.load(out.p + int64_t(row) * out.ld + col, width, a.cols < kC);
   else before.zero();
 }
 
@@ -210,7 +210,7 @@ __device__ __forceinline__ void zero_row(const SumArgs& a, const Mat<float>& out
   constexpr uint32_t kC = kLaneCols<float>;
   const float zero[kC] = {};
   for (uint64_t col = lane * kC; col < a.cols; col += kWave * kC)
-    store_block(out.p + int64_t(row) * out.ld + col, block_width<kC>(col, a.cols), zero);
+    store_block<false>(out.p + int64_t(row) * out.ld + col, block_width<kC>(col, a.cols), zero);
 }
 
 // Zeros in the rows of no token, a wavefront per row.
@@ -223,9 +223,9 @@ __device__ __forceinline__ void fill_rows(const SumArgs& a, const Mat<float>& ou
   }
 }
 
-template <typename T, bool kDrop>
+template <typename T, bool kWhole, bool kDrop, bool kAdd>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T> grad, Mat<float> out) {
-  constexpr uint32_t kC = kLaneCols<T>;
+  constexpr uint32_t kC = kLaneCols<T>, kBatch = kAdd ? kAddBatch : kSetBatch;
   if (blockIdx.x >= a.sum_wgs) {
     fill_rows(a, out);
     return;
@@ -249,20 +249,25 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   const uint32_t width = block_width<kC>(col, a.cols);
   float* parts = a.parts + uint64_t(chunk) * 2 * a.cols + col;
   float sum[kC] = {};
+  // lanes past the columns load block 0, so that the loads are in one piece of code without branches
+  const uint64_t from = width ? col : 0;
+  const uint32_t span = width ? width : block_width<kC>(0, a.cols);
   for (uint32_t e0 = 0; e0 < inside; e0 += kBatch) {
     uint32_t i[kBatch], row[kBatch];
-    Raw<T, kC> raw[kBatch];
-    Raw<float, kC> before[kBatch];
+    Raw<T, kC, kWhole> raw[kBatch];
+    Raw<float, kC, kWhole> before[kBatch];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t e = min(e0 + b, inside - 1);
       i[b] = __builtin_amdgcn_readlane(token, e);
       row[b] = __builtin_amdgcn_readlane(key, e);
-      if (width) raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + col, width);
+      raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + from, span, a.cols < kC);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b)
-      if (width && e0 + b < inside && (ends >> (e0 + b) & 1) && e0 + b != came) read_row(a, out, row[b], col, width, before[b]);
+      if (kAdd && e0 + b < inside && (ends >> (e0 + b) & 1) && e0 + b != came)
+        before[b].load(out.p + int64_t(row[b]) * out.ld + from, span, a.cols < kC);
+    compiler_fence();
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t e = e0 + b;
@@ -270,14 +275,14 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
       uint32_t bits[kC / 2];
       if (kDrop) a.drop.template bits<kC>(i[b], col, bits);
       float v[kC];
-      raw[b].widen(v);
+      raw[b].widen(v, width);
       if (kDrop) a.drop.template apply<kC>(bits, v);
 #pragma unroll
       for (uint32_t x = 0; x < kC; ++x) sum[x] += v[x];
       if (ends >> e & 1) {
         if (width) {
-          if (e == came) store_block(parts, width, sum);
-          else finish_row(a, out, row[b], col, width, sum, before[b]);
+          if (e == came) store_block<kWhole>(parts, width, sum);
+          else finish_row<kAdd>(a, out, row[b], col, width, sum, before[b]);
         }
 #pragma unroll
         for (uint32_t x = 0; x < kC; ++x) sum[x] = 0.0f;
@@ -285,7 +290,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
     }
   }
   // a run that goes on: part 0 where it fills the chunk and came in, else part 1
-  if (!(ends >> (inside - 1) & 1) && width) store_block(parts + (came == inside ? 0 : a.cols), width, sum);
+  if (!(ends >> (inside - 1) & 1) && width) store_block<kWhole>(parts + (came == inside ? 0 : a.cols), width, sum);
 }
 
 constexpr uint32_t kJoinWaves = 4;
@@ -293,7 +298,7 @@ constexpr uint32_t kJoinBatch = 4;  // parts in flight per wavefront
 
 // Joins the parts of the run that begins in this chunk and goes on in the next
 // ones: a workgroup per chunk and slab, its wavefronts taking the parts in turn.
-template <uint32_t kC>
+template <bool kWhole, uint32_t kC>
 __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<float> out) {
   __shared__ float shared[kJoinWaves][kWave][kC];
   const uint32_t chunk = blockIdx.x / a.slabs, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -316,23 +321,24 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
   const uint64_t col = (uint64_t(blockIdx.x - chunk * a.slabs) * kWave + lane) * kC;
   const uint32_t width = block_width<kC>(col, a.cols);
   float sum[kC] = {};
-  Raw<float, kC> before;
+  Raw<float, kC, kWhole> before;
   before.zero();
   if (width) {
     if (wave == 0) read_row(a, out, run, col, width, before);
     // part 0 is this chunk's own
     for (uint32_t k0 = wave; k0 <= parts; k0 += kJoinWaves * kJoinBatch) {
-      Raw<float, kC> part[kJoinBatch];
+      Raw<float, kC, kWhole> part[kJoinBatch];
 #pragma unroll
       for (uint32_t b = 0; b < kJoinBatch; ++b) {
         const uint32_t k = min(k0 + b * kJoinWaves, parts);
-        part[b].load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width);
+        part[b].load(a.parts + (uint64_t(chunk + k) * 2 + (k == 0)) * a.cols + col, width, a.cols < kC);
       }
+      compiler_fence();
 #pragma unroll
       for (uint32_t b = 0; b < kJoinBatch; ++b) {
         if (k0 + b * kJoinWaves > parts) break;
         float v[kC];
-        part[b].widen(v);
+        part[b].widen(v, width);
 #pragma unroll
         for (uint32_t e = 0; e < kC; ++e) sum[e] += v[e];
       }
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
   for (uint32_t w = 1; w < kJoinWaves; ++w)
 #pragma unroll
     for (uint32_t e = 0; e < kC; ++e) sum[e] += shared[w][lane][e];
-  finish_row(a, out, run, col, width, sum, before);
+  finish_row<true>(a, out, run, col, width, sum, before);
 }
 
 // ---------------------------------------------------------------------------
@@ -361,7 +367,7 @@ constexpr uint32_t kFewBatch = 2;                      // rows in flight per wav
 constexpr uint32_t kWords = kFewMost / kWave;
 constexpr uint32_t kFillMost = 16;                     // rows that a workgroup looks for
 
-template <typename T, bool kDrop>
+template <typename T, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, Mat<const T> grad, Mat<float> out) {
   constexpr uint32_t kC = kLaneCols<T>;
   __shared__ uint64_t masks[kWords];
@@ -414,24 +420,24 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   __syncthreads();
   const uint64_t col = (uint64_t(blockIdx.x - mine * a.slabs) * kWave + lane) * kC;
   const uint32_t width = block_width<kC>(col, a.cols);
-  Raw<float, kC> held;
+  Raw<float, kC, kWhole> held;
   held.zero();
   if (width && wave == 0) read_row(a, out, row, col, width, held);
   float sum[kC] = {};
   for (uint32_t e0 = wave * kFewBatch; e0 < total; e0 += kSumWaves * kFewBatch) {
     // all loads, then all of the arithmetic without branches, so that the rows' chains of products overlap
-    Raw<T, kC> raw[kFewBatch];
+    Raw<T, kC, kWhole> raw[kFewBatch];
     uint32_t bits[kFewBatch][kC / 2];
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
       const uint32_t i = __builtin_amdgcn_readfirstlane(list[min(e0 + b, total - 1)]);
-      if (width) raw[b].template load<true>(grad.p + int64_t(i) * grad.ld + col, width);
+      if (width) raw[b].template load<true>(grad.p + int64_t(i) * grad.ld + col, width, a.cols < kC);
       if (kDrop) a.drop.template bits<kC>(i, col, bits[b]);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kFewBatch; ++b) {
       float v[kC];
-      raw[b].widen(v);
+      raw[b].widen(v, width);
       if (kDrop) a.drop.template apply<kC>(bits[b], v);
 #pragma unroll
       for (uint32_t x = 0; x < kC; ++x) sum[x] += e0 + b < total ? v[x] : 0.0f;
@@ -447,7 +453,7 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
 #pragma unroll
         for (uint32_t x = 0; x < kC; ++x) sum[x] += shared[w][lane][x];
   }
-  if (wave == 0 && width) finish_row(a, out, row, col, width, sum, held);
+  if (wave == 0 && width) finish_row<true>(a, out, row, col, width, sum, held);
 }
 
 // ---------------------------------------------------------------------------
@@ -502,6 +508,12 @@ hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, con
   return hipGetLastError();
 }
 
+template <typename T, bool kAdd>
+auto sum_kernel_for(bool whole, bool drop) {
+  return drop ? whole ? sum_kernel<T, true, true, kAdd> : sum_kernel<T, false, true, kAdd>
+              : whole ? sum_kernel<T, true, false, kAdd> : sum_kernel<T, false, false, kAdd>;
+}
+
 template <typename T>
 hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t stream) {
   const uint32_t n = uint32_t(x.tokens.count), rows = uint32_t(x.dtable.rows), cols = uint32_t(x.dtable.cols);
@@ -511,6 +523,7 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   const Mat<const T> grad{static_cast<const T*>(x.grad.data), x.grad.ld};
   const Mat<float> out{static_cast<float*>(x.dtable.data), x.dtable.ld};
   const dim3 block(kSumThreads);
+  const bool whole = whole_blocks(cols, kLaneCols<T>);
   SumArgs a{};
   a.n = n;
   a.rows = rows;
@@ -523,8 +536,9 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
     a.sum_wgs = n * a.slabs;
     a.fill_rows = a.slabs == 1 ? kFillMost : kSumWaves;
     const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + a.fill_rows - 1) / a.fill_rows, 1u << 20)));
-    if (drop.limit) hipLaunchKernelGGL((few_kernel<T, true>), wgs, block, 0, stream, t, a, grad, out);
-    else hipLaunchKernelGGL((few_kernel<T, false>), wgs, block, 0, stream, t, a, grad, out);
+    const auto few = drop.limit ? whole ? few_kernel<T, true, true> : few_kernel<T, false, true>
+                                : whole ? few_kernel<T, true, false> : few_kernel<T, false, false>;
+    hipLaunchKernelGGL(few, wgs, block, 0, stream, t, a, grad, out);
     return hipGetLastError();
   }
   const hipError_t e = sort_tokens(t, work, w, &a.keys, &a.order, stream);
@@ -534,9 +548,10 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   a.chunks = (n + a.chunk - 1) / a.chunk;
   a.sum_wgs = uint32_t((uint64_t(a.chunks) * a.slabs + kSumWaves - 1) / kSumWaves);
   const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20)));
-  if (drop.limit) hipLaunchKernelGGL((sum_kernel<T, true>), wgs, block, 0, stream, a, grad, out);
-  else hipLaunchKernelGGL((sum_kernel<T, false>), wgs, block, 0, stream, a, grad, out);
-  hipLaunchKernelGGL(join_kernel<kLaneCols<T>>, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
+  const auto sum = a.accumulate ? sum_kernel_for<T, true>(whole, drop.limit) : sum_kernel_for<T, false>(whole, drop.limit);
+  hipLaunchKernelGGL(sum, wgs, block, 0, stream, a, grad, out);
+  const auto join = whole ? join_kernel<true, kLaneCols<T>> : join_kernel<false, kLaneCols<T>>;
+  hipLaunchKernelGGL(join, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
   return hipGetLastError();
 }
 

@@ -38,173 +38,178 @@ typedef __bf16 bf16;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Words at any element's address: rows of odd widths start anywhere, and the
-// hardware splits what crosses a line.
+// Accesses of 2 and 4 words at any element's address: rows of odd widths start
+// anywhere, and the hardware splits what crosses a line.  The types' alignment
+// holds where they are named, so no template takes them as arguments.
+// kStream: non-temporal, for what is not used again by this launch.
 template <typename T>
 struct Words;
-template <>
-struct Words<bf16> {
-  typedef uint32_t x1 __attribute__((aligned(2)));
-  typedef uint32_t x2 __attribute__((ext_vector_type(2), aligned(2)));
-  typedef uint32_t x4 __attribute__((ext_vector_type(4), aligned(2)));
-};
-template <>
-struct Words<float> {
-  typedef uint32_t x1;
-  typedef uint32_t x2 __attribute__((ext_vector_type(2), aligned(4)));
-  typedef uint32_t x4 __attribute__((ext_vector_type(4), aligned(4)));
-};
+#define ETC_WORDS(T, A)                                                                       \
+  template <>                                                                                 \
+  struct Words<T> {                                                                           \
+    typedef uint32_t x1 __attribute__((aligned(A)));                                          \
+    typedef uint32_t x2 __attribute__((ext_vector_type(2), aligned(A)));                      \
+    typedef uint32_t x4 __attribute__((ext_vector_type(4), aligned(A)));                      \
+    template <bool kStream>                                                                   \
+    __device__ __forceinline__ static void load2(const void* p, uint32_t* w) {                \
+      x2 v;                                                                                   \
+      if constexpr (kStream) v = __builtin_nontemporal_load(static_cast<const x2*>(p));       \
+      else v = *static_cast<const x2*>(p);                                                    \
+      w[0] = v[0], w[1] = v[1];                                                               \
+    }                                                                                         \
+    template <bool kStream>                                                                   \
+    __device__ __forceinline__ static void load4(const void* p, uint32_t* w) {                \
+      x4 v;                                                                                   \
+      if constexpr (kStream) v = __builtin_nontemporal_load(static_cast<const x4*>(p));       \
+      else v = *static_cast<const x4*>(p);                                                    \
+      w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];                                     \
+    }                                                                                         \
+    template <bool kStream>                                                                   \
+    __device__ __forceinline__ static void store2(void* p, const uint32_t* w) {               \
+      if constexpr (kStream) __builtin_nontemporal_store(x2{w[0], w[1]}, static_cast<x2*>(p)); \
+      else *static_cast<x2*>(p) = x2{w[0], w[1]};                                             \
+    }                                                                                         \
+    template <bool kStream>                                                                   \
+    __device__ __forceinline__ static void store4(void* p, const uint32_t* w) {               \
+      const x4 v{w[0], w[1], w[2], w[3]};                                                     \
+      if constexpr (kStream) __builtin_nontemporal_store(v, static_cast<x4*>(p));             \
+      else *static_cast<x4*>(p) = v;                                                          \
+    }                                                                                         \
+    __device__ __forceinline__ static void store1(void* p, uint32_t w) { *static_cast<x1*>(p) = w; } \
+  }
+ETC_WORDS(bf16, 2);
+ETC_WORDS(float, 4);
+#undef ETC_WORDS
 
 // kC (4 or 8) elements of a row as they are in memory, or the n < kC that a row's
 // last block has.  Loading and widening are apart, so that a kernel can have
 // several rows' loads in flight: a value that is widened where it is loaded, on
-// one side of a branch on n, is waited for right there.  A last block moves in
-// pieces of 4, 2 and 1 elements.  kStream: non-temporal, for what is not used
-// again by this launch.
-template <typename T, uint32_t kC>
-struct Raw;
-
-template <uint32_t kC>
-struct Raw<bf16, kC> {
-  static constexpr uint32_t kWords = kC / 2;
+// one side of a branch, is waited for right there.  A row's last block is loaded
+// as the last kC elements of the row, and shifted when it is widened; only rows
+// of fewer than kC columns (`shorter`) are loaded in pieces of 4, 2 and 1 elements,
+// as all last blocks are stored.  What a last block's load reads of the block
+// before is not used, so that block may be written meanwhile.  kWhole: rows of
+// whole blocks only, and no code for others (whose shifts the compiler lets all
+// lanes do: a lookup 26 us that takes 21). 
+template <typename T, uint32_t kC, bool kWhole>
+struct Raw {
+  static constexpr uint32_t kWords = kC * sizeof(T) / 4;
+  using E = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
   uint32_t w[kWords];
+
   template <bool kStream = false>
-  __device__ __forceinline__ void load(const bf16* p, uint32_t n) {
-    using V = typename std::conditional<kC == 8, Words<bf16>::x4, Words<bf16>::x2>::type;
-    if (n >= kC) {
-      const V* q = reinterpret_cast<const V*>(p);
-      V v;
-      if constexpr (kStream) v = __builtin_nontemporal_load(q);
-      else v = *q;
+  __device__ __forceinline__ void load(const T* p, uint32_t n, bool shorter) {
+    if (kWhole || !shorter) {
+      const T* from = kWhole ? p : p - (kC - n);
+      if constexpr (kWords == 2) Words<T>::template load2<kStream>(from, w);
+      if constexpr (kWords >= 4) Words<T>::template load4<kStream>(from, w);
+      if constexpr (kWords == 8) Words<T>::template load4<kStream>(from + kC / 2, w + 4);
+    } else {  // to the same places: the upper n of kC
+      E x[kC] = {};
 #pragma unroll
-      for (uint32_t e = 0; e < kWords; ++e) w[e] = v[e];
-    } else {
-      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-      Words<bf16>::x2 four = 0;
-      uint32_t two = 0, one = 0;
-      if (kC == 8 && (n & 4)) four = *reinterpret_cast<const Words<bf16>::x2*>(q);
-      if (n & 2) two = *reinterpret_cast<const Words<bf16>::x1*>(q + (n & 4));
-      if (n & 1) one = q[n & 6];
-      const uint32_t low = n & 2 ? two : one, high = n & 2 ? one : 0;  // the last 1 to 3
-      const uint32_t f0 = four[0], f1 = four[1];
-      w[0] = n & 4 ? f0 : low;
-      w[1] = n & 4 ? f1 : high;
-      if constexpr (kC == 8) w[2] = low, w[3] = high;
+      for (uint32_t e = 0; e < kC; ++e)
+        if (e + n >= kC) x[e] = reinterpret_cast<const E*>(p)[e + n - kC];
+#pragma unroll
+      for (uint32_t e = 0; e < kWords; ++e) w[e] = pair(x, e);
     }
   }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (uint32_t e = 0; e < kWords; ++e) w[e] = 0;
   }
-  __device__ __forceinline__ void widen(float (&v)[kC]) const {
+  __device__ __forceinline__ void widen(float (&v)[kC], uint32_t n) const {
+    uint32_t x[kWords];
+#pragma unroll
+    for (uint32_t e = 0; e < kWords; ++e) x[e] = w[e];
+    if (!kWhole && n < kC) {
+      const uint32_t s = kC - n;  // elements to shift down
+      constexpr uint32_t per = 4 / sizeof(T);
+#pragma unroll
+      for (uint32_t d = kWords / 2; d; d /= 2) {
+        const bool on = s & (d * per);
+#pragma unroll
+        for (uint32_t e = 0; e < kWords; ++e) {
+          const uint32_t here = x[e], there = e + d < kWords ? x[e + d < kWords ? e + d : e] : 0;
+          x[e] = on ? there : here;
+        }
+      }
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t bits = s & 1 ? 16 : 0;
+#pragma unroll
+        for (uint32_t e = 0; e < kWords; ++e) {
+          const uint32_t next = e + 1 < kWords ? x[e + 1 < kWords ? e + 1 : e] : 0;
+          x[e] = uint32_t((uint64_t(next) << 32 | x[e]) >> bits);
+        }
+      }
+    }
 #pragma unroll
     for (uint32_t e = 0; e < kWords; ++e) {
-      v[2 * e] = __uint_as_float(w[e] << 16);
-      v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+      if constexpr (sizeof(T) == 2) {
+        v[2 * e] = __uint_as_float(x[e] << 16);
+        v[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+      } else {
+        v[e] = __uint_as_float(x[e]);
+      }
     }
   }
   // rounds to nearest even
   __device__ __forceinline__ void narrow(const float (&v)[kC]) {
 #pragma unroll
-    for (uint32_t e = 0; e < kWords; ++e)
-      w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
-  }
-  template <bool kStream = false>
-  __device__ __forceinline__ void store(bf16* p, uint32_t n) const {
-    using V = typename std::conditional<kC == 8, Words<bf16>::x4, Words<bf16>::x2>::type;
-    if (n >= kC) {
-      V v;
-#pragma unroll
-      for (uint32_t e = 0; e < kWords; ++e) v[e] = w[e];
-      V* q = reinterpret_cast<V*>(p);
-      if constexpr (kStream) __builtin_nontemporal_store(v, q);
-      else *q = v;
-    } else {
-      uint16_t* q = reinterpret_cast<uint16_t*>(p);
-      if (kC == 8 && (n & 4)) *reinterpret_cast<Words<bf16>::x2*>(q) = Words<bf16>::x2{w[0], w[1]};
-      // copies: a choice between elements of an array would be one between their addresses
-      const uint32_t w0 = w[0], w1 = w[1], w2 = w[kWords - 2], w3 = w[kWords - 1];
-      const uint32_t low = n & 4 ? w2 : w0, high = n & 4 ? w3 : w1;
-      if (n & 2) *reinterpret_cast<Words<bf16>::x1*>(q + (n & 4)) = low;
-      if (n & 1) q[n & 6] = uint16_t(n & 2 ? high : low);
+    for (uint32_t e = 0; e < kWords; ++e) {
+      if constexpr (sizeof(T) == 2)
+        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2));
+      else
+        w[e] = __float_as_uint(v[e]);
     }
   }
+  template <bool kStream = false>
+  __device__ __forceinline__ void store(T* p, uint32_t n) const {
+    if (kWhole || n >= kC) {
+      if constexpr (kWords == 2) Words<T>::template store2<kStream>(p, w);
+      if constexpr (kWords >= 4) Words<T>::template store4<kStream>(p, w);
+      if constexpr (kWords == 8) Words<T>::template store4<kStream>(p + kC / 2, w + 4);
+      return;
+    }
+    // four elements where there are as many, then the last 1 to 3: their words, and where they go
+    constexpr uint32_t quad = kWords * 4 / kC;
+    E* q = reinterpret_cast<E*>(p);
+    uint32_t x[quad];
+#pragma unroll
+    for (uint32_t e = 0; e < quad; ++e) {
+      const uint32_t low = w[e], high = w[kWords - quad + e];  // copies: else a choice between addresses
+      x[e] = n & 4 ? high : low;
+    }
+    if constexpr (sizeof(T) == 2) {
+      if (kC == 8 && (n & 4)) Words<T>::template store2<false>(q, w);
+      if (n & 2) Words<T>::store1(q + (n & 4), x[0]);
+      const uint32_t a = x[0], b = x[1];
+      if (n & 1) q[n & 6] = E(n & 2 ? b : a);
+    } else {
+      if (kC == 8 && (n & 4)) Words<T>::template store4<false>(q, w);
+      if (n & 2) Words<T>::template store2<false>(q + (n & 4), x);
+      const uint32_t a = x[0], b = x[2];
+      if (n & 1) q[n & 6] = n & 2 ? b : a;
+    }
+  }
+
+ private:
+  __device__ __forceinline__ static uint32_t pair(const uint16_t (&x)[kC], uint32_t e) {
+    return x[2 * e] | uint32_t(x[2 * e + 1]) << 16;
+  }
+  __device__ __forceinline__ static uint32_t pair(const uint32_t (&x)[kC], uint32_t e) { return x[e]; }
 };
 
-template <uint32_t kC>
-struct Raw<float, kC> {
-  uint32_t w[kC];
-  template <bool kStream = false>
-  __device__ __forceinline__ void load(const float* p, uint32_t n) {
-    using V = Words<float>::x4;
-    if (n >= kC) {
-#pragma unroll
-      for (uint32_t h = 0; h < kC / 4; ++h) {
-        const V* q = reinterpret_cast<const V*>(p + 4 * h);
-        V v;
-        if constexpr (kStream) v = __builtin_nontemporal_load(q);
-        else v = *q;
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) w[4 * h + e] = v[e];
-      }
-    } else {
-      const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
-      V four = 0;
-      Words<float>::x2 two = 0;
-      uint32_t one = 0;
-      if (kC == 8 && (n & 4)) four = *reinterpret_cast<const V*>(q);
-      if (n & 2) two = *reinterpret_cast<const Words<float>::x2*>(q + (n & 4));
-      if (n & 1) one = q[n & 6];
-      const uint32_t tail[4] = {n & 2 ? two[0] : one, two[1], one, 0};  // the last 1 to 3
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t f = four[e], t = tail[e];
-        w[e] = n & 4 ? f : t;
-        if constexpr (kC == 8) w[4 + e] = t;
-      }
-    }
-  }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (uint32_t e = 0; e < kC; ++e) w[e] = 0;
-  }
-  __device__ __forceinline__ void widen(float (&v)[kC]) const {
-#pragma unroll
-    for (uint32_t e = 0; e < kC; ++e) v[e] = __uint_as_float(w[e]);
-  }
-  __device__ __forceinline__ void narrow(const float (&v)[kC]) {
-#pragma unroll
-    for (uint32_t e = 0; e < kC; ++e) w[e] = __float_as_uint(v[e]);
-  }
-  template <bool kStream = false>
-  __device__ __forceinline__ void store(float* p, uint32_t n) const {
-    using V = Words<float>::x4;
-    if (n >= kC) {
-#pragma unroll
-      for (uint32_t h = 0; h < kC / 4; ++h) {
-        const V v{w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
-        V* q = reinterpret_cast<V*>(p + 4 * h);
-        if constexpr (kStream) __builtin_nontemporal_store(v, q);
-        else *q = v;
-      }
-    } else {
-      uint32_t* q = reinterpret_cast<uint32_t*>(p);
-      if (kC == 8 && (n & 4)) *reinterpret_cast<V*>(q) = V{w[0], w[1], w[2], w[3]};
-      // copies: a choice between elements of an array would be one between their addresses
-      const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w4 = w[kC - 4], w5 = w[kC - 3], w6 = w[kC - 2];
-      const uint32_t t0 = n & 4 ? w4 : w0, t1 = n & 4 ? w5 : w1, t2 = n & 4 ? w6 : w2;
-      if (n & 2) *reinterpret_cast<Words<float>::x2*>(q + (n & 4)) = Words<float>::x2{t0, t1};
-      if (n & 1) q[n & 6] = n & 2 ? t2 : t0;
-    }
-  }
-};
-
-template <bool kStream = false, typename T, uint32_t kC>
+template <bool kWhole, bool kStream = false, typename T, uint32_t kC>
 __device__ __forceinline__ void store_block(T* p, uint32_t n, const float (&v)[kC]) {
-  Raw<T, kC> raw;
+  Raw<T, kC, kWhole> raw;
   raw.narrow(v);
   raw.template store<kStream>(p, n);
 }
+
+// Keeps the compiler from moving memory accesses past this place: loads to
+// where their values are used, which would wait for each in turn, and a store into
+// other stores' place, which loses its non-temporal hint on the way.
+__device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory"); }
 
 // Division of n < 2^31 by d >= 1 as a product (Granlund and Montgomery, "Division
 // by Invariant Integers using Multiplication", PLDI 1994): q = (hi(n m) + n) >> s.
@@ -218,6 +223,7 @@ struct Divisor {
   __host__ __device__ uint32_t div(uint32_t n) const { return uint32_t((((uint64_t(n) * m) >> 32) + n) >> s); }
 };
 
+inline bool whole_blocks(int64_t cols, uint32_t block) { return cols % block == 0; }
 inline uint32_t blocks_per_row(int64_t cols, uint32_t block) { return uint32_t((cols + block - 1) / block); }
 
 // Columns of the block of kC that begins at `col`, 0 past the matrix.
