@@ -473,13 +473,16 @@ uint64_t slabs_of(uint64_t cols, uint32_t block) { return (cols + kWave * block 
 
 bool is_few(uint64_t n, uint64_t slabs) { return n <= kFewMost && n * slabs <= kFewJobs; }
 
-// Tokens per chunk: at most kJobs wavefronts in all, but 4 to 64 (one per lane) tokens each.
-constexpr uint64_t kJobs = 4096, kChunkLeast = 4, kChunkMost = kWave;
+// Tokens per chunk: 4 to 64 (one per lane), so that there are at most kJobs
+// wavefronts, and kChunks chunks, for each of which the join has a workgroup per
+// slab.  16384 x 2048, MI355X, in us, with 2048 / 3072 / 4096 / 6144 jobs: 51.5 / 49.8 /
+// 48.2 / 52.5; 16384 x 256 with at most 4096 / 2048 / 1024 chunks: 32.7 / 26.1 / 23.4.
+constexpr uint64_t kJobs = 4096, kChunks = 1024, kChunkLeast = 4, kChunkMost = kWave;
 
 uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 uint32_t chunk_of(uint64_t n, uint64_t slabs) {
-  return uint32_t(std::min(kChunkMost, std::max(kChunkLeast, up(n * slabs, kJobs))));
+  return uint32_t(std::min(kChunkMost, std::max({kChunkLeast, up(n * slabs, kJobs), up(n, kChunks)})));
 }
 
 // Columns of parts, at most, over all chunks: n / kChunkLeast of them, or where
