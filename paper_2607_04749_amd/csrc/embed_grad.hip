@@ -71,24 +71,34 @@ __device__ __forceinline__ uint32_t total_place(uint32_t (&count)[kPlaceWaves][k
   return total;
 }
 
+// Tiles of kEach kTile tokens.  Up to 2 kTile tokens are one tile: 2048 x 2048, 17.8 us,
+// where two tiles and a merge took 20.1; as runs to merge larger tiles cost 2 us more.
+template <uint32_t kEach>
 __global__ __launch_bounds__(kPlaceThreads) void tile_kernel(Tokens t, uint32_t* keys, uint32_t* order) {
-  __shared__ __attribute__((aligned(16))) uint32_t all[kPlaceWaves][kWave];
+  constexpr uint32_t kBlocks = kPlaceWaves * kEach;
+  __shared__ __attribute__((aligned(16))) uint32_t all[kPlaceWaves][kEach][kWave];
   __shared__ uint32_t count[kPlaceWaves][kWave];
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t mine = blockIdx.x, i = mine * kWave + lane;
-  const uint32_t first = mine / kPlaceWaves * kTile, other = mine / kPlaceWaves * kPlaceWaves + wave;
-  const uint32_t j = other * kWave + lane;
+  const uint32_t first = mine / kBlocks * kBlocks * kWave, others = mine / kBlocks * kBlocks + wave * kEach;
   const uint32_t key = i < t.n ? t.key(i) : kNone;
-  all[wave][lane] = j < t.n ? t.key(j) : kNone;
+#pragma unroll
+  for (uint32_t k = 0; k < kEach; ++k) {
+    const uint32_t j = (others + k) * kWave + lane;
+    all[wave][k][lane] = j < t.n ? t.key(j) : kNone;
+  }
   wave_sync();
   uint32_t place = 0;
-  if (other != mine) {
-    const uint32_t below = key + (other < mine);  // equal keys of earlier tokens come before
 #pragma unroll
-    for (uint32_t e = 0; e < kWave; ++e) place += all[wave][e] < below;
-  } else {
+  for (uint32_t k = 0; k < kEach; ++k) {
+    if (others + k != mine) {
+      const uint32_t below = key + (others + k < mine);  // equal keys of earlier tokens come before
 #pragma unroll
-    for (uint32_t e = 0; e < kWave; ++e) place += all[wave][e] < key + (e < lane);
+      for (uint32_t e = 0; e < kWave; ++e) place += all[wave][k][e] < below;
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < kWave; ++e) place += all[wave][k][e] < key + (e < lane);
+    }
   }
   place = total_place(count, place);
   if (wave == 0 && i < t.n) {
@@ -496,9 +506,10 @@ hipError_t sort_tokens(const Tokens& t, char* work, const EmbedGradSizes& w, con
                        const uint32_t** order, hipStream_t stream) {
   auto at = [&](uint64_t byte) { return reinterpret_cast<uint32_t*>(work + byte); };
   const dim3 wgs((t.n + kWave - 1) / kWave), block(kPlaceThreads);
-  hipLaunchKernelGGL(tile_kernel, wgs, block, 0, stream, t, at(w.keys[0]), at(w.order[0]));
+  const bool one = t.n <= 2 * kTile;
+  hipLaunchKernelGGL(one && t.n > kTile ? tile_kernel<2> : tile_kernel<1>, wgs, block, 0, stream, t, at(w.keys[0]), at(w.order[0]));
   uint32_t in = 0;  // the pair of lists that holds the runs
-  for (uint64_t length = kTile, runs = kPlaceWaves; length < t.n; length *= runs, runs = 4 * kPlaceWaves) {
+  for (uint64_t length = kTile, runs = kPlaceWaves; !one && length < t.n; length *= runs, runs = 4 * kPlaceWaves) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     auto merge = length == kTile ? merge_kernel<true, 1> : merge_kernel<false, 4>;

@@ -207,6 +207,11 @@ GRAD = [
     (513, 24, 5000, 5000, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (128, 8192, 40, 40, 0, 0.1, "bf16", "int64", "log", 0, 0),
     (129, 8192, 40, 40, 0, 0.1, "bf16", "int64", "log", 0, 0),
+    (1024, 16, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (1025, 16, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (2048, 16, 900, 900, 0, 0.0, "bf16", "int32", "log", 0, 0),
+    (2049, 16, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
+    (2048, 16, 9, 9, 0, 0.0, "bf16", "int64", "same", 0, 0),
     (16384, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (16385, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (40000, 9, 50000, 50000, 0, 0.1, "f32", "int32", "distinct", 0, 0),
