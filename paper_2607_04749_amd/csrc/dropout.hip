@@ -51,33 +51,35 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_kernel(BlockGrid grid, D
 }
 
 // ---------------------------------------------------------------------------
-// Backward with the bias's gradient.  A workgroup takes `step` rows of a slab of
-// `lanes` blocks of columns: a lane keeps its block's sums over the rows that
-// it visits, the workgroup adds its lanes' and writes one row of partial
-// sums, and a second launch adds those up.
+// Backward with the bias's gradient.  A workgroup has a slab of columns and
+// takes rows a stride apart, kBatch per lane at a time, so that all workgroups
+// together walk the matrix as one front; a lane keeps its block's sums over the
+// rows that it visits, the workgroup adds its lanes' and writes one row of
+// partial sums, and a second launch adds those up.
 
 struct GradShape {
   uint32_t rows, cols;
   uint32_t lane_bits;  // 1 << lane_bits blocks of columns side by side, the other lanes further rows
   uint32_t slabs;      // slabs side by side
-  uint32_t step, parts;
+  uint32_t parts;      // workgroups per slab
 
   uint32_t down() const { return kThreads >> lane_bits; }  // rows that a workgroup visits at once
 };
 
 constexpr uint32_t kBatch = 2;     // rows in flight per lane
-constexpr uint64_t kWgs = 2048;    // workgroups wanted at most
+// Workgroups at most.  Row by row in bands of their own, 2048 workgroups took 26.3 us
+// (16384 x 2048 bf16) and 60 us (fp32); as one front 26.0 and 52.0, 1024 of them
+// 24.3 and 49.8, 512 24.5 and 54.8 (dx alone 22 and 41).  Non-temporal loads cost 3 us.
+constexpr uint64_t kWgs = 1024;
 constexpr uint32_t kSlab = 64;     // blocks of a slab at most
 
 GradShape grad_shape(uint32_t rows, uint32_t cols, uint32_t block) {
-  GradShape g{rows, cols, 0, 0, 0, 0};
+  GradShape g{rows, cols, 0, 0, 0};
   const uint32_t nb = blocks_per_row(cols, block);
   while ((1u << g.lane_bits) < std::min(nb, kSlab)) ++g.lane_bits;
   g.slabs = (nb + kSlab - 1) / kSlab;
-  const uint64_t least = g.down() * kBatch;  // at least 8
-  g.step = uint32_t(std::min<uint64_t>(INT32_MAX, (uint64_t(rows) * g.slabs + kWgs * least - 1) / (kWgs * least) * least));
-  g.step = std::max(g.step, uint32_t(least));
-  g.parts = (rows + g.step - 1) / g.step;
+  const uint32_t visit = g.down() * kBatch;  // rows at a time, at least 8
+  g.parts = uint32_t(std::min<uint64_t>((uint64_t(rows) + visit - 1) / visit, (kWgs + g.slabs - 1) / g.slabs));
   return g;
 }
 
@@ -90,22 +92,22 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
   const uint64_t left = uint64_t(blockIdx.x - part * g.slabs) * kSlab * kC, col = left + across * kC;
   const uint32_t width = block_width<kC>(col, g.cols);
   const uint32_t down = kThreads >> g.lane_bits;
-  const uint32_t end = uint32_t(min(uint64_t(g.rows), (uint64_t(part) + 1) * g.step));
   const bool shorter = g.cols < kC;
   float sum[kC] = {};
   if (width) {
-    for (uint64_t i0 = uint64_t(part) * g.step + (threadIdx.x >> g.lane_bits); i0 < end; i0 += down * kBatch) {
+    for (uint64_t i0 = uint64_t(part) * down * kBatch + (threadIdx.x >> g.lane_bits); i0 < g.rows;
+         i0 += uint64_t(g.parts) * down * kBatch) {
       Raw<T, kC, kWhole> raw[kBatch];
 #pragma unroll
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
-        raw[b].load(grad.p + int64_t(i < end ? i : i0) * grad.ld + col, width, shorter);
+        raw[b].load(grad.p + int64_t(i < g.rows ? i : i0) * grad.ld + col, width, shorter);
       }
       compiler_fence();
 #pragma unroll
       for (uint32_t b = 0; b < kBatch; ++b) {
         const uint64_t i = i0 + b * down;
-        if (i >= end) break;
+        if (i >= g.rows) break;
         uint32_t bits[kC / 2];
         if (kDrop) drop.template bits<kC>(i, col, bits);
         float v[kC];

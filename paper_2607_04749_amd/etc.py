@@ -565,15 +565,16 @@ def _matrix(x, what, device):
         raise ValueError(f"{what} must be bfloat16 or float32, not {x.dtype}")
     if x.get_device() != device:
         raise ValueError(f"{what} must be a tensor on the current GPU")
-    if x.dim() == 2:
-        rows, cols = x.shape
+    shape = x.shape
+    if len(shape) == 2:
+        rows, cols = shape
         ld, step = x.stride()
         if step != 1 and cols > 1 and rows:
             raise ValueError(f"the rows of {what} must be contiguous")
         return x.data_ptr(), rows, cols, ld if rows > 1 else cols, dtype, 0
-    if x.dim() == 0 or not x.is_contiguous():
+    if not shape or not x.is_contiguous():
         raise ValueError(f"{what} must have two dimensions or be contiguous")
-    cols = x.shape[-1]
+    cols = shape[-1]
     return x.data_ptr(), x.numel() // cols if cols else 0, cols, cols, dtype, 0
 
 
