@@ -532,8 +532,9 @@ ETC_API int etc_embed(const etc_embed_args* args, void* stream);
  * those are not touched.  The gradient of pos_table is the same with the
  * positions as ids and scale 1.
  * The ids are sorted first, then each run of equal ids is summed; ids outside
- * the table are skipped.  At most 2^27 tokens, and about 2^29 tokens x columns / 64.
- * workspace: etc_embed_grad_workspace's bytes, for the same sizes or larger ones. */
+ * the table are skipped.  More than 2^27 tokens, or about 2^37 elements of grad, are
+ * UNSUPPORTED.  workspace: etc_embed_grad_workspace's bytes, for the same sizes or
+ * larger ones. */
 typedef struct {
   etc_ids tokens;
   etc_matrix grad, dtable;

@@ -158,27 +158,31 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float
                                                                     float* dbias, uint32_t accumulate) {
   __shared__ float shared[kJoinRows][kJoinCols + 1];
   const uint32_t c = threadIdx.x % kJoinCols, r = threadIdx.x / kJoinCols;
-  const uint64_t col = uint64_t(blockIdx.x) * kJoinCols + c;
-  float sum = 0.0f;
-  if (col < cols) {
-    for (uint32_t k0 = r; k0 < n; k0 += kJoinBatch * kJoinRows) {
-      float v[kJoinBatch];
+  for (uint64_t first = uint64_t(blockIdx.x) * kJoinCols; first < cols; first += uint64_t(gridDim.x) * kJoinCols) {
+    const uint64_t col = first + c;
+    float sum = 0.0f;
+    if (col < cols) {
+      for (uint32_t k0 = r; k0 < n; k0 += kJoinBatch * kJoinRows) {
+        float v[kJoinBatch];
 #pragma unroll
-      for (uint32_t b = 0; b < kJoinBatch; ++b) {
-        const uint32_t k = k0 + b * kJoinRows;
-        v[b] = k < n ? partial[uint64_t(k) * cols + col] : 0.0f;
+        for (uint32_t b = 0; b < kJoinBatch; ++b) {
+          const uint32_t k = k0 + b * kJoinRows;
+          v[b] = k < n ? partial[uint64_t(k) * cols + col] : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t b = 0; b < kJoinBatch; ++b) sum += v[b];
       }
-#pragma unroll
-      for (uint32_t b = 0; b < kJoinBatch; ++b) sum += v[b];
     }
-  }
-  shared[r][c] = sum;
-  __syncthreads();
-  if (r != 0 || col >= cols) return;
-  sum = 0.0f;
+    shared[r][c] = sum;
+    __syncthreads();
+    if (r == 0 && col < cols) {
+      sum = 0.0f;
 #pragma unroll
-  for (uint32_t k = 0; k < kJoinRows; ++k) sum += shared[k][c];
-  dbias[col] = (accumulate ? dbias[col] : 0.0f) + sum;
+      for (uint32_t k = 0; k < kJoinRows; ++k) sum += shared[k][c];
+      dbias[col] = (accumulate ? dbias[col] : 0.0f) + sum;
+    }
+    __syncthreads();
+  }
 }
 
 template <typename T>
@@ -232,8 +236,9 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(dbias_kernel, dim3((g.cols + kJoinCols - 1) / kJoinCols), dim3(kJoinCols * kJoinRows), 0, stream,
-                     partial, g.parts, g.cols, static_cast<float*>(a.dbias.data), uint32_t(a.accumulate != 0));
+  const uint32_t joins = uint32_t(std::min((uint64_t(g.cols) + kJoinCols - 1) / kJoinCols, uint64_t(1) << 16));
+  hipLaunchKernelGGL(dbias_kernel, dim3(joins), dim3(kJoinCols * kJoinRows), 0, stream, partial, g.parts, g.cols,
+                     static_cast<float*>(a.dbias.data), uint32_t(a.accumulate != 0));
   return hipGetLastError();
 }
 

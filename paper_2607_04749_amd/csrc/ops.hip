@@ -117,9 +117,11 @@ int etc_embed(const etc_embed_args* a, void* stream) {
     return rc;
   if (a->out.rows != a->tokens.count) return fail(ETC_ERR_INVALID_ARG, "out needs one row per token");
   if (a->out.cols != a->table.cols) return fail(ETC_ERR_INVALID_ARG, "out and table differ in columns");
-  if (!a->positions.data != !a->pos_table.data)
+  // an empty table has columns, an absent one none; no tokens need no pointer to their positions
+  const bool pos = a->pos_table.data || a->pos_table.cols != 0;
+  if (a->tokens.count && pos != (a->positions.data != nullptr))
     return fail(ETC_ERR_INVALID_ARG, "positions and pos_table go together");
-  if (a->positions.data) {
+  if (pos) {
     if ((rc = check_ids(a->positions, "positions")) || (rc = check_matrix(a->pos_table, "pos_table", kIn))) return rc;
     if (a->positions.count != a->tokens.count) return fail(ETC_ERR_INVALID_ARG, "positions needs one entry per token");
     if (a->pos_table.cols != a->table.cols || a->pos_table.dtype != a->table.dtype)

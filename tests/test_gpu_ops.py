@@ -138,6 +138,18 @@ def test_embed_without_dropout_is_exact():
     assert torch.equal(o, want)
 
 
+def test_embed_empty_position_table():
+    """A position table of no rows contributes nothing, as positions past one do."""
+    say("embed: empty position table")
+    rng = np.random.default_rng(7)
+    w, wn, _ = rand(rng, 6, 40, "bf16")
+    v = torch.arange(6, device=DEV)
+    o, _ = blank(6, 40, "f32")
+    etc.etc_embed(v, w, o, positions=v, pos_table=w[:0])
+    close(o, op_ref.embed(range(6), wn), "empty")
+    etc.etc_embed(v[:0], w, o[:0], positions=v[:0], pos_table=w)
+
+
 def test_embed_extreme_ids():
     """Ids at the ends of 64 and 32 bits are outside, whatever row0 is."""
     say("embed: extreme ids")
@@ -330,7 +342,8 @@ def test_dropout(case):
 @pytest.mark.parametrize("accumulate", (False, True))
 @pytest.mark.parametrize("case", DROPOUT + [(5000, 40, 0.1, "f32", True, False, 0, 0),
                                             (9001, 264, 0.1, "bf16", True, False, 0, 0),
-                                            (70, 20000, 0.1, "bf16", True, False, 0, 0)],
+                                            (70, 20000, 0.1, "bf16", True, False, 0, 0),
+                                            (9, 1200003, 0.1, "f32", True, False, 0, 0)],
                          ids=lambda c: "-".join(map(str, c)))
 def test_dropout_grad(case, accumulate):
     rows, cols, p, dtype, bias, _, more, shift = case

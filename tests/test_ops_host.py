@@ -219,6 +219,8 @@ def test_calls_without_work():
     """Nothing to compute: OK, with nothing launched and no pointer followed."""
     assert embed(tokens=ids(0, ptr=0), out=mat(0, 16, ptr=0)) == OK
     assert embed(table=mat(9, 0, ptr=0), out=mat(3, 0, ptr=0)) == OK
+    assert embed(tokens=ids(0, ptr=0), out=mat(0, 16, ptr=0), positions=ids(0, ptr=0), pos=mat(4, 16)) == OK
+    assert embed(tokens=ids(0, ptr=0), out=mat(0, 16, ptr=0), positions=ids(0, ptr=0), pos=mat(0, 16, ptr=0)) == OK
     assert embed_grad(tokens=ids(0, ptr=0), grad=mat(0, 16, ptr=0), accumulate=1) == OK
     assert embed_grad(dtable=mat(0, 16, F32, ptr=0)) == OK
     assert dropout(x=mat(0, 16, ptr=0), out=mat(0, 16, ptr=0)) == OK
