@@ -25,11 +25,12 @@ def host():
     out = os.path.join(ROOT, "_build", "opshost", h)
     if not os.path.exists(out):
         os.makedirs(os.path.dirname(out), exist_ok=True)
+        part = f"{out}.{os.getpid()}"  # several test processes may build it at once
         r = subprocess.run(["hipcc", "-x", "hip", "--offload-arch=gfx950", "-O1", "-std=c++17", "-Xclang",
                             "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"),
-                            "-I", CSRC, SRC, "-o", out + ".tmp"], capture_output=True, text=True)
+                            "-I", CSRC, SRC, "-o", part], capture_output=True, text=True)
         assert r.returncode == 0, r.stderr[-3000:]
-        os.replace(out + ".tmp", out)
+        os.replace(part, out)
 
     def run(*args):
         r = subprocess.run([out, *map(str, args)], capture_output=True, text=True, timeout=120)
