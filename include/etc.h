@@ -34,7 +34,7 @@
  *   etc_plan_* queries      host: dimensions, pieces, arena sizes, send and
  *                            chunk layouts, receive counts, pairing, roles
  * and the operators of a training step that read and write those states, with
- * results that do not depend on the configuration a rank is in:
+ * dropout masks that do not depend on the configuration a rank is in:
  *   etc_embed, etc_embed_grad      device: lookup in a rank's share of the
  *                                  vocabulary, and the table's gradient
  *   etc_dropout, etc_dropout_grad  device: bias, dropout and residual, with a

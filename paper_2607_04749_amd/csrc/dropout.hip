@@ -51,8 +51,8 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_kernel(BlockGrid grid, D
 }
 
 // ---------------------------------------------------------------------------
-// Backward with the bias's gradient.  A workgroup has a slab of columns and
-// takes rows a stride apart, kBatch per lane at a time, so that all workgroups
+// Backward with the bias's gradient.  Many rows: a workgroup has a slab of columns
+// and takes rows a stride apart, kBatch per lane at a time, so that all workgroups
 // together walk the matrix as one front; a lane keeps its block's sums over the
 // rows that it visits, the workgroup adds its lanes' and writes one row of
 // partial sums, and a second launch adds those up.
@@ -128,6 +128,75 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
     for (uint32_t k = 0; k < down; ++k) total += shared[(k << g.lane_bits) + c / kC][c % kC];
     if (left + c < g.cols) partial[uint64_t(part) * g.cols + left + c] = total;
   }
+}
+
+// Few rows, in one launch: a workgroup has kFewBlocks blocks of columns and all
+// rows, and so the whole of its columns' sums.  There are then few workgroups, so
+// up to kFewRows rows and kFewJobs blocks.  MI355X, in us, graph replays, one launch /
+// two (and 2.5 us less of the host's time for each launch):
+//   rows           256         512         1021          2048
+//   681 bf16    4.6 / 6.1   5.1 / 6.4    6.9 / 6.5    12.6 / 7.3
+//   681 fp32    3.7 / 5.9   4.4 / 6.1    7.0 / 6.7    11.4 / 7.6
+//   8192 bf16   5.2 / 8.1   7.5 / 10.3  10.6 / 12.4   17.9 / 16.6
+//   8192 fp32   6.7 / 8.6  10.1 / 10.9  17.8 / 15.6   41.7 / 24.7
+// Two blocks a workgroup: 8192 bf16 7.9 (256 rows); 4 rows in flight: the same.
+constexpr uint32_t kFewThreads = 1024, kFewBlocks = 4, kFewDown = kFewThreads / kFewBlocks;
+constexpr uint32_t kFewRows = 1024;
+constexpr uint64_t kFewJobs = 1 << 19;
+
+bool is_few(uint64_t rows, uint64_t blocks) { return rows <= kFewRows && std::max<uint64_t>(rows, 1) * blocks <= kFewJobs; }
+
+template <typename T, bool kWhole, bool kDrop>
+__global__ __launch_bounds__(kFewThreads) void dropout_grad_few_kernel(uint32_t rows, uint32_t cols, Drop drop,
+                                                                       Mat<const T> grad, Mat<T> dx, float* dbias,
+                                                                       uint32_t accumulate) {
+  constexpr uint32_t kC = kLaneCols<T>, kWaves = kFewThreads / 64;
+  __shared__ float shared[kWaves][kFewBlocks * kC];
+  const uint32_t across = threadIdx.x % kFewBlocks, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint64_t left = uint64_t(blockIdx.x) * kFewBlocks * kC, col = left + across * kC;
+  const uint32_t width = block_width<kC>(col, cols);
+  const bool shorter = cols < kC;
+  // a column's sum so far, early
+  const bool mine = threadIdx.x < kFewBlocks * kC && left + threadIdx.x < cols;
+  float total = mine && accumulate ? dbias[left + threadIdx.x] : 0.0f;
+  float sum[kC] = {};
+  if (width) {
+    for (uint32_t i0 = threadIdx.x / kFewBlocks; i0 < rows; i0 += kFewDown * kBatch) {
+      Raw<T, kC, kWhole> raw[kBatch];
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint32_t i = i0 + b * kFewDown;
+        raw[b].load(grad.p + int64_t(i < rows ? i : i0) * grad.ld + col, width, shorter);
+      }
+      compiler_fence();
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint32_t i = i0 + b * kFewDown;
+        if (i >= rows) break;
+        uint32_t bits[kC / 2];
+        if (kDrop) drop.template bits<kC>(i, col, bits);
+        float v[kC];
+        raw[b].widen(v, width);
+        if (kDrop) drop.template apply<kC>(bits, v);
+#pragma unroll
+        for (uint32_t e = 0; e < kC; ++e) sum[e] += v[e];
+        store_block<kWhole>(dx.p + int64_t(i) * dx.ld + col, width, v);
+      }
+    }
+  }
+  // over the wavefront's rows, which lie kFewBlocks lanes apart, then over the wavefronts
+#pragma unroll
+  for (uint32_t e = 0; e < kC; ++e) {
+#pragma unroll
+    for (uint32_t d = kFewBlocks; d < 64; d *= 2) sum[e] += __shfl_xor(sum[e], d);
+    if (lane < kFewBlocks) shared[wave][lane * kC + e] = sum[e];
+  }
+  __syncthreads();
+  if (!mine) return;
+  float all = 0.0f;
+#pragma unroll
+  for (uint32_t w = 0; w < kWaves; ++w) all += shared[w][threadIdx.x];
+  dbias[left + threadIdx.x] = total + all;
 }
 
 // dx alone
@@ -223,6 +292,17 @@ hipError_t launch_dx(const etc_dropout_grad_args& a, const Drop& drop, hipStream
 template <typename T>
 hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream) {
   if (!a.dbias.data) return launch_dx<T>(a, drop, stream);
+  if (is_few(uint64_t(a.grad.rows), blocks_per_row(a.grad.cols, kLaneCols<T>))) {
+    const uint32_t rows = uint32_t(a.grad.rows), cols = uint32_t(a.grad.cols);
+    const bool whole = whole_blocks(cols, kLaneCols<T>);
+    const auto kernel = drop.limit ? whole ? dropout_grad_few_kernel<T, true, true> : dropout_grad_few_kernel<T, false, true>
+                                   : whole ? dropout_grad_few_kernel<T, true, false> : dropout_grad_few_kernel<T, false, false>;
+    const dim3 wgs((blocks_per_row(cols, kLaneCols<T>) + kFewBlocks - 1) / kFewBlocks);
+    hipLaunchKernelGGL(kernel, wgs, dim3(kFewThreads), 0, stream, rows, cols, drop,
+                       Mat<const T>{static_cast<const T*>(a.grad.data), a.grad.ld}, Mat<T>{static_cast<T*>(a.dx.data), a.dx.ld}, static_cast<float*>(a.dbias.data),
+                       uint32_t(a.accumulate != 0));
+    return hipGetLastError();
+  }
   const GradShape g = grad_shape(uint32_t(a.grad.rows), uint32_t(a.grad.cols), kLaneCols<T>);
   float* partial = static_cast<float*>(a.workspace);
   if (g.parts) {

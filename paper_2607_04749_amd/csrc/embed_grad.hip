@@ -485,8 +485,8 @@ bool is_few(uint64_t n, uint64_t slabs) { return n <= kFewMost && n * slabs <= k
 
 // Tokens per chunk: 4 to 64 (one per lane), so that there are at most kJobs
 // wavefronts, and kChunks chunks, for each of which the join has a workgroup per
-// slab.  16384 x 2048, MI355X, in us, with 2048 / 3072 / 4096 / 6144 jobs: 51.5 / 49.8 /
-// 48.2 / 52.5; 16384 x 256 with at most 4096 / 2048 / 1024 chunks: 32.7 / 26.1 / 23.4.
+// slab.  16384 x 2048, MI355X, in us, with 2048 / 4096 / 6144 jobs: 51.5 / 48.2 /
+// 52.5; 16384 x 256 with at most 4096 / 2048 / 1024 chunks: 32.7 / 26.1 / 23.4.
 constexpr uint64_t kJobs = 4096, kChunks = 1024, kChunkLeast = 4, kChunkMost = kWave;
 
 uint64_t up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }

@@ -343,7 +343,13 @@ def test_dropout(case):
 @pytest.mark.parametrize("case", DROPOUT + [(5000, 40, 0.1, "f32", True, False, 0, 0),
                                             (9001, 264, 0.1, "bf16", True, False, 0, 0),
                                             (70, 20000, 0.1, "bf16", True, False, 0, 0),
-                                            (9, 1200003, 0.1, "f32", True, False, 0, 0)],
+                                            (9, 1200003, 0.1, "f32", True, False, 0, 0),
+                                            # on both sides of the last sizes of one launch
+                                            (1024, 75, 0.1, "bf16", True, False, 5, 1),
+                                            (1025, 75, 0.1, "bf16", True, False, 5, 1),
+                                            (1024, 512, 0.25, "f32", True, False, 0, 0),
+                                            (256, 8189, 0.1, "f32", True, False, 3, 0),
+                                            (257, 8192, 0.1, "f32", True, False, 0, 0)],
                          ids=lambda c: "-".join(map(str, c)))
 def test_dropout_grad(case, accumulate):
     rows, cols, p, dtype, bias, _, more, shift = case
