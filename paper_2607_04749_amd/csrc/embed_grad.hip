@@ -564,6 +564,7 @@ hipError_t launch(const etc_embed_grad_args& x, const Drop& drop, hipStream_t st
   const dim3 wgs(a.sum_wgs + (a.accumulate ? 0 : std::min((rows + kSumWaves - 1) / kSumWaves, 1u << 20)));
   const auto sum = a.accumulate ? sum_kernel_for<T, true>(whole, drop.limit) : sum_kernel_for<T, false>(whole, drop.limit);
   hipLaunchKernelGGL(sum, wgs, block, 0, stream, a, grad, out);
+  if (a.chunks == 1) return hipGetLastError();  // nothing crosses
   const auto join = whole ? join_kernel<true, kLaneCols<T>> : join_kernel<false, kLaneCols<T>>;
   hipLaunchKernelGGL(join, dim3((a.chunks - 1) * a.slabs), dim3(kJoinWaves * kWave), 0, stream, a, out);
   return hipGetLastError();

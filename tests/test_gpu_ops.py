@@ -224,6 +224,9 @@ GRAD = [
     (2048, 16, 900, 900, 0, 0.0, "bf16", "int32", "log", 0, 0),
     (2049, 16, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (2048, 16, 9, 9, 0, 0.0, "bf16", "int64", "same", 0, 0),
+    # more columns than a launch for few takes, and one chunk of tokens
+    (1, 530001, 2, 2, 0, 0.0, "f32", "int64", "log", 0, 0),
+    (3, 200003, 4, 4, 0, 0.1, "f32", "int64", "same", 0, 0),
     (16384, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (16385, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (40000, 9, 50000, 50000, 0, 0.1, "f32", "int32", "distinct", 0, 0),
