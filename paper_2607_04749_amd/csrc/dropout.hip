@@ -4,7 +4,9 @@
 //   out = residual + drop(x + bias);  dx = drop'(grad);  dbias (+)= column sums of drop'(grad)
 //
 // HBM bound: the mask is worked out from its place, so nothing but x, residual
-// and out (grad and dx) is moved.
+// and out (grad and dx) is moved.  16384 x 2048 bf16, MI355X: the epilogue 31.5 us
+// (201 MB, 6.4 TB/s), its backward 24.3 us with the bias's gradient (main launch 22
+// at 6.1 TB/s, join of the partial sums 4, overlapping in part) and 22 without.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -131,18 +133,20 @@ __global__ __launch_bounds__(kThreads) void dropout_grad_kernel(GradShape g, Dro
 }
 
 // Few rows, in one launch: a workgroup has kFewBlocks blocks of columns and all
-// rows, and so the whole of its columns' sums.  There are then few workgroups, so
-// up to kFewRows rows and kFewJobs blocks.  MI355X, in us, graph replays, one launch /
-// two (and 2.5 us less of the host's time for each launch):
+// rows, and so the whole of its columns' sums.  Neighbours in a row, which share
+// lines, are a gridDim / 8 apart, on one XCD behind one L2 (1021 x 681 fp32: 5.4 us, in
+// the order of the columns 7.0).  There are few workgroups, and what they have
+// in the caches grows, so up to kFewRows rows and kFewJobs blocks.  MI355X, in us, graph
+// replays, one launch / two (which take 2.5 us more of the host's time):
 //   rows           256         512         1021          2048
-//   681 bf16    4.6 / 6.1   5.1 / 6.4    6.9 / 6.5    12.6 / 7.3
-//   681 fp32    3.7 / 5.9   4.4 / 6.1    7.0 / 6.7    11.4 / 7.6
-//   8192 bf16   5.2 / 8.1   7.5 / 10.3  10.6 / 12.4   17.9 / 16.6
-//   8192 fp32   6.7 / 8.6  10.1 / 10.9  17.8 / 15.6   41.7 / 24.7
+//   681 bf16    4.6 / 6.1   5.0 / 6.4    6.7 / 6.5    10.5 / 7.3
+//   681 fp32    3.6 / 5.9   4.1 / 6.1    5.4 / 6.7    10.1 / 7.7
+//   8192 bf16   4.9 / 8.1   5.9 / 10.3   9.1 / 12.4   14.6 / 16.7
+//   8192 fp32   5.4 / 8.6   7.9 / 11.0  13.1 / 15.6   41.3 / 24.9
 // Two blocks a workgroup: 8192 bf16 7.9 (256 rows); 4 rows in flight: the same.
 constexpr uint32_t kFewThreads = 1024, kFewBlocks = 4, kFewDown = kFewThreads / kFewBlocks;
-constexpr uint32_t kFewRows = 1024;
-constexpr uint64_t kFewJobs = 1 << 19;
+constexpr uint32_t kFewRows = 1024, kXcds = 8;
+constexpr uint64_t kFewJobs = 1 << 21;
 
 bool is_few(uint64_t rows, uint64_t blocks) { return rows <= kFewRows && std::max<uint64_t>(rows, 1) * blocks <= kFewJobs; }
 
@@ -153,7 +157,9 @@ __global__ __launch_bounds__(kFewThreads) void dropout_grad_few_kernel(uint32_t 
   constexpr uint32_t kC = kLaneCols<T>, kWaves = kFewThreads / 64;
   __shared__ float shared[kWaves][kFewBlocks * kC];
   const uint32_t across = threadIdx.x % kFewBlocks, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const uint64_t left = uint64_t(blockIdx.x) * kFewBlocks * kC, col = left + across * kC;
+  const uint32_t slab = blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+  const uint64_t left = uint64_t(slab) * kFewBlocks * kC, col = left + across * kC;
+  if (left >= cols) return;
   const uint32_t width = block_width<kC>(col, cols);
   const bool shorter = cols < kC;
   // a column's sum so far, early
@@ -297,7 +303,8 @@ hipError_t launch_backward(const etc_dropout_grad_args& a, const Drop& drop, hip
     const bool whole = whole_blocks(cols, kLaneCols<T>);
     const auto kernel = drop.limit ? whole ? dropout_grad_few_kernel<T, true, true> : dropout_grad_few_kernel<T, false, true>
                                    : whole ? dropout_grad_few_kernel<T, true, false> : dropout_grad_few_kernel<T, false, false>;
-    const dim3 wgs((blocks_per_row(cols, kLaneCols<T>) + kFewBlocks - 1) / kFewBlocks);
+    const uint32_t slabs = (blocks_per_row(cols, kLaneCols<T>) + kFewBlocks - 1) / kFewBlocks;
+    const dim3 wgs((slabs + kXcds - 1) / kXcds * kXcds);
     hipLaunchKernelGGL(kernel, wgs, dim3(kFewThreads), 0, stream, rows, cols, drop,
                        Mat<const T>{static_cast<const T*>(a.grad.data), a.grad.ld}, Mat<T>{static_cast<T*>(a.dx.data), a.dx.ld}, static_cast<float*>(a.dbias.data),
                        uint32_t(a.accumulate != 0));

@@ -12,6 +12,19 @@
 // runs lie inside it.  The parts of a run that crosses chunks go to the
 // workspace and are joined afterwards.
 // All sums are in 32 bits and in a fixed order.
+//
+// The sums are HBM bound (a row of grad per token and of dtable per row, and the
+// parts); the other launches are a few waits long.  bf16 gradients, MI355X, in us:
+//                                            order       sums                    join
+//   16384 x 2048 into 50304 rows, added,     4.6 + 4.5   33, 169 MB, 5.1 TB/s    7.1
+//     dropout
+//   8192 x 4096 into 8000 rows, written      4.8 + 4.0   37, 191 MB, 5.1 TB/s    5.3
+//   128 x 256 into 1024 rows, written        4.3 in all (few)
+// (an addition of three tensors of this size by one elementwise kernel reaches 5.6 TB/s).
+// What was slower: a radix sort (32 us), atomics-free counts of all pairs (1.8 ms),
+// runs that end in the next chunk summed by the wavefront they begin in, which saves
+// parts but leaves chunks of unequal length (the same to 2 us more), and the rows of no token
+// written by the join's launch instead of the sums' (2 to 5 us more).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -352,7 +352,8 @@ def test_dropout(case):
                                             (1025, 75, 0.1, "bf16", True, False, 5, 1),
                                             (1024, 512, 0.25, "f32", True, False, 0, 0),
                                             (256, 8189, 0.1, "f32", True, False, 3, 0),
-                                            (257, 8192, 0.1, "f32", True, False, 0, 0)],
+                                            (1024, 2051, 0.1, "f32", True, False, 0, 0),
+                                            (3, 2796208, 0.1, "f32", True, False, 0, 0)],
                          ids=lambda c: "-".join(map(str, c)))
 def test_dropout_grad(case, accumulate):
     rows, cols, p, dtype, bias, _, more, shift = case
