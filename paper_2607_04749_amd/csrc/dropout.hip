@@ -71,8 +71,9 @@ struct GradShape {
 constexpr uint32_t kBatch = 2;     // rows in flight per lane
 // Workgroups at most.  Row by row in bands of their own, 2048 workgroups took 26.3 us
 // (16384 x 2048 bf16) and 60 us (fp32); as one front 26.0 and 52.0, 1024 of them
-// 24.3 and 49.8, 512 24.5 and 54.8 (dx alone 22 and 41).  Non-temporal loads cost 3 us.
-constexpr uint64_t kWgs = 1024;
+// 24.6 and 50.0, 768 24.1 and 50.2, 512 24.5 and 54.8 (dx alone 22 and 41).  3 or 4 rows
+// in flight: 0.4 to 1 us more.  Non-temporal loads cost 3 us.
+constexpr uint64_t kWgs = 768;
 constexpr uint32_t kSlab = 64;     // blocks of a slab at most
 
 GradShape grad_shape(uint32_t rows, uint32_t cols, uint32_t block) {
@@ -227,7 +228,9 @@ __global__ __launch_bounds__(kFlatThreads) void dropout_dx_kernel(BlockGrid grid
   store_block<kWhole, true>(dx.p + int64_t(i) * dx.ld + col, width, v);
 }
 
-constexpr uint32_t kJoinCols = 16, kJoinRows = 64, kJoinBatch = 8;
+// Whole lines of the partial sums: 16 columns by 64 rows read each line twice, on
+// different XCDs (4096 x 8192 bf16, the whole backward: 27.3 us, so 25.8).
+constexpr uint32_t kJoinCols = 32, kJoinRows = 32, kJoinBatch = 8;
 
 __global__ __launch_bounds__(kJoinCols* kJoinRows) void dbias_kernel(const float* partial, uint32_t n, uint32_t cols,
                                                                     float* dbias, uint32_t accumulate) {
