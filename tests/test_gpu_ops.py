@@ -97,6 +97,11 @@ EMBED = [
     (1000, 256, 1024, 256, 512, 128, 0.1, "bf16", "bf16", "int64", 0, 0),
     (9, 15, 20, 20, 0, 4, 1.0, "bf16", "f32", "int64", 0, 0),
     (300, 7, 40, 40, 0, 0, 0.3, "f32", "bf16", "int64", 2, 1),
+    # as many blocks as make a lane take two rows; an odd number of rows
+    (65537, 128, 300, 100, 100, 0, 0.1, "bf16", "bf16", "int64", 0, 0),
+    (65539, 121, 300, 100, 100, 17, 0.1, "bf16", "bf16", "int32", 3, 1),
+    (32769, 127, 64, 64, 0, 33, 0.5, "f32", "f32", "int64", 0, 0),
+    (65537, 121, 8, 0, 3, 5, 0.1, "bf16", "bf16", "int64", 0, 0),
 ]
 
 
@@ -122,6 +127,20 @@ def test_embed(case):
     torch.cuda.synchronize()
     close(o, op_ref.embed(v, wn, **ref), case)
     assert untouched(full, o)
+
+
+@pytest.mark.parametrize("tokens", (40, 70001))
+def test_embed_reads_no_row_for_ids_outside(tokens):
+    """Whatever the tables hold, infinities and NaN among it, ids and positions
+    outside them contribute zeros."""
+    say("embed: ids outside", tokens)
+    w = torch.full((3, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    q = torch.full((2, 128), float("inf"), dtype=torch.bfloat16, device=DEV)
+    v = torch.arange(tokens, device=DEV) % 2 * 8 - 5  # -5 and 3, of a table of 0 .. 2
+    for kw in ({}, dict(positions=v, pos_table=q), dict(positions=v, pos_table=q[:0])):
+        o = torch.ones(tokens, 128, dtype=torch.bfloat16, device=DEV)
+        etc.etc_embed(v, w, o, dropout=etc.Dropout(0.2, 1), **kw)
+        assert not bool(o.any()) and not bool(o.isnan().any())
 
 
 def test_embed_without_dropout_is_exact():
