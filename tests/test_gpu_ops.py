@@ -102,6 +102,11 @@ EMBED = [
     (65539, 121, 300, 100, 100, 17, 0.1, "bf16", "bf16", "int32", 3, 1),
     (32769, 127, 64, 64, 0, 33, 0.5, "f32", "f32", "int64", 0, 0),
     (65537, 121, 8, 0, 3, 5, 0.1, "bf16", "bf16", "int64", 0, 0),
+] + [
+    # every kernel: types, whole blocks or not, dropout or not, one row a lane or two
+    (tokens, cols, 40, 30, 5, 6, p, table, out, "int64", 1, 1)
+    for table in ("bf16", "f32") for out in ("bf16", "f32")
+    for tokens, cols, p in ((37, 40, 0.0), (37, 39, 0.0), (37, 40, 0.1), (37, 39, 0.1), (32771, 256, 0.1), (32771, 255, 0.1))
 ]
 
 
@@ -249,6 +254,11 @@ GRAD = [
     (16384, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (16385, 8, 900, 900, 0, 0.0, "bf16", "int64", "log", 0, 0),
     (40000, 9, 50000, 50000, 0, 0.1, "f32", "int32", "distinct", 0, 0),
+    # every kernel: types, whole blocks or not, dropout or not
+    (200, 33, 50, 40, 5, 0.0, "bf16", "int64", "log", 1, 1),
+    (200, 64, 50, 40, 5, 0.1, "f32", "int64", "log", 0, 0),
+    (200, 63, 50, 40, 5, 0.1, "f32", "int64", "log", 3, 1),
+    (700, 33, 60, 50, 5, 0.0, "bf16", "int64", "log", 1, 1),
     # three levels of merging
     (1100003, 3, 60000, 50000, 100, 0.0, "f32", "int64", "log", 0, 0),
     (1048577, 1, 3, 3, 0, 0.0, "f32", "int64", "log", 0, 0),
@@ -372,7 +382,10 @@ def test_dropout(case):
                                             (1024, 512, 0.25, "f32", True, False, 0, 0),
                                             (256, 8189, 0.1, "f32", True, False, 3, 0),
                                             (1024, 2051, 0.1, "f32", True, False, 0, 0),
-                                            (3, 2796208, 0.1, "f32", True, False, 0, 0)],
+                                            (3, 2796208, 0.1, "f32", True, False, 0, 0)]
+                         # every kernel: types, whole blocks or not, dropout or not, few rows or many
+                         + [(rows, cols, p, dtype, True, False, 1, 1) for rows in (40, 1100) for cols in (64, 63)
+                            for p in (0.0, 0.1) for dtype in ("bf16", "f32")],
                          ids=lambda c: "-".join(map(str, c)))
 def test_dropout_grad(case, accumulate):
     rows, cols, p, dtype, bias, _, more, shift = case
@@ -518,6 +531,8 @@ ADAM = [
     (1021, 5, 100000, 0.1, 2.0, False),
     (70001, 2, 3, 0.01, None, False),
     (4096, 0, 1, 0.0, None, True),
+    # a launch that reserves LDS
+    (3000003, 5, 7, 0.01, 0.5, False),
 ]
 
 
