@@ -460,7 +460,7 @@ ETC_API int etc_unpack_kind(const etc_plan_t* plan, int dst_rank, int kind, cons
  * arguments alone: every sum has a fixed order (no atomics), so the same call
  * gives the same bits.  Matrices of no elements may have data NULL; a call
  * without work returns ETC_OK.  An input may overlap an output only where a
- * call says so.
+ * call says so.  Factors are used in 32 bits and have to be finite there.
  * Errors of all: INVALID_ARG (NULL, a size, type or stride that does not fit),
  * ALIGN (a pointer not aligned to its elements, an arena or workspace not to
  * 256 bytes), UNSUPPORTED (more than 2^31 - 1 ids, rows of a table or columns),

@@ -99,8 +99,11 @@ int check_workspace(const void* p, uint64_t bytes, uint64_t need) {
   return ETC_OK;
 }
 
+// what a kernel multiplies with: an infinity would turn zeros into NaN
+bool finite32(double x) { return std::isfinite(float(x)); }
+
 int check_scale(double scale) {
-  return std::isfinite(scale) ? int(ETC_OK) : fail(ETC_ERR_INVALID_ARG, "scale must be finite");
+  return finite32(scale) ? int(ETC_OK) : fail(ETC_ERR_INVALID_ARG, "scale must be finite, in 32 bits");
 }
 
 }  // namespace

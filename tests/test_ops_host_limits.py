@@ -1,0 +1,19 @@
+"""The edges of what the operators' C ABI accepts, without a GPU: constants
+that 32 bits do not hold, and calls without work."""
+import test_ops_host as ops
+from paper_2607_04749_amd import etc
+
+INVALID, OK = etc.ERR_INVALID_ARG, etc.OK
+FLT_MAX = (2 - 2.0 ** -23) * 2.0 ** 127
+
+
+def test_scale_has_to_fit_32_bits():
+    """The kernels multiply in 32 bits, where a larger scale is infinite and
+    makes NaN of the zeros that ids outside the table count as."""
+    for scale in (1e39, -1e39, 1e300, FLT_MAX * (1 + 2.0 ** -24)):
+        assert ops.embed(scale=scale) == INVALID and "scale" in etc.last_error()
+        assert ops.embed_grad(scale=scale) == INVALID and "scale" in etc.last_error()
+    none = dict(tokens=ops.ids(0, ptr=0))
+    for scale in (FLT_MAX, -FLT_MAX, 1e-300, 0.0):
+        assert ops.embed(out=ops.mat(0, 16, ptr=0), scale=scale, **none) == OK
+        assert ops.embed_grad(grad=ops.mat(0, 16, ptr=0), accumulate=1, scale=scale, **none) == OK
