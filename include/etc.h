@@ -583,6 +583,8 @@ ETC_API int etc_dropout_grad_workspace(int64_t rows, int64_t cols, uint64_t* byt
  *                 + weight_decay master)
  *   param = master rounded to bf16, to nearest even
  * grad_scale is one fp32 number in device memory, such as a clipping factor.
+ * lr / (1 - beta1^step), lr weight_decay and eps are rounded to 32 bits; it is
+ * INVALID_ARG if one becomes infinite, or a positive eps zero.
  * A whole arena is one range; the elements between its tensors, which no
  * migration reads, are stepped with it. */
 typedef struct {

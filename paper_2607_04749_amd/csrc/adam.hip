@@ -13,7 +13,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "ops.hpp"
 
@@ -29,15 +28,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 struct AdamArgs {
+  AdamFactors f;
   bf16* param;
   float *master, *m, *v;
   const float *grad, *grad_scale;
   uint64_t first, end;  // the range
   uint64_t start;       // of the launch: the first unit's first element
-  float beta1, rest1, beta2, rest2;  // rest = 1 - beta, from 64 bits
-  float step_size;                   // lr / (1 - beta1^t)
-  float root;                        // 1 / (1 - beta2^t)
-  float eps, decay;                  // decay = lr * weight_decay
 };
 
 // A lane steps the four elements of one 16-byte unit of the fp32 arenas, as far
@@ -46,9 +42,9 @@ constexpr uint32_t kUnit = 4;
 
 __device__ __forceinline__ void adam_step(const AdamArgs& a, float c, float grad, float& w, float& m, float& v) {
   const float g = grad * c;
-  m = a.beta1 * m + a.rest1 * g;
-  v = a.beta2 * v + a.rest2 * (g * g);
-  w -= a.step_size * m / (sqrtf(v * a.root) + a.eps) + a.decay * w;
+  m = a.f.beta1 * m + a.f.rest1 * g;
+  v = a.f.beta2 * v + a.f.rest2 * (g * g);
+  w -= a.f.step_size * m / (sqrtf(v * a.f.root) + a.f.eps) + a.f.decay * w;
 }
 
 __global__ __launch_bounds__(kThreads) void adam_kernel(AdamArgs a) {
@@ -85,8 +81,8 @@ __global__ __launch_bounds__(kThreads) void adam_kernel(AdamArgs a) {
 
 }  // namespace
 
-hipError_t launch_adam(const etc_adam_args& x, hipStream_t stream) {
-  AdamArgs a{};
+hipError_t launch_adam(const etc_adam_args& x, const AdamFactors& factors, hipStream_t stream) {
+  AdamArgs a{factors};
   a.param = static_cast<bf16*>(x.arena[0]);
   a.master = static_cast<float*>(x.arena[1]);
   a.m = static_cast<float*>(x.arena[2]);
@@ -95,14 +91,6 @@ hipError_t launch_adam(const etc_adam_args& x, hipStream_t stream) {
   a.grad_scale = static_cast<const float*>(x.grad_scale);
   a.first = x.first;
   a.end = x.first + x.count;
-  a.beta1 = float(x.beta1);
-  a.rest1 = float(1.0 - x.beta1);
-  a.beta2 = float(x.beta2);
-  a.rest2 = float(1.0 - x.beta2);
-  a.step_size = float(x.lr / (1.0 - std::pow(x.beta1, double(x.step))));
-  a.root = float(1.0 / (1.0 - std::pow(x.beta2, double(x.step))));
-  a.eps = float(x.eps);
-  a.decay = float(x.lr * x.weight_decay);
   constexpr uint64_t most = uint64_t(1) << 32;  // elements of a launch: 2^30 lanes
   for (a.start = x.first / kUnit * kUnit; a.start < a.end; a.start += most) {
     const uint64_t units = (std::min(a.end - a.start, most) + kUnit - 1) / kUnit;

@@ -210,6 +210,9 @@ int etc_adam(const etc_adam_args* a, void* stream) {
   if (!(a->eps >= 0.0) || !std::isfinite(a->eps) || !std::isfinite(a->lr) || !std::isfinite(a->weight_decay))
     return fail(ETC_ERR_INVALID_ARG, "lr, eps and weight_decay must be finite, eps not negative");
   if (a->step < 1) return fail(ETC_ERR_INVALID_ARG, "step counts from 1");
+  const etc::AdamFactors f(*a);
+  if (!std::isfinite(f.step_size) || !std::isfinite(f.decay) || !std::isfinite(f.eps) || (a->eps > 0.0 && f.eps == 0.0f))
+    return fail(ETC_ERR_INVALID_ARG, "lr / (1 - beta1^step), lr * weight_decay or eps does not fit 32 bits");
   if (a->count == 0) return ETC_OK;
   for (int k = 0; k < 4; ++k) {
     if (!a->arena[k]) return fail(ETC_ERR_INVALID_ARG, "arena[%d] is NULL", k);
@@ -218,7 +221,7 @@ int etc_adam(const etc_adam_args* a, void* stream) {
   if (!a->grad) return fail(ETC_ERR_INVALID_ARG, "grad is NULL");
   if (!aligned(a->grad, 256)) return fail(ETC_ERR_ALIGN, "grad is not 256-byte aligned");
   if (!aligned(a->grad_scale, 4)) return fail(ETC_ERR_ALIGN, "grad_scale is not 4-byte aligned");
-  return launched(etc::launch_adam(*a, static_cast<hipStream_t>(stream)), "adam");
+  return launched(etc::launch_adam(*a, f, static_cast<hipStream_t>(stream)), "adam");
 }
 
 }  // extern "C"

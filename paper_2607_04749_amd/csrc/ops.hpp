@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -268,10 +269,23 @@ EmbedGradSizes embed_grad_sizes(uint64_t ntokens, uint64_t rows, uint64_t cols);
 bool embed_grad_fits(uint64_t ntokens, uint64_t cols);
 uint64_t dropout_grad_bytes(uint64_t rows, uint64_t cols);
 
+// What an Adam step multiplies with, worked out in 64 bits.
+struct AdamFactors {
+  float beta1, rest1, beta2, rest2;  // rest = 1 - beta
+  float step_size;                   // lr / (1 - beta1^t)
+  float root;                        // 1 / (1 - beta2^t)
+  float eps, decay;                  // decay = lr * weight_decay
+  explicit AdamFactors(const etc_adam_args& x)
+      : beta1(float(x.beta1)), rest1(float(1.0 - x.beta1)), beta2(float(x.beta2)), rest2(float(1.0 - x.beta2)),
+        step_size(float(x.lr / (1.0 - std::pow(x.beta1, double(x.step))))),
+        root(float(1.0 / (1.0 - std::pow(x.beta2, double(x.step))))), eps(float(x.eps)),
+        decay(float(x.lr * x.weight_decay)) {}
+};
+
 hipError_t launch_embed(const etc_embed_args& a, const Drop& drop, hipStream_t stream);
 hipError_t launch_embed_grad(const etc_embed_grad_args& a, const Drop& drop, hipStream_t stream);
 hipError_t launch_dropout(const etc_dropout_args& a, const Drop& drop, hipStream_t stream);
 hipError_t launch_dropout_grad(const etc_dropout_grad_args& a, const Drop& drop, hipStream_t stream);
-hipError_t launch_adam(const etc_adam_args& a, hipStream_t stream);
+hipError_t launch_adam(const etc_adam_args& a, const AdamFactors& factors, hipStream_t stream);
 
 }  // namespace etc

@@ -17,3 +17,15 @@ def test_scale_has_to_fit_32_bits():
     for scale in (FLT_MAX, -FLT_MAX, 1e-300, 0.0):
         assert ops.embed(out=ops.mat(0, 16, ptr=0), scale=scale, **none) == OK
         assert ops.embed_grad(grad=ops.mat(0, 16, ptr=0), accumulate=1, scale=scale, **none) == OK
+
+
+def test_adam_constants_have_to_fit_32_bits():
+    """lr / (1 - beta1^step), lr * weight_decay and eps, as the kernel has
+    them: an infinite one makes NaN of elements that are zero, and so does an eps
+    that vanishes, where the root does too."""
+    for bad in (dict(lr=1e39), dict(lr=-1e300), dict(lr=1e38, b1=0.999, step=1), dict(lr=1e20, wd=1e20), dict(wd=1e300, lr=1.0),
+                dict(eps=1e39), dict(eps=1e-60)):
+        assert ops.adam(**bad) == INVALID and etc.last_error(), bad
+    for good in (dict(lr=1e37), dict(lr=1e38, b1=0.999, step=1 << 40), dict(lr=1e-20, wd=1e39), dict(lr=1e-300, wd=1e-300), dict(eps=0.0),
+                 dict(eps=1e-45), dict(b1=0.0, b2=0.0)):
+        assert ops.adam(count=0, **good) == OK, (good, etc.last_error())
