@@ -518,7 +518,7 @@ typedef struct {
   etc_ids tokens, positions;
   etc_matrix table, pos_table, out;
   etc_dropout_desc drop;
-  int64_t row0;            /* id of the table's first row */
+  int64_t row0;            /* id of the table's first row; row0 + rows < 2^63 */
   double scale;
 } etc_embed_args;
 ETC_API int etc_embed(const etc_embed_args* args, void* stream);

@@ -106,6 +106,11 @@ int check_scale(double scale) {
   return finite32(scale) ? int(ETC_OK) : fail(ETC_ERR_INVALID_ARG, "scale must be finite, in 32 bits");
 }
 
+// the ids row0 .. row0 + rows of a table: an id minus row0 must not wrap into them
+int check_row0(int64_t row0, int64_t rows) {
+  return row0 <= INT64_MAX - rows ? int(ETC_OK) : fail(ETC_ERR_INVALID_ARG, "row0 is out of range");
+}
+
 }  // namespace
 
 extern "C" {
@@ -116,6 +121,7 @@ int etc_embed(const etc_embed_args* a, void* stream) {
   int rc;
   if ((rc = check_ids(a->tokens, "tokens")) || (rc = check_matrix(a->table, "table", kIn)) ||
       (rc = check_matrix(a->out, "out", kOut)) || (rc = check_scale(a->scale)) ||
+      (rc = check_row0(a->row0, a->table.rows)) ||
       (rc = check_drop(a->drop, a->out.rows, &drop)))
     return rc;
   if (a->out.rows != a->tokens.count) return fail(ETC_ERR_INVALID_ARG, "out needs one row per token");
@@ -149,6 +155,7 @@ int etc_embed_grad(const etc_embed_grad_args* a, void* stream) {
   int rc;
   if ((rc = check_ids(a->tokens, "tokens")) || (rc = check_matrix(a->grad, "grad", kIn)) ||
       (rc = check_matrix(a->dtable, "dtable", kOut)) || (rc = check_scale(a->scale)) ||
+      (rc = check_row0(a->row0, a->dtable.rows)) ||
       (rc = check_drop(a->drop, a->grad.rows, &drop)))
     return rc;
   if (a->grad.rows != a->tokens.count) return fail(ETC_ERR_INVALID_ARG, "grad needs one row per token");

@@ -29,3 +29,16 @@ def test_adam_constants_have_to_fit_32_bits():
     for good in (dict(lr=1e37), dict(lr=1e38, b1=0.999, step=1 << 40), dict(lr=1e-20, wd=1e39), dict(lr=1e-300, wd=1e-300), dict(eps=0.0),
                  dict(eps=1e-45), dict(b1=0.0, b2=0.0)):
         assert ops.adam(count=0, **good) == OK, (good, etc.last_error())
+
+
+def test_row0_ends_inside_64_bits():
+    """Ids of the table's rows are 64-bit numbers: past their end, an id minus
+    row0 wraps, and the lowest ids would name rows of the table."""
+    end = (1 << 63) - 1
+    for row0, code in ((end, INVALID), (end - 8, INVALID), (end - 9, OK), (-end - 1, OK)):
+        pack = etc._EMBED.pack(*ops.ids(0, ptr=0), *ops.NO_IDS, *ops.mat(9, 16), *ops.NONE, *ops.mat(0, 16, ptr=0),
+                               *ops.drop(), row0, 1.0)
+        assert etc.lib().etc_embed(pack, None) == code, row0
+        pack = etc._EMBED_GRAD.pack(*ops.ids(0, ptr=0), *ops.mat(0, 16, ptr=0), *ops.mat(9, 16, etc.DTYPE_F32), *ops.drop(),
+                                    row0, 1.0, 0, 0, 1, 0)
+        assert etc.lib().etc_embed_grad(pack, None) == code, row0
