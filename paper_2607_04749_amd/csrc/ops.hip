@@ -126,9 +126,10 @@ int etc_embed(const etc_embed_args* a, void* stream) {
     return rc;
   if (a->out.rows != a->tokens.count) return fail(ETC_ERR_INVALID_ARG, "out needs one row per token");
   if (a->out.cols != a->table.cols) return fail(ETC_ERR_INVALID_ARG, "out and table differ in columns");
-  // an empty table has columns, an absent one none; no tokens need no pointer to their positions
+  // an empty table has columns, an absent one none, unless there are no columns at all; no tokens need no
+  // pointer to their positions
   const bool pos = a->pos_table.data || a->pos_table.cols != 0;
-  if (a->tokens.count && pos != (a->positions.data != nullptr))
+  if (a->tokens.count && a->out.cols && pos != (a->positions.data != nullptr))
     return fail(ETC_ERR_INVALID_ARG, "positions and pos_table go together");
   if (pos) {
     if ((rc = check_ids(a->positions, "positions")) || (rc = check_matrix(a->pos_table, "pos_table", kIn))) return rc;

@@ -42,3 +42,12 @@ def test_row0_ends_inside_64_bits():
         pack = etc._EMBED_GRAD.pack(*ops.ids(0, ptr=0), *ops.mat(0, 16, ptr=0), *ops.mat(9, 16, etc.DTYPE_F32), *ops.drop(),
                                     row0, 1.0, 0, 0, 1, 0)
         assert etc.lib().etc_embed_grad(pack, None) == code, row0
+
+
+def test_lookup_of_no_columns_with_positions():
+    """Matrices of no columns need no data: there is no work, and no refusal,
+    with positions as without."""
+    none = dict(table=ops.mat(9, 0, ptr=0), out=ops.mat(3, 0, ptr=0))
+    assert ops.embed(**none) == OK
+    assert ops.embed(positions=ops.ids(3), pos=ops.mat(4, 0, ptr=0), **none) == OK, etc.last_error()
+    assert ops.embed(positions=ops.ids(3)) == INVALID
