@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from math import prod
 from operator import index
 
 import numpy as np
@@ -575,7 +576,7 @@ def _matrix(x, what, device):
     if not shape or not x.is_contiguous():
         raise ValueError(f"{what} must have two dimensions or be contiguous")
     cols = shape[-1]
-    return x.data_ptr(), x.numel() // cols if cols else 0, cols, cols, dtype, 0
+    return x.data_ptr(), x.numel() // cols if cols else prod(shape[:-1]) if len(shape) > 1 else 0, cols, cols, dtype, 0
 
 
 def _ids(x, what, device):
