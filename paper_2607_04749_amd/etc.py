@@ -579,6 +579,17 @@ def _matrix(x, what, device):
     return x.data_ptr(), x.numel() // cols if cols else prod(shape[:-1]) if len(shape) > 1 else 0, cols, cols, dtype, 0
 
 
+def _optional(x, what, device, of):
+    """Fields of an etc_matrix that may be absent (None) and has elements if
+    `of`, what it goes with, has: an empty tensor's pointer is that of an absent one."""
+    if x is None:
+        return _NO_MATRIX
+    m = _matrix(x, what, device)
+    if not m[0] and of:
+        raise ValueError(f"{what} has no elements")
+    return m
+
+
 def _ids(x, what, device):
     dtype = _IDS_DTYPES.get(x.dtype)
     if dtype is None:
@@ -628,9 +639,9 @@ def etc_embed_grad(tokens, grad, dtable, workspace, row0=0, scale=1.0, dropout=N
 def etc_dropout(x, out, dropout=None, bias=None, residual=None, stream=None):
     """out = residual + drop(x + bias); out may be x or residual itself."""
     d = _device_of(out, "out")
-    b = _NO_MATRIX if bias is None else _matrix(bias, "bias", d)
-    r = _NO_MATRIX if residual is None else _matrix(residual, "residual", d)
-    _check(_lib.etc_dropout(_DROPOUT.pack(*_matrix(x, "x", d), *b, *r, *_matrix(out, "out", d), *_drop(dropout)),
+    m = _matrix(x, "x", d)
+    b, r = _optional(bias, "bias", d, m[2]), _optional(residual, "residual", d, m[1] and m[2])
+    _check(_lib.etc_dropout(_DROPOUT.pack(*m, *b, *r, *_matrix(out, "out", d), *_drop(dropout)),
                             _stream_on(stream, d)), "etc_dropout")
 
 
@@ -644,8 +655,9 @@ def etc_dropout_grad_bytes(rows, cols):
 def etc_dropout_grad(grad, dx, dropout=None, dbias=None, workspace=None, accumulate=False, stream=None):
     """dx = drop'(grad) (dx may be grad itself); dbias (float32) = or += its sum over rows."""
     d = _device_of(dx, "dx")
-    b = _NO_MATRIX if dbias is None else _matrix(dbias, "dbias", d)
-    _check(_lib.etc_dropout_grad(_DROPOUT_GRAD.pack(*_matrix(grad, "grad", d), *_matrix(dx, "dx", d), *b,
+    m = _matrix(grad, "grad", d)
+    b = _optional(dbias, "dbias", d, m[2])
+    _check(_lib.etc_dropout_grad(_DROPOUT_GRAD.pack(*m, *_matrix(dx, "dx", d), *b,
                                                     *_drop(dropout), *_workspace(workspace, d), bool(accumulate), 0),
                                  _stream_on(stream, d)), "etc_dropout_grad")
 
