@@ -518,6 +518,7 @@ _DROPOUT = struct.Struct("@" + 4 * _MATRIX + _DROP)
 _DROPOUT_GRAD = struct.Struct("@" + 3 * _MATRIX + _DROP + "PQii")
 _ADAM = struct.Struct("@4PPPQQdddddq")
 _MATRIX_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+_KIND_DTYPES = (torch.bfloat16, torch.float32, torch.float32, torch.float32)  # of the arenas
 _IDS_DTYPES = {torch.int32: IDS_I32, torch.int64: IDS_I64}
 
 
@@ -662,12 +663,28 @@ def etc_dropout_grad(grad, dx, dropout=None, dbias=None, workspace=None, accumul
                                  _stream_on(stream, d)), "etc_dropout_grad")
 
 
+def _stepped(x, dtype, need, device, what, at=None):
+    """Pointer of what a step reads or writes `need` bytes of: a tensor of its
+    type, or of bytes; an integer pointer is passed through as given."""
+    if x is None or isinstance(x, int):
+        return x or 0
+    t = x.dtype
+    if t != dtype and t != torch.uint8:
+        raise ValueError(f"{_item(what, at)} must be {str(dtype)[6:]} or bytes (uint8), not {t}")
+    if x.get_device() != device or not x.is_contiguous():
+        raise ValueError(f"{_item(what, at)} must be a contiguous tensor on the current GPU")
+    n = x.nbytes
+    if n < need:
+        raise ValueError(f"{_item(what, at)} holds {n} bytes; the range needs {need}")
+    return x.data_ptr()
+
+
 def etc_adam(arenas, grad, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, first=0,
              count=None, stream=None):
     """One Adam step over elements [first, first + count) of a rank's four
     arenas (by default all from `first` on), in place.  grad: an fp32 arena of
-    the same layout; grad_scale: one float32 on the GPU, or None.  Tensors are
-    checked against the range (ValueError if short)."""
+    the same layout; grad_scale: one float32 on the GPU, or None.  Tensors, of
+    the arenas' types or of bytes, are checked against the range (ValueError if short)."""
     if len(arenas) != 4:
         raise ValueError(f"arenas needs 4 arenas, got {len(arenas)}")
     first = index(first)
@@ -677,11 +694,13 @@ def etc_adam(arenas, grad, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_de
     if first < 0 or count < 0:
         raise ValueError("first and count must not be negative")
     end = first + count
-    a = [_buf(arenas[k], end * ESIZE[k], "arenas", k) or 0 for k in range(4)]
-    s = 0
+    d = _current_device()
+    a = [_stepped(arenas[k], _KIND_DTYPES[k], end * ESIZE[k], d, "arenas", k) for k in range(4)]
+    g, c = _stepped(grad, torch.float32, 4 * end, d, "grad"), 0
     if grad_scale is not None:
         if not isinstance(grad_scale, int) and grad_scale.dtype != torch.float32:
             raise ValueError("grad_scale must be float32")
-        s = _buf(grad_scale, 4, "grad_scale")
-    _check(_lib.etc_adam(_ADAM.pack(*a, _buf(grad, 4 * end, "grad") or 0, s, first, count, lr, beta1, beta2, eps,
-                                    weight_decay, step), _stream(stream)), "etc_adam")
+        c = _stepped(grad_scale, torch.float32, 4, d, "grad_scale")
+    # pointers alone do not say that torch knows the GPU by now
+    s = _stream(stream) if isinstance(grad, int) else _stream_on(stream, d)
+    _check(_lib.etc_adam(_ADAM.pack(*a, g, c, first, count, lr, beta1, beta2, eps, weight_decay, step), s), "etc_adam")

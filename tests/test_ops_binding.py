@@ -53,3 +53,34 @@ def test_an_empty_tensor_is_not_an_absent_one(calls):
     etc.etc_dropout(x[:, :0], x[:, :0], drop, bias=x[0, :0], residual=x[:, :0], stream=0)
     etc.etc_dropout_grad(x[:, :0], x[:, :0], drop, dbias=x[0, :0].float(), stream=0)
     assert len(calls) == 3
+
+
+def test_adam_takes_no_other_types(calls, monkeypatch):
+    """The parameter's arena is bfloat16, the others and the gradients float32,
+    each also as bytes; a tensor of another type and enough bytes is refused, and so
+    is one of another device."""
+    monkeypatch.setattr(etc, "_current_device", lambda: -1)
+    n = 64
+    right = [torch.zeros(n, dtype=t) for t in (BF16, F32, F32, F32, F32)]
+
+    def step(*tensors):
+        etc.etc_adam(tensors[:4], tensors[4], step=1, lr=1e-3, count=n, stream=0)
+
+    for k, wrong in ((0, (F32, torch.float16, torch.int16, torch.int64)),
+                     *((k, (BF16, torch.float64, torch.int32, torch.float16)) for k in (1, 2, 3, 4))):
+        for dtype in wrong:
+            with pytest.raises(ValueError, match="bfloat16" if k == 0 else "float32"):
+                step(*right[:k], torch.zeros(2 * n, dtype=dtype), *right[k + 1:])
+    for k in range(5):
+        with pytest.raises(ValueError, match="bytes"):
+            step(*right[:k], right[k][:-1], *right[k + 1:])
+        with pytest.raises(ValueError, match="contiguous"):
+            step(*right[:k], torch.zeros(2 * n, dtype=right[k].dtype)[::2], *right[k + 1:])
+    with monkeypatch.context() as m, pytest.raises(ValueError, match="current GPU"):
+        m.setattr(etc, "_current_device", lambda: 1)
+        step(*right)
+    assert not calls
+    step(*right)
+    step(*(x.view(torch.uint8) for x in right))
+    etc.etc_adam([x.data_ptr() for x in right[:4]], right[4].data_ptr(), step=1, lr=1e-3, count=n, stream=0)
+    assert len(calls) == 3 and len({packed for _, packed in calls}) == 1
