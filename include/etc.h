@@ -511,9 +511,12 @@ typedef struct {
  * another rank's share of the vocabulary, or padding) contributes nothing, a
  * position outside pos_table likewise.  table and pos_table are of one type,
  * out of either; positions and pos_table are both given or both absent, and
- * positions has the tokens' count.  drop.p = 0: no dropout.  With TP > 1 the
- * caller adds the ranks' results, and passes pos_table and dropout where they
- * are to be applied once. */
+ * positions has the tokens' count.  drop.p = 0: no dropout.
+ * With TP > 1 scale, positions and dropout are applied once, to the sum of the
+ * ranks' rows: each rank looks its share up with scale 1 and nothing else, the
+ * caller adds the results, of which one per token is not zero, and a second call takes
+ * the sum as its table, with tokens 0, 1, 2, .. and row0 = 0.  With table,
+ * sum and shares of one type that gives the bits of one call on the whole table. */
 typedef struct {
   etc_ids tokens, positions;
   etc_matrix table, pos_table, out;
