@@ -14,8 +14,7 @@ ranks of a configuration run on one GPU here, one after another.
   reshard    etc_pack on the old ranks, etc_unpack on the new ones
 
 A dropped element depends on (seed, call, row, column), a table's row sums its
-tokens in an order that no other row enters (in a batch as short as
-this one; a longer one's are grouped across rows), and Adam treats each element
+tokens in an order that the batch's ids alone decide, and Adam treats each element
 alone, so what a step computes does not depend on how many ranks share the
 tables: six steps with a change from TP 2 to TP 4 after the third end in the
 states of six steps on TP 2.

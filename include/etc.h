@@ -535,7 +535,8 @@ ETC_API int etc_embed(const etc_embed_args* args, void* stream);
  * those are not touched.  The gradient of pos_table is the same with the
  * positions as ids and scale 1.
  * The ids are sorted first, then each run of equal ids is summed; ids outside
- * the table are skipped.  More than 2^27 tokens, or about 2^37 elements of grad, are
+ * the table are skipped.  For the same tokens and gradients a row has the same bits
+ * whichever rows the table holds beside it, so on any number of ranks.  More than 2^27 tokens, or about 2^37 elements of grad, are
  * UNSUPPORTED.  workspace: etc_embed_grad_workspace's bytes, for the same sizes or
  * larger ones. */
 typedef struct {

@@ -11,7 +11,9 @@
 // one: a wavefront sums one chunk over 512 columns and writes the rows whose
 // runs lie inside it.  The parts of a run that crosses chunks go to the
 // workspace and are joined afterwards.
-// All sums are in 32 bits and in a fixed order.
+// All sums are in 32 bits and in a fixed order.  Ids below the table come first in
+// the list and ids above it last, so the cuts lie in the same places of every run
+// whichever rows the table holds: a share's gradient has the bits of the whole's.
 //
 // The sums are HBM bound (a row of grad per token and of dtable per row, and the
 // parts); the other launches are a few waits long.  bf16 gradients, MI355X, in us:
@@ -36,20 +38,29 @@ namespace etc {
 namespace {
 
 constexpr uint32_t kWave = 64;
-constexpr uint32_t kNone = 0xFFFFFFFFu;  // no key: keys are at most 2^31 - 1
-
-// A token's key: its row of the table, or `rows` for ids outside it, which sort last.
-__device__ __forceinline__ uint32_t key_of(const Ids& ids, int64_t row0, uint32_t rows, uint32_t i) {
-  const uint64_t k = uint64_t(ids.at(i)) - uint64_t(row0);
-  return k < rows ? uint32_t(k) : rows;
-}
+constexpr uint32_t kNone = 0xFFFFFFFFu;  // no row and no key: those are at most 2^31
 
 struct Tokens {
   Ids ids;
   int64_t row0;
   uint32_t rows, n;
-  __device__ __forceinline__ uint32_t key(uint32_t i) const { return key_of(ids, row0, rows, i); }
+  // token i's row of the table, or `rows` for ids outside it
+  __device__ __forceinline__ uint32_t row(uint32_t i) const {
+    const uint64_t k = uint64_t(ids.at(i)) - uint64_t(row0);
+    return k < rows ? uint32_t(k) : rows;
+  }
+  // What tokens are ordered by: row + 1, with ids below the table before all of
+  // its rows and ids above after them.  So a row's tokens have the places that they
+  // have in the order of all ids, whichever of the rows the table holds.
+  __device__ __forceinline__ uint32_t key(uint32_t i) const {
+    const int64_t id = ids.at(i);
+    const uint64_t k = uint64_t(id) - uint64_t(row0);
+    return id < row0 ? 0 : (k < rows ? uint32_t(k) : rows) + 1;
+  }
 };
+
+// Of a key: whether it is a row's.
+__device__ __forceinline__ bool is_row(uint32_t key, uint32_t rows) { return key - 1 < rows; }
 
 // LDS that the lanes of one wavefront exchange through: its accesses are in
 // order, so only the compiler has to be kept from moving them.
@@ -241,8 +252,8 @@ __device__ __forceinline__ void fill_rows(const SumArgs& a, const Mat<float>& ou
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t waves = (gridDim.x - a.sum_wgs) * kSumWaves;
   for (uint32_t r = (blockIdx.x - a.sum_wgs) * kSumWaves + threadIdx.x / kWave; r < a.rows; r += waves) {
-    const uint32_t at = lower_bound(a.keys, a.n, r, lane);
-    if (at == a.n || a.keys[at] != r) zero_row(a, out, r, lane);
+    const uint32_t at = lower_bound(a.keys, a.n, r + 1, lane);
+    if (at == a.n || a.keys[at] != r + 1) zero_row(a, out, r, lane);
   }
 }
 
@@ -261,12 +272,13 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   const uint32_t lo = chunk * a.chunk, size = min(a.chunk, a.n - lo);
   const uint32_t key = lane < size ? a.keys[lo + lane] : kNone, token = lane < size ? a.order[lo + lane] : 0;
   const uint32_t prev = lo > 0 ? a.keys[lo - 1] : kNone, next = lo + size < a.n ? a.keys[lo + size] : kNone;
-  const uint32_t inside = uint32_t(__popcll(__ballot(key < a.rows)));  // the others come last
-  if (inside == 0) return;
+  const uint64_t held = __ballot(is_row(key, a.rows));  // consecutive ones: begin .. end
+  if (held == 0) return;
+  const uint32_t begin = uint32_t(__builtin_ctzll(held)), end = begin + uint32_t(__popcll(held));
   const uint32_t after = __shfl_down(key, 1);
-  const uint64_t ends = __ballot(lane < inside && (lane + 1 == size ? next : after) != key);
+  const uint64_t ends = __ballot(is_row(key, a.rows) && (lane + 1 == size ? next : after) != key);
   // the run that began in an earlier chunk: its end here goes to the parts, not to the table
-  uint32_t came = __builtin_amdgcn_readfirstlane(key) == prev ? (ends ? uint32_t(__builtin_ctzll(ends)) : inside) : kNone;
+  uint32_t came = begin == 0 && __builtin_amdgcn_readfirstlane(key) == prev ? (ends ? uint32_t(__builtin_ctzll(ends)) : end) : kNone;
 
   const uint64_t col = (uint64_t(job - chunk * a.slabs) * kWave + lane) * kC;
   const uint32_t width = block_width<kC>(col, a.cols);
@@ -275,26 +287,26 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
   // lanes past the columns load block 0, so that the loads are in one piece of code without branches
   const uint64_t from = width ? col : 0;
   const uint32_t span = width ? width : block_width<kC>(0, a.cols);
-  for (uint32_t e0 = 0; e0 < inside; e0 += kBatch) {
+  for (uint32_t e0 = begin; e0 < end; e0 += kBatch) {
     uint32_t i[kBatch], row[kBatch];
     Raw<T, kC, kWhole> raw[kBatch];
     Raw<float, kC, kWhole> before[kBatch];
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
-      const uint32_t e = min(e0 + b, inside - 1);
+      const uint32_t e = min(e0 + b, end - 1);
       i[b] = __builtin_amdgcn_readlane(token, e);
-      row[b] = __builtin_amdgcn_readlane(key, e);
+      row[b] = __builtin_amdgcn_readlane(key, e) - 1;
       raw[b].template load<true>(grad.p + int64_t(i[b]) * grad.ld + from, span, a.cols < kC);
     }
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b)
-      if (kAdd && e0 + b < inside && (ends >> (e0 + b) & 1) && e0 + b != came)
+      if (kAdd && e0 + b < end && (ends >> (e0 + b) & 1) && e0 + b != came)
         before[b].load(out.p + int64_t(row[b]) * out.ld + from, span, a.cols < kC);
     compiler_fence();
 #pragma unroll
     for (uint32_t b = 0; b < kBatch; ++b) {
       const uint32_t e = e0 + b;
-      if (e >= inside) break;
+      if (e >= end) break;
       uint32_t bits[kC / 2];
       if (kDrop) a.drop.template bits<kC>(i[b], col, bits);
       float v[kC];
@@ -313,7 +325,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a, Mat<const T
     }
   }
   // a run that goes on: part 0 where it fills the chunk and came in, else part 1
-  if (!(ends >> (inside - 1) & 1) && width) store_block<kWhole>(parts + (came == inside ? 0 : a.cols), width, sum);
+  if (!(ends >> (end - 1) & 1) && width) store_block<kWhole>(parts + (came == end ? 0 : a.cols), width, sum);
 }
 
 constexpr uint32_t kJoinWaves = 4;
@@ -330,7 +342,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
   const uint32_t run = a.keys[hi - 1], prev = lo > 0 ? a.keys[lo - 1] : kNone, head = a.keys[lo];
   uint32_t next = chunk + 1 + lane;
   uint32_t key = next < a.chunks ? a.keys[next * a.chunk] : kNone;
-  if (run >= a.rows || __builtin_amdgcn_readfirstlane(key) != run) return;
+  if (!is_row(run, a.rows) || __builtin_amdgcn_readfirstlane(key) != run) return;
   if (head == run && prev == run) return;  // it began before this chunk
   // the chunks that the run reaches: those whose first key is the run's
   uint32_t parts = 0;
@@ -347,7 +359,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
   Raw<float, kC, kWhole> before;
   before.zero();
   if (width) {
-    if (wave == 0) read_row(a, out, run, col, width, before);
+    if (wave == 0) read_row(a, out, run - 1, col, width, before);
     // part 0 is this chunk's own
     for (uint32_t k0 = wave; k0 <= parts; k0 += kJoinWaves * kJoinBatch) {
       Raw<float, kC, kWhole> part[kJoinBatch];
@@ -375,7 +387,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_kernel(SumArgs a, Mat<
   for (uint32_t w = 1; w < kJoinWaves; ++w)
 #pragma unroll
     for (uint32_t e = 0; e < kC; ++e) sum[e] += shared[w][lane][e];
-  finish_row<true>(a, out, run, col, width, sum, before);
+  finish_row<true>(a, out, run - 1, col, width, sum, before);
 }
 
 // ---------------------------------------------------------------------------
@@ -398,11 +410,11 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   __shared__ float shared[kSumWaves][kWave][kC];
   __shared__ uint32_t seen[kFillMost];
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  uint32_t key[kFewEach];
+  uint32_t rows[kFewEach];
 #pragma unroll
   for (uint32_t p = 0; p < kFewEach; ++p) {
     const uint32_t i = p * kSumThreads + threadIdx.x;
-    key[p] = i < t.n ? t.key(i) : kNone;
+    rows[p] = i < t.n ? t.row(i) : kNone;
   }
   if (blockIdx.x >= a.sum_wgs) {
     for (uint64_t first = uint64_t(blockIdx.x - a.sum_wgs) * a.fill_rows; first < a.rows;
@@ -411,7 +423,7 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
       __syncthreads();
 #pragma unroll
       for (uint32_t p = 0; p < kFewEach; ++p)
-        if (key[p] < a.rows && key[p] >= first && key[p] - first < a.fill_rows) seen[key[p] - first] = 1;
+        if (rows[p] < a.rows && rows[p] >= first && rows[p] - first < a.fill_rows) seen[rows[p] - first] = 1;
       __syncthreads();
       for (uint32_t r = wave; r < a.fill_rows && first + r < a.rows; r += kSumWaves)
         if (!seen[r]) zero_row(a, out, uint32_t(first) + r, lane);
@@ -419,11 +431,11 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
     }
     return;
   }
-  const uint32_t mine = blockIdx.x / a.slabs, row = t.key(mine);
+  const uint32_t mine = blockIdx.x / a.slabs, row = t.row(mine);
   if (row >= a.rows) return;
 #pragma unroll
   for (uint32_t p = 0; p < kFewEach; ++p) {
-    const uint64_t same = __ballot(key[p] == row);
+    const uint64_t same = __ballot(rows[p] == row);
     if (lane == 0) masks[p * kSumWaves + wave] = same;
   }
   __syncthreads();
@@ -439,7 +451,7 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
   }
 #pragma unroll
   for (uint32_t p = 0; p < kFewEach; ++p)
-    if (key[p] == row) list[before[p]] = p * kSumThreads + threadIdx.x;
+    if (rows[p] == row) list[before[p]] = p * kSumThreads + threadIdx.x;
   __syncthreads();
   const uint64_t col = (uint64_t(blockIdx.x - mine * a.slabs) * kWave + lane) * kC;
   const uint32_t width = block_width<kC>(col, a.cols);
