@@ -580,15 +580,9 @@ def _matrix(x, what, device):
     return x.data_ptr(), x.numel() // cols if cols else prod(shape[:-1]) if len(shape) > 1 else 0, cols, cols, dtype, 0
 
 
-def _optional(x, what, device, of):
-    """Fields of an etc_matrix that may be absent (None) and has elements if
-    `of`, what it goes with, has: an empty tensor's pointer is that of an absent one."""
-    if x is None:
-        return _NO_MATRIX
-    m = _matrix(x, what, device)
-    if not m[0] and of:
-        raise ValueError(f"{what} has no elements")
-    return m
+def _no_elements(what):
+    """An empty tensor's pointer is that of an absent matrix, which the library leaves out."""
+    raise ValueError(f"{what} has no elements")
 
 
 def _ids(x, what, device):
@@ -641,7 +635,15 @@ def etc_dropout(x, out, dropout=None, bias=None, residual=None, stream=None):
     """out = residual + drop(x + bias); out may be x or residual itself."""
     d = _device_of(out, "out")
     m = _matrix(x, "x", d)
-    b, r = _optional(bias, "bias", d, m[2]), _optional(residual, "residual", d, m[1] and m[2])
+    b = r = _NO_MATRIX
+    if bias is not None:
+        b = _matrix(bias, "bias", d)
+        if not b[0] and m[2]:
+            _no_elements("bias")
+    if residual is not None:
+        r = _matrix(residual, "residual", d)
+        if not r[0] and m[0]:
+            _no_elements("residual")
     _check(_lib.etc_dropout(_DROPOUT.pack(*m, *b, *r, *_matrix(out, "out", d), *_drop(dropout)),
                             _stream_on(stream, d)), "etc_dropout")
 
@@ -657,7 +659,11 @@ def etc_dropout_grad(grad, dx, dropout=None, dbias=None, workspace=None, accumul
     """dx = drop'(grad) (dx may be grad itself); dbias (float32) = or += its sum over rows."""
     d = _device_of(dx, "dx")
     m = _matrix(grad, "grad", d)
-    b = _optional(dbias, "dbias", d, m[2])
+    b = _NO_MATRIX
+    if dbias is not None:
+        b = _matrix(dbias, "dbias", d)
+        if not b[0] and m[2]:
+            _no_elements("dbias")
     _check(_lib.etc_dropout_grad(_DROPOUT_GRAD.pack(*m, *_matrix(dx, "dx", d), *b,
                                                     *_drop(dropout), *_workspace(workspace, d), bool(accumulate), 0),
                                  _stream_on(stream, d)), "etc_dropout_grad")
