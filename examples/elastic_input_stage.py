@@ -7,8 +7,8 @@ it, trained towards random targets.  The tables and the bias live in the four
 state arenas of their tensor-parallel ranks, where etc_plan lays them out; all
 ranks of a configuration run on one GPU here, one after another.
 
-  step       etc_embed on every rank's share of the vocabulary, the shares'
-             sum with positions and dropout (etc_embed again), the epilogue
+  step       etc_embed on every rank's share of the vocabulary, the shares' sum
+             with scale, positions and dropout (etc_embed again), the epilogue
              (etc_dropout), the way back (etc_dropout_grad, etc_embed_grad) and
              the optimizer (etc_adam) over every rank's arenas
   reshard    etc_pack on the old ranks, etc_unpack on the new ones
@@ -99,11 +99,12 @@ def step(ranks, number, tokens, target):
     summed = torch.zeros(n, h, dtype=torch.bfloat16, device=DEV)
     for rank in ranks:
         share = act()
-        etc.etc_embed(tokens, rank.param("embed"), share, row0=rank.pieces["embed"]["r0"], scale=SCALE)
+        etc.etc_embed(tokens, rank.param("embed"), share, row0=rank.pieces["embed"]["r0"])
         summed += share
     x, y = act(), act()
-    # replicated on all ranks: positions and dropout, with the summed rows in the table's place
-    etc.etc_embed(rows, summed, x, positions=positions, pos_table=ranks[0].param("pos_embed"), dropout=first)
+    # replicated on all ranks: scale, positions and dropout, with the summed rows in the table's place
+    etc.etc_embed(rows, summed, x, scale=SCALE, positions=positions, pos_table=ranks[0].param("pos_embed"),
+                  dropout=first)
     bias = ranks[0].param("layers.0.proj.bias").view(-1)
     etc.etc_dropout(x, y, second, bias=bias, residual=x)
     error = y.float() - target

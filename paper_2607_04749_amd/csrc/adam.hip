@@ -9,7 +9,10 @@
 // large launches of one-wavefront workgroups reserve LDS (never touched) so that
 // ten share a CU.  181 M elements, MI355X, in us: workgroups of 256 lanes 1001,
 // with non-temporal accesses 949; one wavefront with 25 a CU 906, 19 881, 16 869,
-// 12 842, 10 822 (6.6 TB/s), 8 833.
+// 12 842, 10 822 (6.6 TB/s), 8 833.  Ten a CU from 2.6 M elements on; graph replays, in us:
+//   M elements    0.3   0.9   1.5   2.6   4.0   8.0    16    32    64   181
+//   all slots     3.0   5.6   8.9  14.8  22.8  42.0  82.5   162   325   923
+//   ten a CU      3.0   6.2   9.1  14.6  22.1  39.9  75.5   147   293   834
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

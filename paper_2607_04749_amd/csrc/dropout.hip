@@ -4,9 +4,10 @@
 //   out = residual + drop(x + bias);  dx = drop'(grad);  dbias (+)= column sums of drop'(grad)
 //
 // HBM bound: the mask is worked out from its place, so nothing but x, residual
-// and out (grad and dx) is moved.  16384 x 2048 bf16, MI355X: the epilogue 31.5 us
-// (201 MB, 6.4 TB/s), its backward 24.0 us with the bias's gradient (main launch 21 at
-// 6.4 TB/s, join of the partial sums 3 to 4) and 22 without.  1021 x 681 fp32: 5.4 us.
+// and out (grad and dx) is moved.  16384 x 2048 bf16, MI355X, a pass among others: the
+// epilogue 31.7 us (201 MB, 6.4 TB/s), its backward 24.0 us with the bias's gradient (5.6 TB/s;
+// its launches by themselves, medians of a trace, 21.2 and 4.6) and 21.8 without (6.2 TB/s).
+// 1021 x 681 fp32, in graph replays: 5.4 to 5.5 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

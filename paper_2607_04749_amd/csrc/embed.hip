@@ -6,12 +6,13 @@
 // HBM bound: it reads the rows that occur and writes one row per token.  A
 // lane moves one or two blocks of columns; consecutive lanes and wavefronts follow
 // the output, so that it is written as one front, without staying in the caches
-// that hold the rows and positions which tokens share.  bf16, MI355X:
-//   8192 x 8192 of 4000 rows               20.9 us, 138 MB at the least (6.6 TB/s)
-//   16384 x 2048 of 50304 rows with 2048   21 us: 49 MB read and 67 MB written in
+// that hold the rows and positions which tokens share.  bf16, MI355X, medians of a trace:
+//   8192 x 8192, 227 tokens inside the     21.3 us, 138 MB at the least (6.5 TB/s); 23.2 in graph
+//     4000 rows                            replays with the 4000 most frequent ids, most of them inside
+//   16384 x 2048 of 50304 rows with 2048   21.4 us: 49 MB read and 67 MB written in
 //     positions and dropout                HBM, 201 MB through L2, and about 16 us
 //                                          of vector instructions for the mask
-//   1 x 4096                               1.9 us: one wait for the id, one for the row
+//   1 x 4096                               1.8 us: one wait for the id, one for the row
 #include <hip/hip_runtime.h>
 
 #include "ops.hpp"

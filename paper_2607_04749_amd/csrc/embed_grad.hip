@@ -16,12 +16,13 @@
 // whichever rows the table holds: a share's gradient has the bits of the whole's.
 //
 // The sums are HBM bound (a row of grad per token and of dtable per row, and the
-// parts); the other launches are a few waits long.  bf16 gradients, MI355X, in us:
+// parts); the other launches are a few waits long.  bf16 gradients, MI355X, in us,
+// medians of a trace:
 //                                            order       sums                    join
-//   16384 x 2048 into 50304 rows, added,     4.6 + 4.5   33, 169 MB, 5.1 TB/s    7.1
+//   16384 x 2048 into 50304 rows, added,     4.8 + 4.7   32, 169 MB, 5.2 TB/s    7.1
 //     dropout
-//   8192 x 4096 into 8000 rows, written      4.8 + 4.0   37, 191 MB, 5.1 TB/s    5.3
-//   128 x 256 into 1024 rows, written        4.3 in all (few)
+//   8192 x 4096 into 8000 rows, written      4.8 + 4.6   37, 191 MB, 5.2 TB/s    5.5
+//   128 x 256 into 1024 rows, written        4.2 in all (few)
 // (an addition of three tensors of this size by one elementwise kernel reaches 5.6 TB/s).
 // What was slower: a radix sort (32 us), atomics-free counts of all pairs (1.8 ms),
 // runs that end in the next chunk summed by the wavefront they begin in, which saves
@@ -501,6 +502,8 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(Tokens t, SumArgs a, M
 //      256    256: 5.1 / 10.2   512: 7.4 / 10.5    256: 21 / 11.6   512: 39 / 14.6
 //     2048    256: 4.9 / 10.2   512: 6.5 / 10.6    256: 21 / 12.1   512: 39 / 15.1
 //     8192    128: 6.9 / 10.2   512: 22 / 13.4     128: 11.8 / 10.5
+// (half of 512 ids alike: 21 to 22).  The choice is made on the host, which does not
+// see the ids, so a batch that is padded with an id of the table pays for it.
 constexpr uint64_t kFewJobs = 2048;
 
 // Slabs of a row: a wavefront's 64 blocks of `block` columns.
