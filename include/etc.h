@@ -601,6 +601,153 @@ typedef struct {
 } etc_adam_args;
 ETC_API int etc_adam(const etc_adam_args* args, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators around a block's projections
+ *
+ * The norm in front of a projection, with the residual's addition; activations
+ * in 8 bits, kept for the backward pass or taken by a product of 8-bit
+ * integers; and the rotary positions behind it.  What is said of the operators
+ * above holds here too: contiguous rows, sums in 32 bits in an order that the
+ * arguments' sizes decide, no atomics, a call without work returns ETC_OK, the same errors.
+ * A row's norm, its 8 bits, its product and its rotation have the same
+ * bits whatever other rows the call has. */
+
+/* 8-bit data: of an etc_matrix8 only */
+enum { ETC_DTYPE_I8 = 2, ETC_DTYPE_E4M3 = 3 };
+
+/* rows x cols numbers of 8 bits with scales, in device memory.  Element (i, j)
+ * stands for
+ *   scale[i * scale_ld + j / group] * data[i * ld + j],
+ * with group 32, 64, 128 or 256 columns, or 0: one scale for the whole row.
+ * Data are int8, or e4m3 floating point numbers (1 sign, 4 exponent and 3
+ * mantissa bits, no infinities, largest 448).
+ * What the calls below write: with a the largest magnitude of the scale's
+ * elements, at least 2^-100, and t = 127 or 448,
+ *   scale = a / t,  data = x * (t / a), to nearest, ties to even,
+ * in 32 bits.  Where x holds an infinity or NaN the scale is NaN and the data
+ * are 0, so that all its elements read as NaN.  ld >= cols and scale_ld >= the
+ * number of scales in a row for what is written; what is read may repeat rows. */
+typedef struct {
+  void* data;
+  float* scale;
+  int64_t rows, cols, ld, scale_ld;
+  int32_t dtype;           /* ETC_DTYPE_I8 or ETC_DTYPE_E4M3 */
+  int32_t group;
+} etc_matrix8;
+
+/* Root-mean-square norm with the residual's addition:
+ *   s = x + residual,  r[i] = 1 / sqrt(mean over j of s[i, j]^2 + eps),
+ *   y = s * r[i] * weight[j];
+ * sum = s, out = y, out8 = y in 8 bits (group 0), rstd[i] = r[i], each where
+ * given; out or out8 (or both) has to be.  x, residual, weight (one row), sum
+ * and out are of one type; y is worked out from s before its rounding.  sum and
+ * out may be x or residual itself (same data and ld), not both the same one.
+ * Squares have to fit 32 bits: a row whose sum of them is infinite has r = 0.
+ * Matrices of no columns have nothing written. */
+typedef struct {
+  etc_matrix x, residual, weight, sum, out;
+  etc_matrix8 out8;        /* data NULL: absent */
+  float* rstd;             /* rows numbers, or NULL */
+  double eps;              /* > 0 */
+} etc_norm_args;
+ETC_API int etc_norm(const etc_norm_args* args, void* stream);
+
+/* Its backward.  With x the norm's input (etc_norm's sum, or x without a
+ * residual), r its rstd, n = x * r[i], dn = grad * weight:
+ *   dx = dsum + r[i] * (dn - n * mean over j of dn n)
+ *   dweight = (accumulate ? dweight : 0) + the sum over rows of grad * n, unrounded.
+ * dx is the gradient of x and of residual alike; dsum (may be absent) is the one
+ * that reaches the sum past the norm.  x is given as a matrix of grad's type,
+ * or, with x.data NULL, as x8: as etc_store8 kept it.  grad, weight, dsum and dx are
+ * of one type; dweight (ETC_DTYPE_F32, one row) may be absent.  dx may be grad,
+ * x or dsum itself.  workspace: etc_norm_grad_workspace's bytes; only read or
+ * written with dweight, and may be NULL without. */
+typedef struct {
+  etc_matrix grad, x;
+  etc_matrix8 x8;
+  etc_matrix weight, dsum, dx, dweight;
+  const float* rstd;
+  void* workspace;         /* device, 256-byte aligned */
+  uint64_t workspace_bytes;
+  int32_t accumulate;
+  int32_t reserved;        /* 0 */
+} etc_norm_grad_args;
+ETC_API int etc_norm_grad(const etc_norm_grad_args* args, void* stream);
+ETC_API int etc_norm_grad_workspace(int64_t rows, int64_t cols, uint64_t* bytes);
+
+/* out = x in 8 bits, x's columns multiplied with col_scale first (cols numbers,
+ * or NULL for 1): an activation kept for the backward pass, or a product's
+ * operand.  The gradient of etc_matmul8's x is such a product: grad with the
+ * weight's scales as col_scale, times the weight's data transposed. */
+typedef struct {
+  etc_matrix x;
+  const float* col_scale;
+  etc_matrix8 out;
+} etc_store8_args;
+ETC_API int etc_store8(const etc_store8_args* args, void* stream);
+
+/* out = the numbers that x stands for, of either type. */
+typedef struct {
+  etc_matrix8 x;
+  etc_matrix out;
+} etc_load8_args;
+ETC_API int etc_load8(const etc_load8_args* args, void* stream);
+
+/* out[m, n] = x.scale[m] * w.scale[n] * (sum over k of x.data[m, k] *
+ * w.data[n, k]) + bias[n], x and w ETC_DTYPE_I8 with group 0; a scale that is
+ * NULL counts as 1.  The sum is exact (32-bit integers; more than 131071
+ * columns of x are UNSUPPORTED), the rest in 32 bits.  out is of either type,
+ * bias (one row of out's type) may be absent. */
+typedef struct {
+  etc_matrix8 x, w;
+  etc_matrix bias, out;
+} etc_matmul8_args;
+ETC_API int etc_matmul8(const etc_matmul8_args* args, void* stream);
+
+enum { ETC_ROTARY_HALF = 0, ETC_ROTARY_INTERLEAVED = 1 };  /* pairs (j, j + pairs), or (2j, 2j + 1) */
+enum { ETC_ROTARY_PAIRS = 128 };
+
+/* How heads turn: pair j of a head by position * freq[j] radians, the first 2 *
+ * pairs of its columns; sine and cosine are multiplied with scale.  Host memory,
+ * read during a call.  etc_rotary_init fills it; any other frequencies may be
+ * written into it. */
+typedef struct {
+  double freq[ETC_ROTARY_PAIRS];
+  double scale;
+  int32_t pairs;           /* 1 .. ETC_ROTARY_PAIRS */
+  int32_t layout;          /* ETC_ROTARY_HALF or ETC_ROTARY_INTERLEAVED */
+} etc_rotary_desc;
+
+/* freq[j] = base^(-2j / dim) for j < dim / 2, scale = 1, stretched for contexts
+ * `factor` times as long as the one of training:
+ *   NONE    not at all (factor is not read)
+ *   LINEAR  freq[j] / factor
+ *   BASE    base * factor^(dim / (dim - 2)) in place of base: the fastest pair
+ *           keeps its frequency, the slowest one's is divided by factor
+ *   PARTS   a pair that turns k = length freq[j] / 2 pi times in the context of
+ *           training: kept from k = high on, divided by factor up to k = low, and
+ *           between them freq[j] * (u + (1 - u) / factor), u = (k - low) / (high - low).
+ * dim is even, 2 .. 2 ETC_ROTARY_PAIRS (BASE: from 4 on); base, factor, length > 0, high > low. */
+enum { ETC_ROTARY_NONE = 0, ETC_ROTARY_LINEAR = 1, ETC_ROTARY_BASE = 2, ETC_ROTARY_PARTS = 3 };
+ETC_API int etc_rotary_init(etc_rotary_desc* out, int32_t dim, int32_t layout, double base, int32_t scaling,
+                            double factor, double length, double low, double high);
+
+/* Turns heads by their positions: out = x with, in each head (head_dim columns
+ * of a row, cols / head_dim heads) and pair (a, b),
+ *   a' = scale (a cos - b sin),  b' = scale (b cos + a sin),
+ * or, with `backward`, the gradient: sin negated.  Columns past the pairs are
+ * copied.  Row i turns by positions[i], any whole number; angles are worked out
+ * in 64 bits.  x and out are of one type and out may be x itself, so that the query and key
+ * heads of a projection's output are turned where they are. */
+typedef struct {
+  etc_matrix x, out;
+  etc_ids positions;
+  const etc_rotary_desc* rotary;
+  int32_t head_dim;
+  int32_t backward;
+} etc_rotary_args;
+ETC_API int etc_rotary(const etc_rotary_args* args, void* stream);
+
 /* Text of the calling thread's last error ("" if none).  Valid until the
  * thread's next failing call. */
 ETC_API const char* etc_last_error(void);

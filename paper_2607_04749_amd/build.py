@@ -16,7 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libetc.so")
 BUILD_DIR = os.path.join(ROOT, "_build", "etc")
 SOURCES = ("plan.hip", "tiles.hip", "sketch.hip", "defrag.hip", "copy.hip", "cost.hip", "capi.hip",
-           "embed.hip", "embed_grad.hip", "dropout.hip", "adam.hip", "ops.hip")
+           "embed.hip", "embed_grad.hip", "dropout.hip", "adam.hip", "ops.hip",
+           "norm.hip", "norm_grad.hip", "eight.hip", "matmul8.hip", "rotary.hip", "block.hip")
 
 # Packed fp32 ops are disabled for all device code (-packed-fp32-ops); the
 # host pass only warns that it does not know the feature.

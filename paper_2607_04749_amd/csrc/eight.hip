@@ -1,0 +1,235 @@
+// eight.hip -- activations into 8 bits with scales and back (etc_store8,
+// etc_load8).
+//
+//   scale = a / t, data = x col_scale (t / a) to nearest;  out = scale data
+//
+// HBM bound: x is read and the data written once, and the other way round.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "eight.hpp"
+
+namespace etc {
+
+namespace {
+
+constexpr uint32_t kFlatThreads = 64;
+constexpr uint32_t kMostWaves = 16;
+constexpr uint32_t kMostBlocks = 4;
+
+template <typename T, uint32_t kC, bool kWhole>
+__device__ __forceinline__ void load_columns(const Raw<T, kC, kWhole>& raw, const Raw<float, kC, kWhole>& factors, bool scaled,
+                                             uint32_t width, float (&v)[kC]) {
+  raw.widen(v, width);
+  if (!scaled) return;
+  float f[kC];
+  factors.widen(f, width);
+#pragma unroll
+  for (uint32_t e = 0; e < kC; ++e) v[e] *= f[e];
+}
+
+template <uint32_t kC>
+__device__ __forceinline__ uint32_t block_top(const float (&v)[kC]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (uint32_t e = 0; e < kC; ++e) top = max(top, magnitude(v[e]));
+  return top;
+}
+
+// Scales of groups: a lane has a block, a group's lanes are neighbours in one
+// wavefront (rows are counted in whole groups of lanes).
+template <typename T, bool kWhole, Kind8 k8>
+__global__ __launch_bounds__(kFlatThreads) void store8_group_kernel(BlockGrid grid, uint32_t lanes, Mat<const T> x,
+                                                                    const float* col_scale, Mat8 out) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
+  uint32_t i = 0, block = 0;
+  if (at < grid.n) grid.place(at, &i, &block);
+  const uint64_t col = uint64_t(block) * kC;
+  const uint32_t width = at < grid.n ? block_width<kC>(col, grid.cols) : 0;
+  Raw<T, kC, kWhole> raw;
+  Raw<float, kC, kWhole> factors;
+  raw.zero();
+  factors.zero();
+  if (width) {
+    raw.template load<true>(x.p + int64_t(i) * x.ld + col, width, grid.cols < kC);
+    if (col_scale) factors.load(col_scale + col, width, grid.cols < kC);
+  }
+  float v[kC];
+  load_columns(raw, factors, col_scale != nullptr, width, v);
+  const uint32_t top = lanes_max(block_top(v), lanes);
+  if (!width) return;
+  float scale, factor;
+  scale_of<k8>(top, &scale, &factor);
+  Raw8<kC, kWhole> q;
+  q.template narrow<k8>(v, factor);
+  q.template store<true>(out.p + int64_t(i) * out.ld + col, width);
+  if (threadIdx.x % lanes == 0) out.scale[int64_t(i) * out.sld + (col >> out.shift)] = scale;
+}
+
+__device__ __forceinline__ uint32_t row_top(uint32_t top) {
+  __shared__ uint32_t tops[kMostWaves];
+  top = lanes_max(top, 64);
+  const uint32_t waves = blockDim.x / 64;
+  if (waves == 1) return top;
+  if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+  __syncthreads();
+  for (uint32_t w = 0; w < waves; ++w) top = max(top, tops[w]);
+  return top;
+}
+
+// One scale a row: a workgroup has a row, a lane kB blocks of it.
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8>
+__global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t cols, Mat<const T> x, const float* col_scale,
+                                                                     Mat8 out) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const int64_t i = blockIdx.x;
+  Raw<T, kC, kWhole> raw[kB];
+  Raw<float, kC, kWhole> factors[kB];
+#pragma unroll
+  for (uint32_t b = 0; b < kB; ++b) {
+    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
+    const uint32_t width = block_width<kC>(col, cols);
+    raw[b].zero();
+    factors[b].zero();
+    if (!width) continue;
+    raw[b].template load<true>(x.p + i * x.ld + col, width, cols < kC);
+    if (col_scale) factors[b].load(col_scale + col, width, cols < kC);
+  }
+  compiler_fence();
+  float v[kB][kC];
+  uint32_t top = 0;
+#pragma unroll
+  for (uint32_t b = 0; b < kB; ++b) {
+    const uint32_t width = block_width<kC>(uint64_t(b * blockDim.x + threadIdx.x) * kC, cols);
+    load_columns(raw[b], factors[b], col_scale != nullptr, width, v[b]);
+    top = max(top, block_top(v[b]));
+  }
+  float scale, factor;
+  scale_of<k8>(row_top(top), &scale, &factor);
+#pragma unroll
+  for (uint32_t b = 0; b < kB; ++b) {
+    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
+    const uint32_t width = block_width<kC>(col, cols);
+    if (!width) continue;
+    Raw8<kC, kWhole> q;
+    q.template narrow<k8>(v[b], factor);
+    q.template store<true>(out.p + i * out.ld + col, width);
+  }
+  if (threadIdx.x == 0) out.scale[i * out.sld] = scale;
+}
+
+// Rows that no workgroup's registers hold: read twice, the second time from the caches.
+template <typename T, bool kWhole, Kind8 k8>
+__global__ __launch_bounds__(kMostWaves * 64) void store8_long_kernel(uint32_t cols, Mat<const T> x, const float* col_scale,
+                                                                      Mat8 out) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const int64_t i = blockIdx.x;
+  uint32_t top = 0;
+  float scale = 0.0f, factor = 0.0f;
+  for (uint32_t pass = 0; pass < 2; ++pass) {
+    for (uint64_t col = uint64_t(threadIdx.x) * kC; col < cols; col += uint64_t(blockDim.x) * kC) {
+      const uint32_t width = block_width<kC>(col, cols);
+      Raw<T, kC, kWhole> raw;
+      Raw<float, kC, kWhole> factors;
+      factors.zero();
+      raw.load(x.p + i * x.ld + col, width, false);
+      if (col_scale) factors.load(col_scale + col, width, false);
+      float v[kC];
+      load_columns(raw, factors, col_scale != nullptr, width, v);
+      if (pass == 0) {
+        top = max(top, block_top(v));
+      } else {
+        Raw8<kC, kWhole> q;
+        q.template narrow<k8>(v, factor);
+        q.store(out.p + i * out.ld + col, width);
+      }
+    }
+    if (pass == 0) scale_of<k8>(row_top(top), &scale, &factor);
+  }
+  if (threadIdx.x == 0) out.scale[i * out.sld] = scale;
+}
+
+// A lane has a block of the output's columns, which lies in one group.
+template <typename T, bool kWhole, Kind8 k8>
+__global__ __launch_bounds__(kFlatThreads) void load8_kernel(BlockGrid grid, Mat8 x, Mat<T> out) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const uint32_t at = blockIdx.x * kFlatThreads + threadIdx.x;
+  if (at >= grid.n) return;
+  uint32_t i, block;
+  grid.place(at, &i, &block);
+  const uint64_t col = uint64_t(block) * kC;
+  const uint32_t width = block_width<kC>(col, grid.cols);
+  Raw8<kC, kWhole> q;
+  q.template load<true>(x.p + int64_t(i) * x.ld + col, width, grid.cols < kC);
+  const float scale = x.scale[int64_t(i) * x.sld + (col >> x.shift)];
+  float v[kC];
+  q.template widen<k8>(v, width);
+#pragma unroll
+  for (uint32_t e = 0; e < kC; ++e) v[e] *= scale;
+  store_block<kWhole, true>(out.p + int64_t(i) * out.ld + col, width, v);
+}
+
+template <typename T, bool kWhole, Kind8 k8>
+hipError_t launch_store(const etc_store8_args& a, hipStream_t stream) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  if (a.out.group) {
+    const uint32_t lanes = uint32_t(a.out.group) / kC;
+    const int64_t groups = (a.x.cols + a.out.group - 1) / a.out.group;
+    return for_row_runs(a.x.rows, groups * a.out.group, kC, 1, [&](int64_t first, const BlockGrid& g) -> hipError_t {
+      BlockGrid grid = g;
+      grid.cols = uint32_t(a.x.cols);
+      hipLaunchKernelGGL((store8_group_kernel<T, kWhole, k8>), dim3((grid.n + kFlatThreads - 1) / kFlatThreads),
+                         dim3(kFlatThreads), 0, stream, grid, lanes, cmat<T>(a.x, first), a.col_scale, mat8(a.out, first));
+      return hipGetLastError();
+    });
+  }
+  const uint32_t blocks = blocks_per_row(a.x.cols, kC);
+  const uint32_t per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
+  const uint32_t waves = std::min((blocks + 64 * per - 1) / (64 * per), kMostWaves);
+  const auto kernel = blocks > waves * 64 * per ? store8_long_kernel<T, kWhole, k8>
+                      : per == 1                ? store8_row_kernel<T, 1, kWhole, k8>
+                      : per == 2                ? store8_row_kernel<T, 2, kWhole, k8>
+                                                : store8_row_kernel<T, kMostBlocks, kWhole, k8>;
+  return for_row_groups(a.x.rows, waves * 64, [&](int64_t first, uint32_t rows) -> hipError_t {
+    hipLaunchKernelGGL(kernel, dim3(rows), dim3(waves * 64), 0, stream, uint32_t(a.x.cols), cmat<T>(a.x, first), a.col_scale,
+                       mat8(a.out, first));
+    return hipGetLastError();
+  });
+}
+
+template <typename T, bool kWhole, Kind8 k8>
+hipError_t launch_load(const etc_load8_args& a, hipStream_t stream) {
+  return for_row_runs(a.out.rows, a.out.cols, kLaneCols<T>, 1, [&](int64_t first, const BlockGrid& grid) -> hipError_t {
+    hipLaunchKernelGGL((load8_kernel<T, kWhole, k8>), dim3((grid.n + kFlatThreads - 1) / kFlatThreads), dim3(kFlatThreads), 0,
+                       stream, grid, mat8(a.x, first), mat<T>(a.out, first));
+    return hipGetLastError();
+  });
+}
+
+template <typename T, Kind8 k8>
+hipError_t store_type(const etc_store8_args& a, hipStream_t stream) {
+  return whole_blocks(a.x.cols, kLaneCols<T>) ? launch_store<T, true, k8>(a, stream) : launch_store<T, false, k8>(a, stream);
+}
+
+template <typename T, Kind8 k8>
+hipError_t load_type(const etc_load8_args& a, hipStream_t stream) {
+  return whole_blocks(a.out.cols, kLaneCols<T>) ? launch_load<T, true, k8>(a, stream) : launch_load<T, false, k8>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_store8(const etc_store8_args& a, hipStream_t stream) {
+  if (a.x.dtype == ETC_DTYPE_F32)
+    return kind8(a.out) == kE4m3 ? store_type<float, kE4m3>(a, stream) : store_type<float, kInt8>(a, stream);
+  return kind8(a.out) == kE4m3 ? store_type<bf16, kE4m3>(a, stream) : store_type<bf16, kInt8>(a, stream);
+}
+
+hipError_t launch_load8(const etc_load8_args& a, hipStream_t stream) {
+  if (a.out.dtype == ETC_DTYPE_F32)
+    return kind8(a.x) == kE4m3 ? load_type<float, kE4m3>(a, stream) : load_type<float, kInt8>(a, stream);
+  return kind8(a.x) == kE4m3 ? load_type<bf16, kE4m3>(a, stream) : load_type<bf16, kInt8>(a, stream);
+}
+
+}  // namespace etc

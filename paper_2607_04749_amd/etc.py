@@ -39,6 +39,10 @@ DEFRAG_NONE, DEFRAG_OCCUPANCY, DEFRAG_EFFICIENCY = 0, 1, 2
 ESIZE = (2, 4, 4, 4)
 DTYPE_BF16, DTYPE_F32 = 0, 1
 IDS_I32, IDS_I64 = 0, 1
+DTYPE_I8, DTYPE_E4M3 = 2, 3
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_PAIRS = 128
 
 
 class ModelDesc(ctypes.Structure):
@@ -124,11 +128,15 @@ def _load():
     L.etc_unpack_kind.argtypes = [vp, ctypes.c_int, ctypes.c_int, vp, vp, vp]
     L.etc_plan_message.argtypes = [vp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, i32p]
     L.etc_plan_refer.argtypes = [vp, ctypes.c_int, vp, ctypes.c_int, i32p]
-    for name in ("etc_embed", "etc_embed_grad", "etc_dropout", "etc_dropout_grad", "etc_adam"):
+    for name in ("etc_embed", "etc_embed_grad", "etc_dropout", "etc_dropout_grad", "etc_adam", "etc_norm",
+                 "etc_norm_grad", "etc_store8", "etc_load8", "etc_matmul8", "etc_rotary"):
         getattr(L, name).argtypes = [ctypes.c_char_p, vp]
     i64 = ctypes.c_int64
     L.etc_embed_grad_workspace.argtypes = [i64, i64, i64, u64p]
     L.etc_dropout_grad_workspace.argtypes = [i64, i64, u64p]
+    L.etc_norm_grad_workspace.argtypes = [i64, i64, u64p]
+    i32, f64 = ctypes.c_int32, ctypes.c_double
+    L.etc_rotary_init.argtypes = [vp, i32, i32, f64, i32, f64, f64, f64, f64]
     L.etc_last_error.argtypes = []
     L.etc_last_error.restype = ctypes.c_char_p
     if len(hip_runtimes()) > 1:
@@ -710,3 +718,223 @@ def etc_adam(arenas, grad, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_de
     # pointers alone do not say that torch knows the GPU by now
     s = _stream(stream) if isinstance(grad, int) else _stream_on(stream, d)
     _check(_lib.etc_adam(_ADAM.pack(*a, g, c, first, count, lr, beta1, beta2, eps, weight_decay, step), s), "etc_adam")
+
+
+# ---------------------------------------------------------------------------
+# Operators around a block's projections
+
+_MATRIX8 = "PPqqqqii"
+_NO_MATRIX8 = (0, 0, 0, 0, 0, 0, 0, 0)
+_NORM = struct.Struct("@" + 5 * _MATRIX + _MATRIX8 + "Pd")
+_NORM_GRAD = struct.Struct("@" + 2 * _MATRIX + _MATRIX8 + 4 * _MATRIX + "PPQii")
+_STORE8 = struct.Struct("@" + _MATRIX + "P" + _MATRIX8)
+_LOAD8 = struct.Struct("@" + _MATRIX8 + _MATRIX)
+_MATMUL8 = struct.Struct("@" + 2 * _MATRIX8 + 2 * _MATRIX)
+_ROTARY = struct.Struct("@" + 2 * _MATRIX + _IDS + "Pii")
+_MATRIX8_DTYPES = {torch.int8: DTYPE_I8, torch.float8_e4m3fn: DTYPE_E4M3}
+_LAYOUTS = {"half": ROTARY_HALF, "interleaved": ROTARY_INTERLEAVED}
+_SCALINGS = {None: ROTARY_NONE, "linear": ROTARY_LINEAR, "base": ROTARY_BASE, "parts": ROTARY_PARTS}
+
+
+class Matrix8:
+    """A matrix of 8-bit numbers with scales: element (i, j) stands for
+    scale[i, j // group] * data[i, j].  data: int8 or float8_e4m3fn, two
+    dimensions with contiguous rows, or contiguous of any (its last dimension is the
+    row); scale: float32, one for each row (group 0) or for each `group` (32,
+    64, 128 or 256) columns of it, or None in a product, where it counts as 1."""
+
+    __slots__ = ("data", "scale", "group")
+
+    def __init__(self, data, scale=None, group=0):
+        self.data, self.scale, self.group = data, scale, index(group)
+        if self.group not in (0, 32, 64, 128, 256):
+            raise ValueError(f"group must be 0, 32, 64, 128 or 256, not {group}")
+
+
+def _matrix8(m, what, device):
+    """Fields of an etc_matrix8."""
+    x, s, group = m.data, m.scale, m.group
+    dtype = _MATRIX8_DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"{what} must be int8 or float8_e4m3fn, not {x.dtype}")
+    if x.get_device() != device:
+        raise ValueError(f"{what} must be a tensor on the current GPU")
+    shape = x.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        ld, step = x.stride()
+        if step != 1 and cols > 1 and rows:
+            raise ValueError(f"the rows of {what} must be contiguous")
+        if rows <= 1:
+            ld = cols
+    elif not shape or not x.is_contiguous():
+        raise ValueError(f"{what} must have two dimensions or be contiguous")
+    else:
+        cols = ld = shape[-1]
+        rows = x.numel() // cols if cols else prod(shape[:-1]) if len(shape) > 1 else 0
+    if s is None:
+        return x.data_ptr(), 0, rows, cols, ld, 0, dtype, group
+    if s.dtype != torch.float32 or s.get_device() != device:
+        raise ValueError(f"{what}: scale must be float32 on the current GPU")
+    groups = -(-cols // group) if group else 1
+    shape = s.shape
+    if len(shape) == 1 and groups == 1 and shape[0] == rows:
+        sld = s.stride()[0]
+    elif len(shape) == 2 and shape[0] == rows and shape[1] == groups:
+        sld, step = s.stride()
+        if step != 1 and groups > 1 and rows:
+            raise ValueError(f"{what}: the scales of a row must be contiguous")
+    elif s.numel() == rows * groups and s.is_contiguous():
+        sld = groups
+    else:
+        raise ValueError(f"{what}: scale must hold {groups} numbers for each of {rows} rows")
+    return x.data_ptr(), s.data_ptr(), rows, cols, ld, sld if rows > 1 else groups, dtype, group
+
+
+def _optional(x, what, device, empty):
+    """Fields of an etc_matrix that may be absent (None); one without elements is refused where the call has some."""
+    if x is None:
+        return _NO_MATRIX
+    m = _matrix(x, what, device)
+    if not m[0] and not empty:
+        _no_elements(what)
+    return m
+
+
+def _optional8(x, what, device, empty):
+    if x is None:
+        return _NO_MATRIX8
+    m = _matrix8(x, what, device)
+    if not m[0] and not empty:
+        _no_elements(what)
+    return m
+
+
+def _numbers(x, what, count, device):
+    """Pointer of `count` contiguous float32 numbers, or of none."""
+    if x is None:
+        return 0
+    if x.dtype != torch.float32 or x.get_device() != device or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 tensor on the current GPU")
+    if x.numel() != count:
+        raise ValueError(f"{what} must hold {count} numbers, not {x.numel()}")
+    return x.data_ptr()
+
+
+def etc_norm(x, weight, out=None, out8=None, residual=None, sum=None, rstd=None, eps=1e-6, stream=None):
+    """s = x + residual, r = 1 / sqrt(mean of s^2 + eps), y = s * r * weight:
+    writes s to sum, y to out and, in 8 bits with one scale a row, to out8 (a
+    Matrix8), r to rstd (float32), each where given.  sum and out may be x or residual itself."""
+    d = _device_of(x, "x")
+    m = _matrix(x, "x", d)
+    empty = not m[0]
+    if out is None and out8 is None:
+        raise ValueError("out or out8 is needed")
+    _check(_lib.etc_norm(_NORM.pack(*m, *_optional(residual, "residual", d, empty), *_matrix(weight, "weight", d),
+                                    *_optional(sum, "sum", d, empty), *_optional(out, "out", d, empty),
+                                    *_optional8(out8, "out8", d, empty), _numbers(rstd, "rstd", m[1], d), eps),
+                         _stream_on(stream, d)), "etc_norm")
+
+
+def etc_norm_grad_bytes(rows, cols):
+    """Bytes of etc_norm_grad's workspace, needed with dweight."""
+    n = ctypes.c_uint64()
+    _check(_lib.etc_norm_grad_workspace(rows, cols, ctypes.byref(n)), "etc_norm_grad_workspace")
+    return n.value
+
+
+def etc_norm_grad(grad, x, weight, rstd, dx, dsum=None, dweight=None, workspace=None, accumulate=False, stream=None):
+    """The norm's backward: dx = dsum + r (dn - n mean(dn n)) with n = x r, dn =
+    grad * weight; dweight (float32) = or += the sum over rows of grad * n.  x:
+    the norm's input (its sum, with a residual), or the Matrix8 that it was kept
+    in; rstd: etc_norm's; dx may be grad, x or dsum itself."""
+    d = _device_of(dx, "dx")
+    g = _matrix(grad, "grad", d)
+    empty = not g[0]
+    kept = isinstance(x, Matrix8)
+    x16, x8 = (_NO_MATRIX, _matrix8(x, "x", d)) if kept else (_matrix(x, "x", d), _NO_MATRIX8)
+    if kept and not x8[0] and not empty:
+        _no_elements("x")
+    w = _NO_MATRIX
+    if dweight is not None:
+        w = _matrix(dweight, "dweight", d)
+        if not w[0] and g[2]:
+            _no_elements("dweight")
+    _check(_lib.etc_norm_grad(_NORM_GRAD.pack(*g, *x16, *x8, *_matrix(weight, "weight", d),
+                                              *_optional(dsum, "dsum", d, empty), *_matrix(dx, "dx", d), *w,
+                                              _numbers(rstd, "rstd", g[1], d), *_workspace(workspace, d),
+                                              bool(accumulate), 0), _stream_on(stream, d)), "etc_norm_grad")
+
+
+def etc_store8(x, out, col_scale=None, stream=None):
+    """out (a Matrix8) = x in 8 bits with scales, its columns multiplied with col_scale (float32) first."""
+    d = _device_of(x, "x")
+    m = _matrix(x, "x", d)
+    _check(_lib.etc_store8(_STORE8.pack(*m, _numbers(col_scale, "col_scale", m[2], d), *_matrix8(out, "out", d)),
+                           _stream_on(stream, d)), "etc_store8")
+
+
+def etc_load8(x, out, stream=None):
+    """out = the numbers that x (a Matrix8) stands for."""
+    d = _device_of(out, "out")
+    _check(_lib.etc_load8(_LOAD8.pack(*_matrix8(x, "x", d), *_matrix(out, "out", d)), _stream_on(stream, d)), "etc_load8")
+
+
+def etc_matmul8(x, w, out, bias=None, stream=None):
+    """out[m, n] = x.scale[m] * w.scale[n] * sum over k of x.data[m, k] *
+    w.data[n, k], + bias[n]; x and w: Matrix8 of int8 with one scale a row, or none."""
+    d = _device_of(out, "out")
+    o = _matrix(out, "out", d)
+    b = _NO_MATRIX
+    if bias is not None:
+        b = _matrix(bias, "bias", d)
+        if not b[0] and o[2]:
+            _no_elements("bias")
+    _check(_lib.etc_matmul8(_MATMUL8.pack(*_matrix8(x, "x", d), *_matrix8(w, "w", d), *b, *o), _stream_on(stream, d)),
+           "etc_matmul8")
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_double * ROTARY_PAIRS), ("scale", ctypes.c_double), ("pairs", ctypes.c_int32),
+                ("layout", ctypes.c_int32)]
+
+
+class Rotary:
+    """How heads turn by their positions: `dim` columns of each head, in pairs
+    (j, j + dim / 2) ("half") or (2 j, 2 j + 1) ("interleaved"), pair j by position *
+    base^(-2 j / dim).  scaling, for contexts `factor` times as long as that of
+    training: "linear" (frequencies / factor), "base" (a larger base) or "parts"
+    (pairs that turn `high` times or more in a context of `length` keep their
+    frequency, those of `low` times or fewer have it divided by factor, and
+    between them it is blended).  scale multiplies sine and cosine.  freq: own
+    frequencies, dim / 2 of them, in radians a position.  One object serves any number of calls."""
+
+    def __init__(self, dim, base=10000.0, layout="half", scaling=None, factor=1.0, length=0.0, low=1.0, high=32.0,
+                 scale=1.0, freq=None):
+        if layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}, not {layout!r}")
+        if scaling not in _SCALINGS:
+            raise ValueError(f"scaling must be None, 'linear', 'base' or 'parts', not {scaling!r}")
+        self._desc = RotaryDesc()
+        _check(_lib.etc_rotary_init(ctypes.byref(self._desc), index(dim), _LAYOUTS[layout], base, _SCALINGS[scaling],
+                                    factor, length, low, high), "etc_rotary_init")
+        if freq is not None:
+            if len(freq) != self._desc.pairs:
+                raise ValueError(f"freq needs {self._desc.pairs} numbers, got {len(freq)}")
+            for j, f in enumerate(freq):
+                self._desc.freq[j] = f
+        self._desc.scale = scale
+        self._at = ctypes.addressof(self._desc)
+
+    @property
+    def freq(self):
+        """Radians a position of each pair."""
+        return list(self._desc.freq[:self._desc.pairs])
+
+
+def etc_rotary(x, out, positions, rotary, head_dim, backward=False, stream=None):
+    """out = x, [tokens, heads * head_dim], with each head turned by its token's
+    position (a Rotary), or turned back for the gradient; out may be x itself."""
+    d = _device_of(out, "out")
+    _check(_lib.etc_rotary(_ROTARY.pack(*_matrix(x, "x", d), *_matrix(out, "out", d), *_ids(positions, "positions", d),
+                                        rotary._at, head_dim, bool(backward)), _stream_on(stream, d)), "etc_rotary")

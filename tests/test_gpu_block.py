@@ -1,0 +1,547 @@
+"""The operators around a block's projections on the GPU, through the C ABI,
+against plain implementations in 64 bits (block_ref.py): the norm, its 8 bits and
+its backward, 8-bit activations, products of 8-bit integers, rotary positions.
+Sizes from nothing over one to odd ones and long rows, strides and shifts of one
+element, infinities and NaN, rows of zeros, in-place calls, offsets past 32 bits."""
+import numpy as np
+import pytest
+import torch
+
+import block_ref
+from gpu_util import DEV, say
+from paper_2607_04749_amd import etc
+from test_gpu_ops import CANARY, DT, blank, close, rand, untouched, workspace
+
+pytestmark = pytest.mark.gpu
+
+DT8 = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+MARK = 0x5A  # in the bytes between the rows of 8-bit data
+
+
+@pytest.fixture(autouse=True)
+def _free_memory():
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def blank8(rows, cols, eight, group=0, more=0, shift=0):
+    """(Matrix8 of marked memory, its bytes, their buffer, the scales and their buffer)."""
+    full = torch.full((shift + rows * (cols + more) + 32,), MARK, dtype=torch.uint8, device=DEV)
+    view = full[shift:shift + rows * (cols + more)].view(rows, cols + more)[:, :cols]
+    n = block_ref.groups(cols, group)
+    fs = torch.full((rows * (n + more) + 8,), CANARY, device=DEV)
+    scale = fs[:rows * (n + more)].view(rows, n + more)[:, :n]
+    return etc.Matrix8(view.view(DT8[eight]), scale, group), view, full, scale, fs
+
+
+def marked(full, view):
+    outside = torch.ones_like(full, dtype=torch.bool)
+    torch.as_strided(outside, view.shape, view.stride(), view.storage_offset()).fill_(False)
+    return bool((full[outside] == MARK).all())
+
+
+def kept8(data, scale, eight, group, more=0, shift=0):
+    """A Matrix8 on the GPU of bytes and scales in numpy."""
+    m, view, _, s, _ = blank8(*data.shape, eight, group, more, shift)
+    view.copy_(torch.from_numpy(data).to(DEV))
+    s.copy_(torch.from_numpy(scale).to(DEV))
+    return m
+
+
+WIDTHS = (1, 2, 3, 7, 8, 9, 15, 16, 31, 40, 63, 64, 65, 127, 256, 504, 511, 512, 513, 681, 1023, 1024, 1025, 2048, 2688, 4096, 4097, 8192)
+NORM = [
+    # rows, cols, dtype, residual, sum, out, eight, more, shift
+    (0, 64, "bf16", True, True, True, "i8", 0, 0),
+    (5, 0, "bf16", True, True, True, None, 0, 0),
+    (1, 4096, "bf16", True, True, True, None, 0, 0),
+    (1, 8192, "bf16", True, True, False, "i8", 0, 0),
+    (67, 681, "bf16", True, True, True, "e4m3", 3, 1),
+    (33, 597, "f32", True, False, True, "i8", 1, 3),
+    (40, 5120, "bf16", False, True, False, "e4m3", 8, 0),
+    (3, 32768, "bf16", True, True, True, "i8", 0, 0),
+    (2, 16384, "f32", True, True, True, "e4m3", 0, 0),
+    (3, 32769, "bf16", True, True, True, "i8", 1, 1),
+    (3, 16385, "f32", False, True, True, "e4m3", 1, 1),
+    (2, 100003, "bf16", True, True, True, "e4m3", 0, 1),
+    (2, 131072, "f32", True, True, True, "i8", 0, 0),
+    (1, 262144, "bf16", False, False, True, None, 0, 0),
+    (4000, 256, "bf16", True, True, False, "i8", 0, 0),
+] + [(3, cols, dtype, residual, residual, not eight or cols % 2 == 0, eight, 1, 1)
+     for cols in WIDTHS for dtype in ("bf16", "f32") for residual, eight in ((True, None), (False, "i8"), (True, "e4m3"))]
+
+
+@pytest.mark.parametrize("case", NORM, ids=lambda c: "-".join(map(str, c)))
+def test_norm(case):
+    rows, cols, dtype, with_residual, with_sum, with_out, eight, more, shift = case
+    say("norm", case)
+    rng = np.random.default_rng([rows, cols])
+    x, xn, _ = rand(rng, rows, cols, dtype, more=more, shift=shift)
+    res, rn, _ = rand(rng, rows, cols, dtype, std=3.0) if with_residual else (None, None, None)
+    w, wn, _ = rand(rng, 1, cols, dtype)
+    total, tfull = blank(rows, cols, dtype, more, shift) if with_sum else (None, None)
+    out, ofull = blank(rows, cols, dtype, more, shift) if with_out else (None, None)
+    m8, view, full8, scale, fs = blank8(rows, cols, eight, 0, more, shift) if eight else (None,) * 5
+    rstd = torch.full((rows,), CANARY, device=DEV)
+    etc.etc_norm(x, w[0], out=out, out8=m8, residual=res, sum=total, rstd=rstd, eps=1e-5)
+    torch.cuda.synchronize()
+    if rows == 0 or cols == 0:
+        assert cols or bool((rstd == CANARY).all())
+        return
+    want = block_ref.norm(xn, wn[0], rn, 1e-5)
+    close(rstd, want["rstd"], "rstd")
+    if with_sum:
+        close(total, want["sum"], "sum")
+        assert untouched(tfull, total)
+    if with_out:
+        close(out, want["out"], "out")
+        assert untouched(ofull, out)
+    if eight:
+        block_ref.check_norm8(view.cpu().numpy(), scale[:, 0].cpu().numpy().astype(np.float64), eight, want["out"])
+        assert marked(full8, view) and untouched(fs, scale)
+
+
+@pytest.mark.parametrize("dtype,cols", (("bf16", 4096), ("f32", 681), ("bf16", 40000), ("f32", 20001)))
+def test_norm_in_place(dtype, cols):
+    """sum and out may be x and residual themselves, either way round."""
+    say("norm in place", dtype, cols)
+    rng = np.random.default_rng(3)
+    x, xn, _ = rand(rng, 5, cols, dtype)
+    res, rn, _ = rand(rng, 5, cols, dtype)
+    w, wn, _ = rand(rng, 1, cols, dtype)
+    want = block_ref.norm(xn, wn[0], rn, 1e-6)
+    for total, out in (("res", "x"), ("x", "res"), ("x", None), ("res", None)):
+        a = {"x": x.clone(), "res": res.clone()}
+        free, _ = blank(5, cols, dtype)
+        o = a[out] if out else free
+        etc.etc_norm(a["x"], w, out=o, residual=a["res"], sum=a[total])
+        close(a[total], want["sum"], (total, out))
+        close(o, want["out"], (total, out))
+
+
+def test_norm_rows_are_alone():
+    """A row has the same bits in a batch of one and of many."""
+    say("norm: rows alone")
+    rng = np.random.default_rng(4)
+    for dtype, cols in (("bf16", 4096), ("bf16", 681), ("f32", 2048)):
+        x, _, _ = rand(rng, 3000, cols, dtype)
+        w, _, _ = rand(rng, 1, cols, dtype)
+        many, one = (etc.Matrix8(torch.empty(n, cols, dtype=torch.int8, device=DEV), torch.empty(n, device=DEV)) for n in (3000, 1))
+        out, single = (torch.empty(n, cols, dtype=DT[dtype], device=DEV) for n in (3000, 1))
+        etc.etc_norm(x, w, out=out, out8=many)
+        for i in (0, 1, 1500, 2999):
+            etc.etc_norm(x[i:i + 1], w, out=single, out8=one)
+            assert torch.equal(single[0], out[i]) and torch.equal(one.data[0], many.data[i])
+            assert one.scale[0] == many.scale[i]
+
+
+@pytest.mark.parametrize("cols", (40, 1000, 33000))
+def test_norm_of_what_is_not_finite(cols):
+    """A row of zeros is zeros; a row that holds NaN or an infinity reads as NaN from
+    its 8 bits, and leaves other rows alone; a sum of squares past 32 bits has r = 0."""
+    say("norm: not finite", cols)
+    x = torch.zeros(6, cols, device=DEV)
+    x[1:] = 1.0
+    x[2, cols - 1], x[3, 0], x[4, cols // 2] = float("nan"), float("inf"), 1e30
+    w = torch.ones(cols, device=DEV)
+    for eight in ("i8", "e4m3"):
+        m8, view, _, scale, _ = blank8(6, cols, eight)
+        out, rstd = torch.empty(6, cols, device=DEV), torch.empty(6, device=DEV)
+        etc.etc_norm(x, w, out=out, out8=m8, rstd=rstd)
+        back = torch.empty(6, cols, device=DEV)
+        etc.etc_load8(m8, back)
+        assert not bool(out[0].any()) and not bool(back[0].any())
+        assert bool(torch.isfinite(out[1]).all()) and torch.equal(back[1], back[5]) and bool((back[1] - 1).abs().max() < 0.01)
+        assert bool(out[2].isnan().all()) and bool(back[2:4].isnan().all()) and not bool(view[2:4].any())
+        assert bool(out[3, 0].isnan()) and float(rstd[3]) == 0.0 and not bool(out[3, 1:].any())
+        assert not bool(back[4].any()) and not bool(out[4].any()) and float(rstd[4]) == 0.0
+    # with no residual's sum to round, weights that are not finite
+    w[1] = float("inf")
+    etc.etc_norm(x[:2], w, out8=etc.Matrix8(m8.data[:2], m8.scale[:2]))
+    etc.etc_load8(etc.Matrix8(m8.data[:2], m8.scale[:2]), back[:2])
+    assert bool(back[:2].isnan().all())
+
+
+GRAD = [
+    # rows, cols, dtype, kept, group, dsum, dweight, more, shift
+    (0, 64, "bf16", None, 0, True, True, 0, 0),
+    (5, 0, "bf16", None, 0, True, True, 0, 0),
+    (1, 4096, "bf16", None, 0, True, True, 0, 0),
+    (1, 1, "f32", None, 0, False, True, 0, 0),
+    (300, 4096, "bf16", "i8", 128, True, True, 0, 0),
+    (67, 681, "bf16", "e4m3", 64, True, True, 3, 1),
+    (1021, 681, "f32", None, 0, False, True, 1, 3),
+    (5000, 256, "bf16", "i8", 0, True, True, 0, 0),
+    (4097, 40, "bf16", None, 0, True, True, 0, 0),
+    (9001, 17, "f32", "i8", 32, False, True, 1, 1),
+    (3, 32768, "bf16", "i8", 256, True, True, 0, 0),
+    (3, 16384, "f32", None, 0, True, True, 0, 0),
+    (3, 32777, "bf16", "e4m3", 256, True, True, 1, 1),
+    (300, 33000, "bf16", "i8", 0, False, True, 0, 0),
+    (3, 16385, "f32", None, 0, True, False, 1, 1),
+    (2, 131072, "bf16", None, 0, True, True, 0, 0),
+] + [(rows, cols, dtype, kept, group, dsum, dweight, 1, 1)
+     for cols in WIDTHS for rows, dtype, kept, group, dsum, dweight in
+     ((3, "bf16", None, 0, True, True), (70, "f32", "i8", 32, False, True), (5, "bf16", "e4m3", 0, True, False),
+      (130, "f32", None, 0, True, True), (130, "bf16", "i8", 256, False, True))]
+
+
+@pytest.mark.parametrize("case", GRAD, ids=lambda c: "-".join(map(str, c)))
+def test_norm_grad(case):
+    rows, cols, dtype, kept, group, with_dsum, with_dweight, more, shift = case
+    say("norm_grad", case)
+    rng = np.random.default_rng([rows, cols, 1])
+    g, gn, _ = rand(rng, rows, cols, dtype, more=more, shift=shift)
+    w, wn, _ = rand(rng, 1, cols, dtype)
+    ds, dn, _ = rand(rng, rows, cols, dtype) if with_dsum else (None, None, None)
+    if kept and rows and cols:
+        data, scale = block_ref.store8(rng.standard_normal((rows, cols)).astype(np.float32), kept, group)
+        x, xn = kept8(data, scale, kept, group, more, shift), block_ref.load8(data, scale, kept, group)
+    else:
+        x, xn, _ = rand(rng, rows, cols, dtype, more=more, shift=shift)
+    r = (1 + rng.random(rows)).astype(np.float32)
+    rstd = torch.from_numpy(r).to(DEV)
+    for accumulate in (False, True):
+        dx, full = blank(rows, cols, dtype, more, shift)
+        dw, before, wfull = rand(rng, 1, cols, "f32") if with_dweight else (None, None, None)
+        ws, end = workspace(etc.etc_norm_grad_bytes(rows, cols))
+        etc.etc_norm_grad(g, x, w, rstd, dx, dsum=ds, dweight=None if dw is None else dw[0], workspace=ws if with_dweight else None,
+                          accumulate=accumulate)
+        torch.cuda.synchronize()
+        assert untouched(full, dx) and bool((end == 0xEE).all())
+        if cols == 0:
+            continue
+        want = block_ref.norm_grad(gn, xn, wn[0], r, dn, None if dw is None else before[0], accumulate, bool(kept))
+        if rows:
+            close(dx, want["dx"], "dx")
+        if with_dweight:
+            close(dw[0], want["dweight"], "dweight")
+            assert untouched(wfull, dw)
+
+
+def test_norm_grad_in_place():
+    """dx may be grad, x or dsum itself."""
+    say("norm_grad in place")
+    rng = np.random.default_rng(5)
+    for dtype, cols in (("bf16", 4096), ("f32", 20001), ("bf16", 681)):
+        r = (1 + rng.random(7)).astype(np.float32)
+        (g, gn, _), (x, xn, _), (d, dn, _), (w, wn, _) = (rand(rng, n, cols, dtype) for n in (7, 7, 7, 1))
+        want = block_ref.norm_grad(gn, xn, wn[0], r, dn, np.zeros(cols))
+        ws, _ = workspace(etc.etc_norm_grad_bytes(7, cols))
+        for k in range(3):
+            a = [g.clone(), x.clone(), d.clone()]
+            dw = torch.empty(cols, device=DEV)
+            etc.etc_norm_grad(a[0], a[1], w, torch.from_numpy(r).to(DEV), a[k], dsum=a[2], dweight=dw, workspace=ws)
+            close(a[k], want["dx"], k)
+            close(dw, want["dweight"], k)
+
+
+def test_norm_grad_repeats_to_the_bit():
+    say("norm_grad repeated")
+    rng = np.random.default_rng(6)
+    g, _, _ = rand(rng, 3000, 1000, "bf16")
+    x, _, _ = rand(rng, 3000, 1000, "bf16")
+    w, _, _ = rand(rng, 1, 1000, "bf16")
+    r = torch.rand(3000, device=DEV)
+    ws = torch.empty(etc.etc_norm_grad_bytes(3000, 1000) + 4096, dtype=torch.uint8, device=DEV)
+    first = None
+    for _ in range(4):
+        ws.random_(0, 256)
+        dx, dw = torch.empty(3000, 1000, dtype=torch.bfloat16, device=DEV), torch.empty(1000, device=DEV)
+        etc.etc_norm_grad(g, x, w, r, dx, dweight=dw, workspace=ws)
+        first = first or (dx, dw)
+        assert torch.equal(dx, first[0]) and torch.equal(dw, first[1])
+
+
+EIGHT = [
+    # rows, cols, dtype, eight, group, scaled, more, shift
+    (0, 64, "bf16", "i8", 0, False, 0, 0), (5, 0, "bf16", "e4m3", 32, False, 0, 0),
+    (1, 8192, "bf16", "i8", 0, True, 0, 0), (300, 8192, "bf16", "e4m3", 128, False, 0, 0),
+    (2, 32769, "bf16", "i8", 0, True, 1, 1), (2, 100003, "f32", "e4m3", 0, True, 1, 1), (3, 70000, "f32", "i8", 256, True, 1, 3),
+    (2, 32768, "bf16", "i8", 0, False, 0, 0), (2, 16385, "f32", "i8", 0, False, 0, 0), (70001, 33, "bf16", "i8", 32, False, 0, 0),
+] + [(5, cols, dtype, eight, group, cols % 2 == 0, 1, 1) for cols in WIDTHS for dtype in ("bf16", "f32")
+     for eight, group in (("i8", 0), ("e4m3", 0), ("i8", 32), ("e4m3", 64), ("e4m3", 128), ("i8", 256))]
+
+
+@pytest.mark.parametrize("case", EIGHT, ids=lambda c: "-".join(map(str, c)))
+def test_store8_and_load8(case):
+    """Bit for bit: data, scales, and what they are read as, in either type."""
+    rows, cols, dtype, eight, group, scaled, more, shift = case
+    say("store8", case)
+    rng = np.random.default_rng([rows, cols, group])
+    x, xn, _ = rand(rng, rows, cols, dtype, more=more, shift=shift)
+    cs = np.exp(rng.standard_normal(cols)).astype(np.float32) if scaled else None
+    m8, view, full, scale, fs = blank8(rows, cols, eight, group, more, shift)
+    etc.etc_store8(x, m8, col_scale=None if cs is None else torch.from_numpy(cs).to(DEV))
+    torch.cuda.synchronize()
+    assert marked(full, view)
+    if not rows or not cols:
+        return
+    data, scales = block_ref.store8(xn, eight, group, cs)
+    assert untouched(fs, scale)
+    assert np.array_equal(scale.cpu().numpy(), scales)
+    got = view.cpu().numpy()
+    assert np.array_equal(got, data), np.argwhere(got != data)[:5].tolist()
+    want = torch.from_numpy(block_ref.load8(data, scales, eight, group))
+    for back in ("bf16", "f32"):
+        out, ofull = blank(rows, cols, back, more, shift)
+        etc.etc_load8(m8, out)
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu(), want.to(DT[back])) and untouched(ofull, out)
+
+
+@pytest.mark.parametrize("group", (0, 32, 128))
+def test_store8_of_what_is_not_finite(group):
+    """NaN or an infinity makes its own group NaN and no other; zeros, the smallest and the largest numbers."""
+    say("store8: not finite", group)
+    cols = 300
+    rng = np.random.default_rng(7)
+    x = rng.standard_normal((9, cols)).astype(np.float32)
+    x[0, 7], x[1, 299], x[2, 0], x[3] = np.nan, np.inf, -np.inf, 0.0
+    x[4] = 1e-45 * rng.integers(-3, 4, cols)  # subnormal
+    x[5] *= np.float32(1e38)
+    x[6, 1:] = 0.0
+    x[7] *= np.float32(1e-33)
+    x[8] = -0.0
+    x.view(np.uint32)[0, 9] = 0x7F800055  # NaN with low bits set
+    for eight in ("i8", "e4m3"):
+        m8, view, _, scale, _ = blank8(9, cols, eight, group)
+        etc.etc_store8(torch.from_numpy(x).to(DEV), m8)
+        data, scales = block_ref.store8(x, eight, group)
+        assert np.array_equal(scale.cpu().numpy(), scales, equal_nan=True)
+        got, sure = view.cpu().numpy(), np.ones(data.shape, bool)
+        assert np.array_equal(block_ref.values8(got, eight)[sure], block_ref.values8(data, eight)[sure])
+        out = torch.empty(9, cols, device=DEV)
+        etc.etc_load8(m8, out)
+        assert np.array_equal(out.cpu().numpy(), block_ref.load8(data, scales, eight, group), equal_nan=True)
+
+
+def test_load8_of_every_code():
+    """All 256 bytes of either kind, e4m3's NaN among them."""
+    say("load8: codes")
+    codes = np.arange(256, dtype=np.uint8)[None, :].repeat(3, 0)
+    scale = np.array([[1.0], [0.37], [2.0 ** -130]], np.float32)
+    for eight in ("i8", "e4m3"):
+        m8 = kept8(codes, scale, eight, 0)
+        out = torch.empty(3, 256, device=DEV)
+        etc.etc_load8(m8, out)
+        assert np.array_equal(out.cpu().numpy(), block_ref.load8(codes, scale, eight, 0), equal_nan=True)
+
+
+def test_read_rows_may_repeat():
+    """What is read may have rows at distance 0."""
+    say("repeated rows")
+    rng = np.random.default_rng(8)
+    x, xn, _ = rand(rng, 1, 200, "bf16")
+    data, scale = block_ref.store8(xn, "i8", 32)
+    m8 = kept8(data, scale, "i8", 32)
+    out = torch.empty(4, 200, device=DEV)
+    etc.etc_load8(etc.Matrix8(m8.data.expand(4, 200), m8.scale.expand(4, 7), 32), out)
+    want = block_ref.load8(data, scale, "i8", 32)
+    assert np.array_equal(out.cpu().numpy(), want.repeat(4, 0))
+    w, wn, _ = rand(rng, 1, 200, "bf16")
+    y = torch.empty(4, 200, dtype=torch.bfloat16, device=DEV)
+    etc.etc_norm(x.expand(4, 200), w, out=y, residual=x.expand(4, 200))
+    close(y, tuple(v.repeat(4, 0) for v in block_ref.norm(xn, wn[0], xn)["out"]), "norm")
+
+
+def ints(rng, rows, cols, lo=-127, hi=127):
+    return rng.integers(lo, hi + 1, (rows, cols), dtype=np.int64).astype(np.int8)
+
+
+def operand(a, scale, more=0, shift=0):
+    m, view, _, _, _ = blank8(*a.shape, "i8", 0, more, shift)
+    view.copy_(torch.from_numpy(a.view(np.uint8)).to(DEV))
+    return etc.Matrix8(m.data, None if scale is None else torch.from_numpy(scale).to(DEV))
+
+
+PRODUCT = [
+    # m, n, k, dtype, bias, scales, more (x, w, out), shift
+    (0, 16, 16, "bf16", False, True, (0, 0, 0), 0), (3, 0, 16, "bf16", False, True, (0, 0, 0), 0),
+    (3, 5, 0, "f32", True, True, (0, 0, 0), 0), (3, 5, 0, "bf16", False, False, (0, 0, 0), 0),
+    (1, 1, 1, "f32", True, True, (0, 0, 0), 0), (1, 64, 131071, "f32", False, False, (0, 0, 0), 0),
+    (67, 1280, 8192, "bf16", False, True, (0, 0, 0), 0), (300, 520, 4096, "bf16", True, True, (16, 32, 8), 16),
+    (1000, 1000, 1000, "f32", True, True, (0, 0, 0), 0), (513, 257, 2048, "bf16", False, True, (0, 0, 1), 0),
+    (2048, 4096, 512, "bf16", True, True, (0, 0, 0), 0), (4100, 2056, 272, "f32", False, True, (0, 0, 0), 0),
+] + [(m, n, k, dtype, n % 2 == 1, (m + n) % 3 > 0, more, shift)
+     for m in (1, 2, 7, 15, 16, 17, 31, 33, 64, 65, 127, 129, 200)
+     for n, k, dtype, more, shift in ((1, 64, "bf16", (0, 0, 0), 0), (15, 63, "f32", (1, 0, 1), 1), (17, 65, "bf16", (0, 3, 3), 3),
+                                      (48, 128, "bf16", (0, 0, 0), 0), (130, 1000, "f32", (0, 0, 0), 0), (64, 4096, "bf16", (0, 16, 0), 16),
+                                      (129, 4112, "bf16", (0, 0, 0), 0), (400, 17, "bf16", (7, 5, 1), 5), (1024, 256, "f32", (0, 0, 0), 0))]
+
+
+@pytest.mark.parametrize("case", PRODUCT, ids=lambda c: "-".join(map(str, c)))
+def test_matmul8(case):
+    m, n, k, dtype, with_bias, scaled, more, shift = case
+    say("matmul8", case)
+    rng = np.random.default_rng([m, n, k])
+    x, w = ints(rng, m, k), ints(rng, n, k)
+    sx, sw = (np.exp(rng.standard_normal(r)).astype(np.float32) if scaled else None for r in (m, n))
+    b, bn, _ = rand(rng, 1, n, dtype, std=100.0) if with_bias else (None, None, None)
+    out, full = blank(m, n, dtype, more[2], shift % 8)
+    etc.etc_matmul8(operand(x, sx, more[0], shift), operand(w, sw, more[1], shift), out, bias=None if b is None else b[0])
+    torch.cuda.synchronize()
+    close(out, block_ref.matmul8(x, w, sx, sw, None if b is None else bn[0]), case)
+    assert untouched(full, out)
+
+
+@pytest.mark.parametrize("m,n,k", ((5, 40, 131071), (130, 70, 131071), (300, 300, 40000)))
+def test_matmul8_largest_sums(m, n, k):
+    """All operands -128 or 127: sums at the ends of 32 bits, exactly."""
+    say("matmul8: largest sums", m, n, k)
+    x, w = np.full((m, k), -128, np.int8), np.full((n, k), -128, np.int8)
+    w[1::2] = 127
+    out = torch.empty(m, n, device=DEV)
+    etc.etc_matmul8(operand(x, None), operand(w, None), out)
+    want = np.where(np.arange(n) % 2 == 0, np.float32(k * 16384), np.float32(-k * 16256))
+    assert np.array_equal(out.cpu().numpy(), want[None, :].repeat(m, 0))
+
+
+def test_matmul8_rows_are_alone():
+    """A row has the same bits in a batch of one and of many."""
+    say("matmul8: rows alone")
+    rng = np.random.default_rng(9)
+    x, w = operand(ints(rng, 700, 2048), rng.random(700).astype(np.float32)), operand(ints(rng, 1000, 2048), rng.random(1000).astype(np.float32))
+    bias = torch.randn(1000, device=DEV).bfloat16()
+    out = torch.empty(700, 1000, dtype=torch.bfloat16, device=DEV)
+    etc.etc_matmul8(x, w, out, bias=bias)
+    for a, b in ((0, 1), (699, 700), (100, 117), (30, 130), (0, 400)):
+        part = torch.empty(b - a, 1000, dtype=torch.bfloat16, device=DEV)
+        etc.etc_matmul8(etc.Matrix8(x.data[a:b], x.scale[a:b]), w, part, bias=bias)
+        assert torch.equal(part, out[a:b])
+
+
+def test_matmul8_scales_that_are_not_finite():
+    """A row of NaN scale is NaN, whatever its data, and no other row is."""
+    say("matmul8: NaN scales")
+    rng = np.random.default_rng(10)
+    x, w = ints(rng, 40, 256), ints(rng, 50, 256)
+    x[7] = 0
+    sx, sw = np.ones(40, np.float32), np.ones(50, np.float32)
+    sx[7], sw[9] = np.nan, np.nan
+    out = torch.empty(40, 50, dtype=torch.bfloat16, device=DEV)
+    etc.etc_matmul8(operand(x, sx), operand(w, sw), out)
+    bad = out.isnan().cpu().numpy()
+    want = np.zeros((40, 50), bool)
+    want[7], want[:, 9] = True, True
+    assert np.array_equal(bad, want)
+
+
+ROTARY = [
+    # tokens, heads, head_dim, dim, layout, dtype, far, scaling, factor, more, shift
+    (0, 4, 64, 64, "half", "bf16", 10, None, 1.0, 0, 0), (1, 64, 128, 128, "half", "bf16", 4096, None, 1.0, 0, 0),
+    (300, 72, 128, 128, "half", "bf16", 131072, "parts", 8.0, 1024, 0), (1021, 9, 80, 52, "interleaved", "f32", 2048, None, 1.0, 0, 0),
+    (67, 3, 256, 256, "half", "f32", 1 << 20, "base", 32.0, 3, 1), (67, 3, 256, 256, "interleaved", "bf16", 1 << 31, "linear", 4.0, 8, 0),
+    (4000, 2, 64, 32, "half", "bf16", 5000, None, 1.0, 0, 0), (33, 1, 300, 256, "half", "bf16", 5000, None, 1.0, 0, 0),
+    (5, 1, 100000, 128, "interleaved", "f32", 5000, None, 1.0, 0, 0), (9, 5, 2, 2, "half", "bf16", 100, None, 1.0, 1, 1),
+    (9, 200, 1000, 250, "half", "bf16", 100, None, 1.0, 0, 0),
+] + [(tokens, heads, head_dim, dim, layout, dtype, 100000, None, 1.0, more, shift)
+     for tokens, heads, head_dim, dim, more, shift in
+     ((5, 7, 64, 64, 0, 0), (5, 7, 64, 64, 3, 1), (33, 1, 128, 64, 0, 0), (3, 2, 6, 4, 1, 1), (17, 40, 96, 96, 96, 0),
+      (3, 3, 80, 72, 0, 0), (200, 8, 128, 96, 1, 3), (2, 5, 33, 32, 0, 0), (70, 12, 65, 2, 0, 0), (1, 1, 3, 2, 0, 0))
+     for layout in ("half", "interleaved") for dtype in ("bf16", "f32")]
+
+
+@pytest.mark.parametrize("case", ROTARY, ids=lambda c: "-".join(map(str, c)))
+def test_rotary(case):
+    tokens, heads, head_dim, dim, layout, dtype, far, scaling, factor, more, shift = case
+    say("rotary", case)
+    rng = np.random.default_rng([tokens, heads, head_dim])
+    x, xn, _ = rand(rng, tokens, heads * head_dim, dtype, more=more, shift=shift)
+    ids = torch.int32 if far < 1 << 31 and tokens % 2 else torch.int64
+    pos = rng.integers(0, far, tokens)
+    pos[:3] = [0, 1, -5][:tokens]
+    kw = dict(scaling=scaling, factor=factor, **(dict(length=4096.0, low=1.0, high=32.0) if scaling == "parts" else {}))
+    rot = etc.Rotary(dim, layout=layout, scale=1.25, **kw)
+    freq = block_ref.frequencies(dim, **kw)
+    assert np.allclose(rot.freq, freq, rtol=1e-13, atol=0)
+    at = torch.from_numpy(pos).to(ids).to(DEV)
+    for backward in (False, True):
+        want = block_ref.rotary(xn, pos, freq, head_dim, layout, 1.25, backward)
+        out, full = blank(tokens, heads * head_dim, dtype, more, shift)
+        etc.etc_rotary(x, out, at, rot, head_dim, backward=backward)
+        torch.cuda.synchronize()
+        close(out, want, backward)
+        assert untouched(full, out)
+        same, sfull = blank(tokens, heads * head_dim, dtype, more, shift)
+        same.copy_(x)
+        etc.etc_rotary(same, same, at, rot, head_dim, backward=backward)
+        assert torch.equal(same, out) and untouched(sfull, same)
+
+
+def test_rotary_is_transposed_by_its_backward():
+    """The rotation is linear: sum(c * rotary(x)) changes with one element of x by that
+    element of the gradient, and turning back undoes turning (scale 1)."""
+    say("rotary: gradient")
+    rng = np.random.default_rng(11)
+    x, _, _ = rand(rng, 6, 40, "f32")
+    c, _, _ = rand(rng, 6, 40, "f32")
+    pos = torch.tensor([0, 3, 1000, 77, 5, 4], device=DEV)
+    for layout in ("half", "interleaved"):
+        rot = etc.Rotary(12, layout=layout)
+        dx, y, back = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        etc.etc_rotary(c.contiguous(), dx, pos, rot, 20, backward=True)
+        etc.etc_rotary(x, y, pos, rot, 20)
+        etc.etc_rotary(y, back, pos, rot, 20, backward=True)
+        assert float((back - x).abs().max()) < 1e-5
+        for i in range(6):
+            for j in range(0, 40, 3):
+                x2 = x.clone()
+                x2[i, j] += 1.0
+                y2 = torch.empty_like(x)
+                etc.etc_rotary(x2, y2, pos, rot, 20)
+                change = float(((y2 - y).double() * c.double()).sum())
+                assert abs(change - float(dx[i, j])) < 40 * 3 * 8 * 2.0 ** -23, (i, j)
+
+
+def test_rotary_own_frequencies():
+    say("rotary: own frequencies")
+    rng = np.random.default_rng(12)
+    freq = rng.random(20)
+    x, xn, _ = rand(rng, 9, 80, "f32")
+    rot, pos = etc.Rotary(40, freq=freq), np.arange(9) * 1000
+    out = torch.empty(9, 80, device=DEV)
+    etc.etc_rotary(x, out, torch.from_numpy(pos).to(DEV), rot, 40)
+    close(out, block_ref.rotary(xn, pos, freq, 40), "own")
+
+
+def test_offsets_past_32_bits():
+    """Rows 65536 elements apart, so the last ones lie past 2^32 elements."""
+    say("block: offsets past 32 bits")
+    rng = np.random.default_rng(13)
+    rows, cols, ld = 66000, 40, 65536
+    full = torch.empty((rows - 1) * ld + cols, dtype=torch.bfloat16, device=DEV)
+    far = torch.as_strided(full, (rows, cols), (ld, 1))
+    last, ln, _ = rand(rng, 8, cols, "bf16")
+    far.zero_()
+    far[-8:] = last
+    w, wn, _ = rand(rng, 1, cols, "bf16")
+    rstd = torch.empty(rows, device=DEV)
+    etc.etc_norm(far, w, out=far, rstd=rstd, eps=1e-6)
+    want = block_ref.norm(ln, wn[0])
+    close(far[-8:], want["out"], "norm")
+    far[-8:] = last
+    etc.etc_norm_grad(far, far, w, rstd, far)
+    close(far[-8:], block_ref.norm_grad(ln, ln, wn[0], rstd[-8:].cpu().numpy())["dx"], "norm_grad")
+    far[-8:] = last
+    rot, pos = etc.Rotary(40), np.arange(rows) % 100
+    etc.etc_rotary(far, far, torch.from_numpy(pos).to(DEV), rot, 40)
+    close(far[-8:], block_ref.rotary(ln, pos[-8:], np.array(rot.freq), 40), "rotary")
+    far[-8:] = last
+    data, scale = block_ref.store8(ln, "i8", 32)
+    full8 = torch.empty((rows - 1) * ld + cols, dtype=torch.int8, device=DEV)
+    far8 = etc.Matrix8(torch.as_strided(full8, (rows, cols), (ld, 1)), torch.empty(rows, 2, device=DEV), 32)
+    etc.etc_store8(far, far8)
+    assert np.array_equal(far8.data[-8:].cpu().numpy().view(np.uint8), data)
+    far.zero_()
+    etc.etc_load8(far8, far)
+    assert torch.equal(far[-8:].cpu(), torch.from_numpy(block_ref.load8(data, scale, "i8", 32)).bfloat16())
+    x = ints(rng, 8, cols)
+    far8.data[-8:] = torch.from_numpy(x).to(DEV)
+    ww = ints(rng, 30, cols)
+    out = torch.as_strided(full, (rows, 30), (ld, 1))
+    etc.etc_matmul8(etc.Matrix8(far8.data), operand(ww, None), out)
+    close(out[-8:], block_ref.matmul8(x, ww), "matmul8 x")
+    few = torch.empty(8, rows, device=DEV)
+    etc.etc_matmul8(operand(ww[:8], None), etc.Matrix8(far8.data), few)
+    close(few[:, -8:], block_ref.matmul8(ww[:8], x), "matmul8 w")
