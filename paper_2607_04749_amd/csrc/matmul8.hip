@@ -165,7 +165,8 @@ template <typename T, uint32_t kF, bool kDirect>
 __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
   constexpr uint32_t kTile = 64 * kF;
   constexpr uint32_t kLoads = kTile / 32;  // of a wavefront, of 8 rows each, for one operand
-  __shared__ __attribute__((aligned(1024))) uint8_t buffer[2][2][kTile * kDepth];
+  constexpr uint32_t kOperand = kTile * kDepth, kCopy = 2 * kOperand;
+  __shared__ __attribute__((aligned(1024))) uint8_t buffer[2 * kCopy];  // copies of x's and w's rows
   uint32_t tm, tn;
   place_tile(tiles, &tm, &tn);
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -181,23 +182,75 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
     offset[0][i] = uint32_t(min(uint64_t(row), p.m - 1 - m0)) * uint32_t(p.xld) + chunk;
     offset[1][i] = uint32_t(min(uint64_t(row), p.n - 1 - n0)) * uint32_t(p.wld) + chunk;
   }
-  const uint32_t stages = (p.k + kDepth - 1) / kDepth;
   Raw8<16, false> staged[2][kLoads];
+  // load `i` of operand o, of 128 columns from k on, into copy c or on its way there in registers
+  auto start = [&](uint64_t k, uint32_t c, uint32_t o, uint32_t i) {
+    if constexpr (kDirect)
+      __builtin_amdgcn_global_load_lds((global_void*)(base[o] + k + offset[o][i]),
+                                       (lds_void*)&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024], 16, 0, 0);
+    else staged[o][i].load(base[o] + k + offset[o][i], 16, false);
+  };
+  auto place = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t o = 0; o < 2; ++o) {
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i) {
+        const Raw8<16, false>& r = staged[o][i];
+        *reinterpret_cast<i32x4*>(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16]) =
+            i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
+      }
+    }
+  };
+  // until all wavefronts have filled their part of a copy
+  auto finish = [&](uint32_t c) {
+    if (!kDirect) place(c);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
 
-  auto start = [&](uint32_t s) {
-    const uint64_t k = uint64_t(s) * kDepth;
-    if (k + kDepth <= p.k) {
+  const uint32_t left[2] = {wave % 2 * (kTile / 2), wave / 2 * (kTile / 2)};  // the wavefront's rows of x and of w
+  uint32_t place0[2];  // of a lane's operand in the first step; in step s, s * 32 is added to its chunk's place
 #pragma unroll
-      for (uint32_t o = 0; o < 2; ++o) {
+  for (uint32_t o = 0; o < 2; ++o) place0[o] = o * kOperand + (left[o] + lane % 32) * kDepth + (lane / 32 ^ lane % 8) * 16;
+  auto read = [&](uint32_t c, uint32_t step, uint32_t o, uint32_t b) {
+    return *reinterpret_cast<const i32x4*>(&buffer[c * kCopy + (place0[o] ^ step * 32) + b * 32 * kDepth]);
+  };
+
+  i32x16 acc[kF][kF] = {};  // [of w][of x]
+  i32x4 x[2][kF], w[2][kF];
+  // Multiplies copy c, whose first operands are in x[0] and w[0].  `more`: meanwhile fills the other copy with the
+  // columns from k on, and leaves its first operands in their place.  The order is kept as it
+  // stands: reads of the next step's operands and loads of the next copy's, one by one between matrix instructions.
+  auto multiply = [&](uint32_t c, bool more, uint64_t k) {
+    constexpr uint32_t kEach = kF * kF, kReads = 2 * kF;
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) {
-          if constexpr (kDirect)
-            __builtin_amdgcn_global_load_lds((global_void*)(base[o] + k + offset[o][i]),
-                                             (lds_void*)&buffer[s % 2][o][(wave * kLoads + i) * 1024], 16, 0, 0);
-          else staged[o][i].load(base[o] + k + offset[o][i], 16, false);
+    for (uint32_t step = 0; step < 4; ++step) {
+      const uint32_t now = step % 2, next = 1 - now;
+#pragma unroll
+      for (uint32_t q = 0; q < kEach; ++q) {
+        if (more && step == 0) {
+#pragma unroll
+          for (uint32_t d = q * 2 * kLoads / kEach; d < (q + 1) * 2 * kLoads / kEach; ++d) start(k, 1 - c, d / kLoads, d % kLoads);
+        }
+        if (more && step == 3 && q == kEach / 2) finish(1 - c);
+        __builtin_amdgcn_sched_barrier(0);
+        acc[q / kF][q % kF] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[now][q / kF], x[now][q % kF], acc[q / kF][q % kF], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t r = 0; r < kReads; ++r) {
+          const uint32_t b = r / 2, o = 1 - r % 2;
+          i32x4& to = o ? w[next][b] : x[next][b];
+          if (step < 3 && r * kEach * 3 / (4 * kReads) == q) to = read(c, step + 1, o, b);
+          if (more && step == 3 && kEach / 2 + r * (kEach - kEach / 2) * 3 / (4 * kReads) == q) to = read(1 - c, 0, o, b);
         }
       }
-    } else {
+    }
+  };
+
+  // The columns past whole stages come first, so that the loop has whole ones only.
+  const uint32_t whole = p.k / kDepth, rest = p.k % kDepth;
+  if (p.k) {
+    if (rest) {
+      const uint64_t k = uint64_t(whole) * kDepth;
       const uint32_t width = block_width<16>(k + chunk, p.k);
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
@@ -208,76 +261,63 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
           staged[o][i].shift(width);
         }
       }
-    }
-  };
-  // fills what start() has left in registers, and waits until all have filled theirs
-  auto finish = [&](uint32_t s) {
-    if (!kDirect || uint64_t(s + 1) * kDepth > p.k) {
+      if (kDirect) place(0);
+    } else {
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) {
-          const Raw8<16, false>& r = staged[o][i];
-          *reinterpret_cast<i32x4*>(&buffer[s % 2][o][(wave * kLoads + i) * 1024 + lane * 16]) =
-              i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
-        }
+        for (uint32_t i = 0; i < kLoads; ++i) start(0, 0, o, i);
       }
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  };
-
-  const uint32_t left[2] = {wave % 2 * (kTile / 2), wave / 2 * (kTile / 2)};  // the wavefront's rows of x and of w
-  auto read = [&](uint32_t s, uint32_t step, uint32_t o, uint32_t b) {
-    const uint32_t at = (left[o] + b * 32 + lane % 32) * kDepth + ((step * 2 + lane / 32) ^ lane % 8) * 16;
-    return *reinterpret_cast<const i32x4*>(&buffer[s % 2][o][at]);
-  };
-
-  i32x16 acc[kF][kF] = {};  // [of w][of x]
-  if (stages) {
-    start(0);
     finish(0);
-    i32x4 x[2][kF], w[2][kF];
 #pragma unroll
     for (uint32_t b = 0; b < kF; ++b) x[0][b] = read(0, 0, 0, b), w[0][b] = read(0, 0, 1, b);
-    for (uint32_t s = 0; s < stages; ++s) {
-      const bool more = s + 1 < stages;
-      if (more) start(s + 1);
+    uint32_t c = 0;
+    for (uint32_t s = rest ? 0 : 1; s < whole; ++s) {
+      multiply(c, true, uint64_t(s) * kDepth);
+      c = 1 - c;
+    }
+    multiply(c, false, 0);
+  }
+  // Each wavefront turns 32 rows of its quarter at a time round in a part of the
+  // LDS of its own, so that it stores whole rows of 32 kF columns.
+  constexpr uint32_t kC = kLaneCols<T>, kCols = 32 * kF, kPitch = kCols * sizeof(T) + 16;
+  static_assert(4 * 32 * kPitch <= sizeof buffer, "LDS");
+  uint8_t* part = buffer + wave * 32 * kPitch;
+  float scale_w[kF][16], bias[kF][16];
+  const uint64_t n1 = n0 + left[1], m1 = m0 + left[0];
 #pragma unroll
-      for (uint32_t step = 0; step < 4; ++step) {
-        const uint32_t now = step % 2, next = 1 - now;
-        if (step < 3) {
+  for (uint32_t i = 0; i < kF; ++i) {
 #pragma unroll
-          for (uint32_t b = 0; b < kF; ++b) x[next][b] = read(s, step + 1, 0, b), w[next][b] = read(s, step + 1, 1, b);
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kF; ++i) {
-          if (step == 3 && i == kF / 2) {  // the next copy, in the midst of this one's last instructions
-            __builtin_amdgcn_sched_barrier(0);
-            if (more) {
-              finish(s + 1);
-#pragma unroll
-              for (uint32_t b = 0; b < kF; ++b) x[next][b] = read(s + 1, 0, 0, b), w[next][b] = read(s + 1, 0, 1, b);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-#pragma unroll
-          for (uint32_t j = 0; j < kF; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[now][i], x[now][j], acc[i][j], 0, 0, 0);
-        }
-      }
+    for (uint32_t e = 0; e < 16; ++e) {
+      const uint64_t n = min(n1 + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4, uint64_t(p.n) - 1);
+      scale_w[i][e] = p.w_scale(uint32_t(n));
+      bias[i][e] = p.bias ? float(static_cast<const T*>(p.bias)[n]) : 0.0f;
     }
   }
+  __syncthreads();  // all have read their operands
 #pragma unroll
   for (uint32_t j = 0; j < kF; ++j) {
-    const uint64_t m = m0 + left[0] + j * 32 + lane % 32;
-    if (m >= p.m) continue;
-    const float scale = p.x_scale(uint32_t(m));
+    const float scale_x = p.x_scale(uint32_t(min(m1 + j * 32 + lane % 32, uint64_t(p.m) - 1)));
 #pragma unroll
     for (uint32_t i = 0; i < kF; ++i) {
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        const int sums[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        store4<T>(p, uint32_t(m), n0 + left[1] + i * 32 + q * 8 + lane / 32 * 4, sums, scale);
+        float v[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+          v[e] = float(acc[i][j][4 * q + e]) * scale_x * scale_w[i][4 * q + e] + bias[i][4 * q + e];
+        store_block<true>(reinterpret_cast<T*>(part + lane % 32 * kPitch) + i * 32 + q * 8 + lane / 32 * 4, 4, v);
       }
+    }
+    constexpr uint32_t kAcross = kCols / kC, kDown = 64 / kAcross;  // lanes to a row, rows at a time
+#pragma unroll
+    for (uint32_t u = 0; u < 32 / kDown; ++u) {
+      const uint32_t r = u * kDown + lane / kAcross;
+      const uint64_t m = m1 + j * 32 + r, n = n1 + lane % kAcross * kC;
+      Raw<T, kC, false> raw;
+      raw.load(reinterpret_cast<const T*>(part + r * kPitch) + lane % kAcross * kC, kC, false);
+      if (m < p.m && n < p.n) raw.template store<true>(static_cast<T*>(p.out) + int64_t(m) * p.ld + int64_t(n), block_width<kC>(n, p.n));
     }
   }
 }
