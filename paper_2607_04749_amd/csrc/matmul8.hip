@@ -48,88 +48,134 @@ __device__ __forceinline__ void store4(const Product& p, uint32_t m, uint64_t n,
   if (width) raw.store(out, width);
 }
 
-// ---------------------------------------------------------------------------
-// Few rows: the weights are read once, and everything waits for them.  A workgroup
-// has 16 columns of the output and all its rows (kM blocks of 16); its wavefronts
-// share the sums' length between them, each with its operands straight from memory into
-// registers, and add up in LDS.
+// Operands stand in LDS as rows of 128 columns, whose 8 chunks of 16 bytes are
+// permuted: row r has chunk c at place c ^ (r % 8), so that reads of one chunk of 8
+// rows touch all banks.  They come straight from memory (`direct`, 16 bytes a lane
+// at multiples of 16, 8 rows to an instruction, whose lanes take the chunks in the order
+// of their places), or by way of registers.  Neighbouring lanes have neighbouring
+// chunks: fragments of matrix instructions, whose neighbours are rows, took four times as long to load.
+constexpr uint32_t kDepth = 128;
 
-constexpr uint32_t kFewStep = 64;  // of the sum by one matrix instruction
-constexpr uint32_t kFewBatch = 4;  // steps whose loads are under way at once
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
 
-template <uint32_t kM>
-__device__ __forceinline__ void few_multiply(const i32x4& w, const i32x4 (&x)[kM], i32x4 (&acc)[kM]) {
-#pragma unroll
-  for (uint32_t t = 0; t < kM; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x[t], acc[t], 0, 0, 0);
+__device__ __forceinline__ void load_direct(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)to, 16, 0, 0);
 }
 
-__device__ __forceinline__ i32x4 load16(const uint8_t* p) {
-  Raw8<16, true> r;
-  r.load(p, 16, false);
-  return i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
+__device__ __forceinline__ void place16(uint8_t* to, const Raw8<16, false>& r) {
+  *reinterpret_cast<i32x4*>(to) = i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
 }
 
-__device__ __forceinline__ i32x4 load16_tail(const uint8_t* p, uint64_t k, uint32_t end) {
-  Raw8<16, false> r;
-  r.zero();
+// The 16 bytes from column k of the row at p on, zeros past `end`.
+__device__ __forceinline__ void load_tail(Raw8<16, false>& r, const uint8_t* p, uint64_t k, uint32_t end) {
   const uint32_t width = block_width<16>(k, end);
+  r.zero();
   if (width) r.load(p + k, width, end < 16);
   r.shift(width);
-  return i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
 }
 
-template <typename T, uint32_t kM>
-__global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p) {
-  extern __shared__ i32x4 parts[];  // [wavefront][kM][lane]
+// ---------------------------------------------------------------------------
+// Few rows: the weights are read once, and everything waits for them.  A workgroup
+// has 16 columns of the output and all its rows (kG groups of 8); its wavefronts
+// share the sums' length between them, each with kAhead stages of 128 columns on their way into LDS
+// of its own, and add up at the end.
+
+template <uint32_t kG>
+constexpr uint32_t kAhead = kG == 1 ? 4 : kG == 2 ? 3 : 2;
+template <uint32_t kG>
+constexpr uint32_t kStage = (2 + kG) * 1024;  // bytes: 16 rows of w, 8 kG of x
+
+template <uint32_t kG, bool kDirect>
+__global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t wide) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t memory[];
+  constexpr uint32_t kM = (kG + 1) / 2, kLoads = 2 + kG, kSlots = kAhead<kG>;
   const uint32_t lane = threadIdx.x % 64, waves = blockDim.x / 64;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint64_t n0 = uint64_t(blockIdx.x) * 16;
+  uint8_t* slots = memory + wave * kSlots * kStage<kG>;
   // rows past the end repeat the last one; what comes of them is not stored
-  const uint8_t* w = p.w + int64_t(min(n0 + lane % 16, uint64_t(p.n) - 1)) * p.wld;
-  const uint8_t* x[kM];
+  const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+  const uint8_t* rows[kLoads];
 #pragma unroll
-  for (uint32_t t = 0; t < kM; ++t) x[t] = p.x + int64_t(min(t * 16 + lane % 16, p.m - 1)) * p.xld;
-  const uint32_t steps = p.k / kFewStep, part = lane / 16 * 16;
-  const uint32_t from = uint32_t(uint64_t(steps) * wave / waves), to = uint32_t(uint64_t(steps) * (wave + 1) / waves);
+  for (uint32_t i = 0; i < kLoads; ++i)
+    rows[i] = i < 2 ? p.w + int64_t(min(n0 + i * 8 + lane / 8, uint64_t(p.n) - 1)) * p.wld
+                    : p.x + int64_t(min((i - 2) * 8 + lane / 8, p.m - 1)) * p.xld;
+  const uint32_t whole = p.k / kDepth;
+  const uint32_t from = uint32_t(uint64_t(whole) * wave / waves), to = uint32_t(uint64_t(whole) * (wave + 1) / waves);
+
   i32x4 acc[kM] = {};
-  uint32_t s = from;
-  for (; s + kFewBatch <= to; s += kFewBatch) {
-    i32x4 rw[kFewBatch], rx[kFewBatch][kM];
+  const uint32_t at = lane % 16 * kDepth + (lane / 16 ^ lane % 8) * 16;
+  auto multiply = [&](const uint8_t* slot) {
 #pragma unroll
-    for (uint32_t b = 0; b < kFewBatch; ++b) {
-      const uint64_t k = uint64_t(s + b) * kFewStep + part;
-      rw[b] = load16(w + k);
+    for (uint32_t step = 0; step < 2; ++step) {
+      const i32x4 w = *reinterpret_cast<const i32x4*>(slot + (at ^ step * 64));
 #pragma unroll
-      for (uint32_t t = 0; t < kM; ++t) rx[b][t] = load16(x[t] + k);
+      for (uint32_t t = 0; t < kM; ++t) {
+        // of a last group of 8 rows, lanes 8 .. 15 read the same again
+        const uint32_t row = kG % 2 && t == kM - 1 ? at & ~(8 * kDepth) : at;
+        const i32x4 x = *reinterpret_cast<const i32x4*>(slot + 2048 + t * 2048 + (row ^ step * 64));
+        acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc[t], 0, 0, 0);
+      }
     }
-    compiler_fence();
+  };
+  if constexpr (kDirect) {
+    auto start = [&](uint32_t s) {
 #pragma unroll
-    for (uint32_t b = 0; b < kFewBatch; ++b) few_multiply<kM>(rw[b], rx[b], acc);
-  }
-  for (; s < to; ++s) {
-    const uint64_t k = uint64_t(s) * kFewStep + part;
-    i32x4 rx[kM];
+      for (uint32_t i = 0; i < kLoads; ++i) load_direct(rows[i] + uint64_t(s) * kDepth + chunk, slots + s % kSlots * kStage<kG> + i * 1024);
+    };
+    const uint32_t first = min(from + kSlots, to);
+    for (uint32_t s = from; s < first; ++s) start(s);
+    for (uint32_t s = from; s < to; ++s) {
+      // the oldest stage has arrived where at most the loads of kSlots - 1 later ones are under way
+      if (s + kSlots <= to) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kSlots - 1)) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      multiply(slots + s % kSlots * kStage<kG>);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+      if (s + kSlots < to) start(s + kSlots);
+    }
+  } else {
+    for (uint32_t s0 = from; s0 < to; s0 += kSlots) {
+      Raw8<16, false> r[kSlots][kLoads];
 #pragma unroll
-    for (uint32_t t = 0; t < kM; ++t) rx[t] = load16(x[t] + k);
-    few_multiply<kM>(load16(w + k), rx, acc);
-  }
-  if (wave == waves - 1 && p.k % kFewStep) {
-    const uint64_t k = uint64_t(steps) * kFewStep + part;
-    i32x4 rx[kM];
+      for (uint32_t b = 0; b < kSlots; ++b) {
+        if (s0 + b >= to) break;
 #pragma unroll
-    for (uint32_t t = 0; t < kM; ++t) rx[t] = load16_tail(x[t], k, p.k);
-    few_multiply<kM>(load16_tail(w, k, p.k), rx, acc);
+        for (uint32_t i = 0; i < kLoads; ++i) r[b][i].load(rows[i] + uint64_t(s0 + b) * kDepth + chunk, 16, false);
+      }
+      compiler_fence();
+#pragma unroll
+      for (uint32_t b = 0; b < kSlots; ++b) {
+        if (s0 + b >= to) break;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) place16(slots + b * kStage<kG> + i * 1024 + lane * 16, r[b][i]);
+        multiply(slots + b * kStage<kG>);
+      }
+    }
   }
+  if (wave == waves - 1 && p.k % kDepth) {
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+      Raw8<16, false> r;
+      load_tail(r, rows[i], uint64_t(whole) * kDepth + chunk, p.k);
+      place16(slots + i * 1024 + lane * 16, r);
+    }
+    multiply(slots);
+  }
+  __syncthreads();
+  i32x4* parts = reinterpret_cast<i32x4*>(memory);  // [wavefront][kM][lane]
 #pragma unroll
   for (uint32_t t = 0; t < kM; ++t) parts[(wave * kM + t) * 64 + lane] = acc[t];
   __syncthreads();
-  for (uint32_t at = threadIdx.x; at < kM * 64; at += blockDim.x) {
-    i32x4 sum = parts[at];
-    for (uint32_t v = 1; v < waves; ++v) sum += parts[v * kM * 64 + at];
-    const uint32_t m = at / 64 * 16 + at % 16;
+  for (uint32_t e = threadIdx.x; e < kM * 64; e += blockDim.x) {
+    i32x4 sum = parts[e];
+    for (uint32_t v = 1; v < waves; ++v) sum += parts[v * kM * 64 + e];
+    const uint32_t m = e / 64 * 16 + e % 16;
     if (m >= p.m) continue;
     const int sums[4] = {sum[0], sum[1], sum[2], sum[3]};
-    store4<T>(p, m, n0 + at % 64 / 16 * 4, sums, p.x_scale(m));
+    const uint64_t n = n0 + e % 64 / 16 * 4;
+    if (wide) store4<float>(p, m, n, sums, p.x_scale(m));
+    else store4<bf16>(p, m, n, sums, p.x_scale(m));
   }
 }
 
@@ -138,8 +184,6 @@ __global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p) {
 // quarter in registers.  128 columns of the operands at a time stand in LDS, twice:
 // while one copy is multiplied the other one is filled, straight from memory
 // (kDirect: rows at multiples of 16 bytes), or by way of registers.
-
-constexpr uint32_t kDepth = 128;
 
 struct Tiles {
   uint32_t m, n;  // tiles down and across
@@ -158,9 +202,6 @@ __device__ __forceinline__ void place_tile(const Tiles& t, uint32_t* tm, uint32_
   *tm = band * kBand + rest - *tn * down;
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
-
 template <typename T, uint32_t kF, bool kDirect>
 __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
   constexpr uint32_t kTile = 64 * kF;
@@ -172,8 +213,6 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint64_t m0 = uint64_t(tm) * kTile, n0 = uint64_t(tn) * kTile;
   const uint8_t* base[2] = {p.x + int64_t(m0) * p.xld, p.w + int64_t(n0) * p.wld};
-  // Row r of a tile has its chunk c of 16 bytes at place c ^ (r % 8), so that reads of 8 rows
-  // of one chunk touch all banks; a load's lanes have the chunks that fill 8 rows in order.
   const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
   uint32_t offset[2][kLoads];
 #pragma unroll
@@ -186,19 +225,15 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
   // load `i` of operand o, of 128 columns from k on, into copy c or on its way there in registers
   auto start = [&](uint64_t k, uint32_t c, uint32_t o, uint32_t i) {
     if constexpr (kDirect)
-      __builtin_amdgcn_global_load_lds((global_void*)(base[o] + k + offset[o][i]),
-                                       (lds_void*)&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024], 16, 0, 0);
+      load_direct(base[o] + k + offset[o][i], &buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024]);
     else staged[o][i].load(base[o] + k + offset[o][i], 16, false);
   };
   auto place = [&](uint32_t c) {
 #pragma unroll
     for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) {
-        const Raw8<16, false>& r = staged[o][i];
-        *reinterpret_cast<i32x4*>(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16]) =
-            i32x4{int(r.w[0]), int(r.w[1]), int(r.w[2]), int(r.w[3])};
-      }
+      for (uint32_t i = 0; i < kLoads; ++i)
+        place16(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16], staged[o][i]);
     }
   };
   // until all wavefronts have filled their part of a copy
@@ -250,16 +285,11 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
   const uint32_t whole = p.k / kDepth, rest = p.k % kDepth;
   if (p.k) {
     if (rest) {
-      const uint64_t k = uint64_t(whole) * kDepth;
-      const uint32_t width = block_width<16>(k + chunk, p.k);
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) {
-          staged[o][i].zero();
-          if (width) staged[o][i].load(base[o] + k + offset[o][i], width, p.k < 16);
-          staged[o][i].shift(width);
-        }
+        for (uint32_t i = 0; i < kLoads; ++i)
+          load_tail(staged[o][i], base[o] + offset[o][i] - chunk, uint64_t(whole) * kDepth + chunk, p.k);
       }
       if (kDirect) place(0);
     } else {
@@ -331,28 +361,30 @@ hipError_t launch_tiles(const Product& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, uint32_t kM>
-hipError_t launch_few(const Product& p, hipStream_t stream) {
-  const uint32_t wgs = (p.n + 15) / 16;
-  // 64 KB of LDS at most
-  const uint32_t waves = std::max(1u, std::min({wgs >= 512 ? 8u : 16u, 64 / kM, p.k / kFewStep}));
-  hipLaunchKernelGGL((matmul8_few_kernel<T, kM>), dim3(wgs), dim3(waves * 64), waves * kM * 1024, stream, p);
+template <uint32_t kG>
+hipError_t launch_few(const Product& p, bool wide, bool direct, hipStream_t stream) {
+  const uint32_t wgs = (p.n + 15) / 16, stages = p.k / kDepth;
+  // all workgroups at once if the CUs' LDS holds them, with as many wavefronts as it then has room for
+  constexpr uint32_t each = kAhead<kG> * kStage<kG>, kLds = 160 << 10, kCus = 256;
+  const uint32_t share = kLds / std::min((wgs + kCus - 1) / kCus, 4u);
+  const uint32_t waves = std::max(1u, std::min({kG > 12 ? 4u : 16u, share / each, (stages + 1) / 2}));
+  const auto kernel = direct ? matmul8_few_kernel<kG, true> : matmul8_few_kernel<kG, false>;
+  hipLaunchKernelGGL(kernel, dim3(wgs), dim3(waves * 64), waves * each, stream, p, uint32_t(wide));
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_block(const Product& p, hipStream_t stream) {
-  switch ((p.m + 15) / 16) {
-    case 1: return launch_few<T, 1>(p, stream);
-    case 2: return launch_few<T, 2>(p, stream);
-    case 3: return launch_few<T, 3>(p, stream);
-    case 4: return launch_few<T, 4>(p, stream);
-    case 5: return launch_few<T, 5>(p, stream);
-    case 6: return launch_few<T, 6>(p, stream);
-    case 7: return launch_few<T, 7>(p, stream);
-    case 8: return launch_few<T, 8>(p, stream);
-  }
   const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | uintptr_t(p.xld) | uintptr_t(p.wld)) & 15) == 0;
+  constexpr bool wide = sizeof(T) == 4;
+  if (p.m <= 8) return launch_few<1>(p, wide, direct, stream);
+  if (p.m <= 16) return launch_few<2>(p, wide, direct, stream);
+  if (p.m <= 32) return launch_few<4>(p, wide, direct, stream);
+  if (p.m <= 48) return launch_few<6>(p, wide, direct, stream);
+  if (p.m <= 64) return launch_few<8>(p, wide, direct, stream);
+  if (p.m <= 80) return launch_few<10>(p, wide, direct, stream);
+  if (p.m <= 96) return launch_few<12>(p, wide, direct, stream);
+  if (p.m <= 128) return launch_few<16>(p, wide, direct, stream);
   auto tiles = [&](uint64_t tile) { return ((p.m + tile - 1) / tile) * ((p.n + tile - 1) / tile); };
   if (tiles(256) >= 256) return direct ? launch_tiles<T, 4, true>(p, stream) : launch_tiles<T, 4, false>(p, stream);
   if (tiles(128) >= 256) return direct ? launch_tiles<T, 2, true>(p, stream) : launch_tiles<T, 2, false>(p, stream);
