@@ -55,6 +55,7 @@ __device__ __forceinline__ void store4(const Product& p, uint32_t m, uint64_t n,
 // of their places), or by way of registers.  Neighbouring lanes have neighbouring
 // chunks: fragments of matrix instructions, whose neighbours are rows, took four times as long to load.
 constexpr uint32_t kDepth = 128;
+constexpr uint32_t kCus = 256;
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
@@ -76,23 +77,27 @@ __device__ __forceinline__ void load_tail(Raw8<16, false>& r, const uint8_t* p, 
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: the weights are read once, and everything waits for them.  A workgroup
-// has 16 columns of the output and all its rows (kG groups of 8); its wavefronts
-// share the sums' length between them, each with kAhead stages of 128 columns on their way into LDS
-// of its own, and add up at the end.
+// Few rows: everything waits for the weights.  A workgroup has 16 columns of the
+// output and kG groups of 8 rows; its wavefronts share the sums' length between
+// them, each with kAhead stages of 128 columns on their way into LDS of its own, and add
+// up at the end.
 
 template <uint32_t kG>
 constexpr uint32_t kAhead = kG == 1 ? 4 : kG == 2 ? 3 : 2;
 template <uint32_t kG>
 constexpr uint32_t kStage = (2 + kG) * 1024;  // bytes: 16 rows of w, 8 kG of x
+template <uint32_t kG>
+constexpr uint32_t kFewWaves = kG == 1 ? 6 : kG < 6 ? 16 : kG < 12 ? 8 : 4;  // at most
 
 template <uint32_t kG, bool kDirect>
-__global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t wide) {
+__global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product p, uint32_t wide, uint32_t across) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t memory[];
   constexpr uint32_t kM = (kG + 1) / 2, kLoads = 2 + kG, kSlots = kAhead<kG>;
   const uint32_t lane = threadIdx.x % 64, waves = blockDim.x / 64;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint64_t n0 = uint64_t(blockIdx.x) * 16;
+  const uint32_t down = blockIdx.x / across, m0 = down * kG * 8;
+  const uint64_t n0 = uint64_t(blockIdx.x - down * across) * 16;
+  if (n0 >= p.n) return;
   uint8_t* slots = memory + wave * kSlots * kStage<kG>;
   // rows past the end repeat the last one; what comes of them is not stored
   const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
@@ -100,8 +105,20 @@ __global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t w
 #pragma unroll
   for (uint32_t i = 0; i < kLoads; ++i)
     rows[i] = i < 2 ? p.w + int64_t(min(n0 + i * 8 + lane / 8, uint64_t(p.n) - 1)) * p.wld
-                    : p.x + int64_t(min((i - 2) * 8 + lane / 8, p.m - 1)) * p.xld;
+                    : p.x + int64_t(min(m0 + (i - 2) * 8 + lane / 8, p.m - 1)) * p.xld;
   const uint32_t whole = p.k / kDepth;
+  // the columns past whole stages are the last wavefront's, loaded first and multiplied last
+  const bool rest = wave == waves - 1 && p.k % kDepth;
+  Raw8<16, false> tail[kLoads];
+  const uint32_t tail_width = block_width<16>(uint64_t(whole) * kDepth + chunk, p.k);
+  if (rest) {
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+      tail[i].zero();
+      if (tail_width) tail[i].load(rows[i] + uint64_t(whole) * kDepth + chunk, tail_width, p.k < 16);
+    }
+    compiler_fence();
+  }
   const uint32_t from = uint32_t(uint64_t(whole) * wave / waves), to = uint32_t(uint64_t(whole) * (wave + 1) / waves);
 
   i32x4 acc[kM] = {};
@@ -153,12 +170,11 @@ __global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t w
       }
     }
   }
-  if (wave == waves - 1 && p.k % kDepth) {
+  if (rest) {
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
-      Raw8<16, false> r;
-      load_tail(r, rows[i], uint64_t(whole) * kDepth + chunk, p.k);
-      place16(slots + i * 1024 + lane * 16, r);
+      tail[i].shift(tail_width);
+      place16(slots + i * 1024 + lane * 16, tail[i]);
     }
     multiply(slots);
   }
@@ -170,8 +186,8 @@ __global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t w
   for (uint32_t e = threadIdx.x; e < kM * 64; e += blockDim.x) {
     i32x4 sum = parts[e];
     for (uint32_t v = 1; v < waves; ++v) sum += parts[v * kM * 64 + e];
-    const uint32_t m = e / 64 * 16 + e % 16;
-    if (m >= p.m) continue;
+    const uint32_t m = m0 + e / 64 * 16 + e % 16;
+    if (e / 64 * 16 + e % 16 >= kG * 8 || m >= p.m) continue;
     const int sums[4] = {sum[0], sum[1], sum[2], sum[3]};
     const uint64_t n = n0 + e % 64 / 16 * 4;
     if (wide) store4<float>(p, m, n, sums, p.x_scale(m));
@@ -181,9 +197,9 @@ __global__ __launch_bounds__(1024) void matmul8_few_kernel(Product p, uint32_t w
 
 // ---------------------------------------------------------------------------
 // Tiles of 64 kF x 64 kF of the output by four wavefronts, each of which has a
-// quarter in registers.  128 columns of the operands at a time stand in LDS, twice:
-// while one copy is multiplied the other one is filled, straight from memory
-// (kDirect: rows at multiples of 16 bytes), or by way of registers.
+// quarter in registers.  Stages of 128 columns of the operands stand in kCopies parts of the LDS:
+// while one is multiplied the others are filled, straight from memory
+// (kDirect: rows at multiples of 16 bytes), or, one of them, by way of registers.
 
 struct Tiles {
   uint32_t m, n;  // tiles down and across
@@ -202,12 +218,12 @@ __device__ __forceinline__ void place_tile(const Tiles& t, uint32_t* tm, uint32_
   *tm = band * kBand + rest - *tn * down;
 }
 
-template <typename T, uint32_t kF, bool kDirect>
-__global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
+template <typename T, uint32_t kF, uint32_t kCopies, bool kDirect>
+__global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
   constexpr uint32_t kTile = 64 * kF;
   constexpr uint32_t kLoads = kTile / 32;  // of a wavefront, of 8 rows each, for one operand
   constexpr uint32_t kOperand = kTile * kDepth, kCopy = 2 * kOperand;
-  __shared__ __attribute__((aligned(1024))) uint8_t buffer[2 * kCopy];  // copies of x's and w's rows
+  __shared__ __attribute__((aligned(1024))) uint8_t buffer[kCopies * kCopy];  // of x's and w's rows
   uint32_t tm, tn;
   place_tile(tiles, &tm, &tn);
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -236,10 +252,10 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
         place16(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16], staged[o][i]);
     }
   };
-  // until all wavefronts have filled their part of a copy
-  auto finish = [&](uint32_t c) {
+  // until all wavefronts have filled their part of a copy, with at most kLater loads of others under way
+  auto finish = [&](uint32_t c, auto later) {
     if (!kDirect) place(c);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(later)::value) : "memory");
   };
 
   const uint32_t left[2] = {wave % 2 * (kTile / 2), wave / 2 * (kTile / 2)};  // the wavefront's rows of x and of w
@@ -252,21 +268,23 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
 
   i32x16 acc[kF][kF] = {};  // [of w][of x]
   i32x4 x[2][kF], w[2][kF];
-  // Multiplies copy c, whose first operands are in x[0] and w[0].  `more`: meanwhile fills the other copy with the
-  // columns from k on, and leaves its first operands in their place.  The order is kept as it
-  // stands: reads of the next step's operands and loads of the next copy's, one by one between matrix instructions.
-  auto multiply = [&](uint32_t c, bool more, uint64_t k) {
+  // Multiplies copy c, whose first operands are in x[0] and w[0].  kMore: leaves those of the next copy there.
+  // kFill: meanwhile starts to fill the copy before with the columns from k on.  The order is kept as it
+  // stands: loads, and reads of the next step's operands, one by one between matrix instructions.
+  auto multiply = [&](uint32_t c, auto fill, auto more, uint64_t k) {
+    constexpr bool kFill = decltype(fill)::value, kMore = decltype(more)::value;
     constexpr uint32_t kEach = kF * kF, kReads = 2 * kF;
+    const uint32_t after = c + 1 == kCopies ? 0 : c + 1, before = c ? c - 1 : kCopies - 1;
 #pragma unroll
     for (uint32_t step = 0; step < 4; ++step) {
       const uint32_t now = step % 2, next = 1 - now;
 #pragma unroll
       for (uint32_t q = 0; q < kEach; ++q) {
-        if (more && step == 0) {
+        if (kFill && step == 0) {
 #pragma unroll
-          for (uint32_t d = q * 2 * kLoads / kEach; d < (q + 1) * 2 * kLoads / kEach; ++d) start(k, 1 - c, d / kLoads, d % kLoads);
+          for (uint32_t d = q * 2 * kLoads / kEach; d < (q + 1) * 2 * kLoads / kEach; ++d) start(k, before, d / kLoads, d % kLoads);
         }
-        if (more && step == 3 && q == kEach / 2) finish(1 - c);
+        if (kMore && step == 3 && q == kEach / 2) finish(after, std::integral_constant<uint32_t, kFill ? (kCopies - 2) * 2 * kLoads : 0>());
         __builtin_amdgcn_sched_barrier(0);
         acc[q / kF][q % kF] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[now][q / kF], x[now][q % kF], acc[q / kF][q % kF], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -275,39 +293,47 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
           const uint32_t b = r / 2, o = 1 - r % 2;
           i32x4& to = o ? w[next][b] : x[next][b];
           if (step < 3 && r * kEach * 3 / (4 * kReads) == q) to = read(c, step + 1, o, b);
-          if (more && step == 3 && kEach / 2 + r * (kEach - kEach / 2) * 3 / (4 * kReads) == q) to = read(1 - c, 0, o, b);
+          if (kMore && step == 3 && kEach / 2 + r * (kEach - kEach / 2) * 3 / (4 * kReads) == q) to = read(after, 0, o, b);
         }
       }
     }
   };
 
   // The columns past whole stages come first, so that the loop has whole ones only.
-  const uint32_t whole = p.k / kDepth, rest = p.k % kDepth;
-  if (p.k) {
+  const uint32_t rest = p.k % kDepth != 0, stages = p.k / kDepth + rest;
+  if (stages) {
     if (rest) {
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i)
-          load_tail(staged[o][i], base[o] + offset[o][i] - chunk, uint64_t(whole) * kDepth + chunk, p.k);
+          load_tail(staged[o][i], base[o] + offset[o][i] - chunk, uint64_t(stages - 1) * kDepth + chunk, p.k);
       }
       if (kDirect) place(0);
-    } else {
+    }
+    auto column = [&](uint32_t s) { return uint64_t(s - rest) * kDepth; };
+#pragma unroll
+    for (uint32_t s = 0; s + 1 < kCopies; ++s) {
+      if (s < rest || s >= stages) continue;
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) start(0, 0, o, i);
+        for (uint32_t i = 0; i < kLoads; ++i) start(column(s), s, o, i);
       }
     }
-    finish(0);
+    finish(0, std::integral_constant<uint32_t, 0>());
 #pragma unroll
     for (uint32_t b = 0; b < kF; ++b) x[0][b] = read(0, 0, 0, b), w[0][b] = read(0, 0, 1, b);
-    uint32_t c = 0;
-    for (uint32_t s = rest ? 0 : 1; s < whole; ++s) {
-      multiply(c, true, uint64_t(s) * kDepth);
-      c = 1 - c;
+    uint32_t s = 0, c = 0;
+    for (; s + kCopies - 1 < stages; ++s) {
+      multiply(c, std::true_type(), std::true_type(), column(s + kCopies - 1));
+      c = c + 1 == kCopies ? 0 : c + 1;
     }
-    multiply(c, false, 0);
+    for (; s + 1 < stages; ++s) {
+      multiply(c, std::false_type(), std::true_type(), 0);
+      c = c + 1 == kCopies ? 0 : c + 1;
+    }
+    multiply(c, std::false_type(), std::false_type(), 0);
   }
   // Each wavefront turns 32 rows of its quarter at a time round in a part of the
   // LDS of its own, so that it stores whole rows of 32 kF columns.
@@ -352,24 +378,25 @@ __global__ __launch_bounds__(256, kF == 4 ? 1 : 2) void matmul8_tile_kernel(Prod
   }
 }
 
-template <typename T, uint32_t kF, bool kDirect>
+template <typename T, uint32_t kF, uint32_t kCopies, bool kDirect>
 hipError_t launch_tiles(const Product& p, hipStream_t stream) {
   constexpr uint32_t kTile = 64 * kF;
   Tiles t{(p.m + kTile - 1) / kTile, (p.n + kTile - 1) / kTile, 0};
   t.count = t.m * t.n;
-  hipLaunchKernelGGL((matmul8_tile_kernel<T, kF, kDirect>), dim3(t.count), dim3(256), 0, stream, p, t);
+  hipLaunchKernelGGL((matmul8_tile_kernel<T, kF, kCopies, kDirect>), dim3(t.count), dim3(256), 0, stream, p, t);
   return hipGetLastError();
 }
 
 template <uint32_t kG>
 hipError_t launch_few(const Product& p, bool wide, bool direct, hipStream_t stream) {
-  const uint32_t wgs = (p.n + 15) / 16, stages = p.k / kDepth;
+  // workgroups of the same columns on one XCD, behind one L2
+  const uint32_t across = (p.n + 127) / 128 * 8, wgs = across * ((p.m + 8 * kG - 1) / (8 * kG));
   // all workgroups at once if the CUs' LDS holds them, with as many wavefronts as it then has room for
-  constexpr uint32_t each = kAhead<kG> * kStage<kG>, kLds = 160 << 10, kCus = 256;
-  const uint32_t share = kLds / std::min((wgs + kCus - 1) / kCus, 4u);
-  const uint32_t waves = std::max(1u, std::min({kG > 12 ? 4u : 16u, share / each, (stages + 1) / 2}));
+  constexpr uint32_t each = kAhead<kG> * kStage<kG>, kLds = 160 << 10;
+  const uint32_t share = kLds / std::min((wgs + kCus - 1) / kCus, 4u), stages = p.k / kDepth;
+  const uint32_t waves = std::max(1u, std::min({kFewWaves<kG>, share / each, (stages + 1) / 2}));
   const auto kernel = direct ? matmul8_few_kernel<kG, true> : matmul8_few_kernel<kG, false>;
-  hipLaunchKernelGGL(kernel, dim3(wgs), dim3(waves * 64), waves * each, stream, p, uint32_t(wide));
+  hipLaunchKernelGGL(kernel, dim3(wgs), dim3(waves * 64), waves * each, stream, p, uint32_t(wide), across);
   return hipGetLastError();
 }
 
@@ -377,18 +404,25 @@ template <typename T>
 hipError_t launch_block(const Product& p, hipStream_t stream) {
   const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | uintptr_t(p.xld) | uintptr_t(p.wld)) & 15) == 0;
   constexpr bool wide = sizeof(T) == 4;
-  if (p.m <= 8) return launch_few<1>(p, wide, direct, stream);
-  if (p.m <= 16) return launch_few<2>(p, wide, direct, stream);
-  if (p.m <= 32) return launch_few<4>(p, wide, direct, stream);
-  if (p.m <= 48) return launch_few<6>(p, wide, direct, stream);
-  if (p.m <= 64) return launch_few<8>(p, wide, direct, stream);
-  if (p.m <= 80) return launch_few<10>(p, wide, direct, stream);
-  if (p.m <= 96) return launch_few<12>(p, wide, direct, stream);
-  if (p.m <= 128) return launch_few<16>(p, wide, direct, stream);
+  if (p.m <= 128) {
+    // rows of a workgroup: as many as leave a workgroup to each CU
+    const uint32_t across = (p.n + 15) / 16, split = std::max(1u, std::min((p.m + 7) / 8, kCus / across));
+    const uint32_t groups = ((p.m + 7) / 8 + split - 1) / split;
+    if (groups == 1) return launch_few<1>(p, wide, direct, stream);
+    if (groups == 2) return launch_few<2>(p, wide, direct, stream);
+    if (groups == 3) return launch_few<3>(p, wide, direct, stream);
+    if (groups == 4) return launch_few<4>(p, wide, direct, stream);
+    if (groups <= 6) return launch_few<6>(p, wide, direct, stream);
+    if (groups <= 8) return launch_few<8>(p, wide, direct, stream);
+    if (groups <= 10) return launch_few<10>(p, wide, direct, stream);
+    if (groups <= 12) return launch_few<12>(p, wide, direct, stream);
+    return launch_few<16>(p, wide, direct, stream);
+  }
   auto tiles = [&](uint64_t tile) { return ((p.m + tile - 1) / tile) * ((p.n + tile - 1) / tile); };
-  if (tiles(256) >= 256) return direct ? launch_tiles<T, 4, true>(p, stream) : launch_tiles<T, 4, false>(p, stream);
-  if (tiles(128) >= 256) return direct ? launch_tiles<T, 2, true>(p, stream) : launch_tiles<T, 2, false>(p, stream);
-  return direct ? launch_tiles<T, 1, true>(p, stream) : launch_tiles<T, 1, false>(p, stream);
+  if (tiles(256) >= kCus) return direct ? launch_tiles<T, 4, 2, true>(p, stream) : launch_tiles<T, 4, 2, false>(p, stream);
+  if (tiles(128) >= 2 * kCus) return direct ? launch_tiles<T, 2, 2, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
+  if (tiles(128) >= kCus) return direct ? launch_tiles<T, 2, 4, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
+  return direct ? launch_tiles<T, 1, 4, true>(p, stream) : launch_tiles<T, 1, 2, false>(p, stream);
 }
 
 // Blocks of the output that a launch takes: offsets within them, and workgroups, in 32 bits.

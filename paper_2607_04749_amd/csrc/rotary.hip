@@ -1,4 +1,4 @@
-// rotary.hip -- rotary positions (etc_rotary) and their frequencies.
+// rotary.hip -- rotary positions (etc_rotary).
 //
 //   a' = scale (a cos - b sin), b' = scale (b cos + a sin), the angle position * freq[pair]
 //
@@ -15,8 +15,6 @@ namespace etc {
 
 namespace {
 
-constexpr uint32_t kFlatThreads = 256;
-
 struct Turns {
   double freq[ETC_ROTARY_PAIRS];  // turns a position
   float scale;
@@ -31,16 +29,92 @@ __device__ __forceinline__ void angle(double turns, float scale, float sign, flo
   *s *= scale * sign;
 }
 
-// Any sizes: a lane has one pair, or one column past the pairs.
+// ---------------------------------------------------------------------------
+// Heads whose parts that turn and that do not are whole blocks of 16 bytes: a lane has
+// two blocks, whose columns are pairs (kHalf: of either half of the pairs; else
+// neighbours), of kHeads heads of a token, so that their sines are worked out once; or
+// two blocks of what is copied.
+
+constexpr uint32_t kThreads = 256;
+
+struct Blocks {
+  uint32_t n;            // lanes with work
+  uint32_t heads;
+  uint32_t units;        // pairs of blocks in a head, of which the first `turned` turn
+  uint32_t turned;
+  Divisor by_token, by_unit;  // lanes of a token, units of a head
+};
+
+template <typename T, bool kHalf, uint32_t kHeads>
+__global__ __launch_bounds__(kThreads) void rotary_block_kernel(Turns t, Blocks g, Mat<const T> x, Ids positions, Mat<T> out) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+  if (at >= g.n) return;
+  const uint32_t i = g.by_token.div(at), in_token = at - i * g.by_token.d;
+  const uint32_t slice = g.by_unit.div(in_token), unit = in_token - slice * g.by_unit.d;
+  const bool turns = unit < g.turned;
+  uint32_t ja, jb;  // the columns of the two blocks
+  if (turns) {
+    ja = kHalf ? unit * kC : unit * 2 * kC;
+    jb = kHalf ? ja + t.pairs : ja + kC;
+  } else {
+    ja = 2 * t.pairs + (unit - g.turned) * 2 * kC;
+    jb = ja + kC;
+  }
+  const bool second = jb < t.head_dim;
+  const uint32_t head0 = slice * kHeads;
+  Raw<T, kC, true> a[kHeads], b[kHeads];
+#pragma unroll
+  for (uint32_t h = 0; h < kHeads; ++h) {
+    if (head0 + h >= g.heads) break;
+    const T* from = x.p + int64_t(i) * x.ld + int64_t(head0 + h) * t.head_dim;
+    a[h].template load<true>(from + ja, kC, false);
+    if (second) b[h].template load<true>(from + jb, kC, false);
+  }
+  compiler_fence();
+  float c[kC], s[kC];
+  if (turns) {
+    const double position = double(positions.at(i));
+#pragma unroll
+    for (uint32_t e = 0; e < kC; ++e) angle(position * t.freq[unit * kC + e], t.scale, t.sign, &c[e], &s[e]);
+  }
+#pragma unroll
+  for (uint32_t h = 0; h < kHeads; ++h) {
+    if (head0 + h >= g.heads) break;
+    T* to = out.p + int64_t(i) * out.ld + int64_t(head0 + h) * t.head_dim;
+    if (turns) {
+      float u[kC], v[kC], p[kC], q[kC];
+      a[h].widen(u, kC);
+      b[h].widen(v, kC);
+#pragma unroll
+      for (uint32_t e = 0; e < kC; ++e) {
+        if (kHalf) {
+          p[e] = u[e] * c[e] - v[e] * s[e];
+          q[e] = v[e] * c[e] + u[e] * s[e];
+        } else if (e % 2 == 0) {
+          p[e] = u[e] * c[e / 2] - u[e + 1] * s[e / 2];
+          p[e + 1] = u[e + 1] * c[e / 2] + u[e] * s[e / 2];
+          q[e] = v[e] * c[kC / 2 + e / 2] - v[e + 1] * s[kC / 2 + e / 2];
+          q[e + 1] = v[e + 1] * c[kC / 2 + e / 2] + v[e] * s[kC / 2 + e / 2];
+        }
+      }
+      a[h].narrow(p);
+      b[h].narrow(q);
+    }
+    a[h].template store<true>(to + ja, kC);
+    if (second) b[h].template store<true>(to + jb, kC);
+  }
+}
+
+// Any other sizes: a lane has one pair, or one column past the pairs.
 template <typename T, bool kHalf>
-__global__ __launch_bounds__(kFlatThreads) void rotary_pair_kernel(Turns t, uint64_t n, uint32_t heads, uint32_t items,
-                                                                   Mat<const T> x, Ids positions, Mat<T> out) {
-  const uint64_t at = uint64_t(blockIdx.x) * kFlatThreads + threadIdx.x;
+__global__ __launch_bounds__(kThreads) void rotary_pair_kernel(Turns t, uint32_t n, uint32_t heads, Divisor by_item, Divisor by_head,
+                                                               Mat<const T> x, Ids positions, Mat<T> out) {
+  const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
   if (at >= n) return;
-  const uint32_t item = uint32_t(at % items);
-  const uint64_t rest = at / items;
-  const uint64_t i = rest / heads;
-  const uint64_t head = uint64_t(rest - i * heads) * t.head_dim;
+  const uint32_t rest = by_item.div(at), item = at - rest * by_item.d;
+  const uint32_t i = by_head.div(rest);
+  const int64_t head = int64_t(rest - i * by_head.d) * t.head_dim;
   const T* from = x.p + int64_t(i) * x.ld + head;
   T* to = out.p + int64_t(i) * out.ld + head;
   if (item >= t.pairs) {
@@ -55,6 +129,38 @@ __global__ __launch_bounds__(kFlatThreads) void rotary_pair_kernel(Turns t, uint
   to[jb] = T(b * c + a * s);
 }
 
+template <typename T, bool kHalf>
+hipError_t launch_layout(const etc_rotary_args& a, const Turns& t, hipStream_t stream) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  const uint32_t heads = uint32_t(a.x.cols / a.head_dim);
+  const bool in_place = a.x.data == a.out.data;  // columns past the pairs are where they belong
+  const bool blocks = t.pairs % kC == 0 && t.head_dim % kC == 0;
+  const uint32_t past = in_place ? 0 : t.head_dim - 2 * t.pairs;
+  const uint32_t items = blocks ? t.pairs / kC + (past / kC + 1) / 2 : t.pairs + past;  // lanes of a head
+  // sines once for several heads, where that leaves lanes enough
+  const uint32_t each = !blocks ? 1 : int64_t(a.x.rows) * heads * items >= (1 << 20) ? 4 : 1;
+  const uint32_t lanes = (heads + each - 1) / each * items;  // of a token
+  const int64_t most = std::max<int64_t>(1, INT32_MAX / lanes);
+  for (int64_t at = 0; at < a.x.rows; at += most) {
+    const uint32_t rows = uint32_t(std::min(most, a.x.rows - at));
+    const uint32_t wide = a.positions.dtype == ETC_IDS_I64;
+    const Ids ids{static_cast<const char*>(a.positions.data) + at * (wide ? 8 : 4), wide};
+    const uint32_t n = rows * lanes;
+    const dim3 wgs((n + kThreads - 1) / kThreads), threads(kThreads);
+    if (blocks) {
+      const Blocks g{n, heads, items, t.pairs / kC, Divisor(lanes), Divisor(items)};
+      const auto kernel = each == 1 ? rotary_block_kernel<T, kHalf, 1> : rotary_block_kernel<T, kHalf, 4>;
+      hipLaunchKernelGGL(kernel, wgs, threads, 0, stream, t, g, cmat<T>(a.x, at), ids, mat<T>(a.out, at));
+    } else {
+      hipLaunchKernelGGL((rotary_pair_kernel<T, kHalf>), wgs, threads, 0, stream, t, n, heads, Divisor(items), Divisor(heads),
+                         cmat<T>(a.x, at), ids, mat<T>(a.out, at));
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <typename T>
 hipError_t launch_type(const etc_rotary_args& a, hipStream_t stream) {
   Turns t;
@@ -65,22 +171,7 @@ hipError_t launch_type(const etc_rotary_args& a, hipStream_t stream) {
   t.sign = a.backward ? -1.0f : 1.0f;
   t.pairs = uint32_t(d.pairs);
   t.head_dim = uint32_t(a.head_dim);
-  const uint32_t heads = uint32_t(a.x.cols / a.head_dim);
-  const bool in_place = a.x.data == a.out.data;  // columns past the pairs are where they belong
-  const uint32_t items = in_place ? t.pairs : t.head_dim - t.pairs;
-  const auto kernel = d.layout == ETC_ROTARY_HALF ? rotary_pair_kernel<T, true> : rotary_pair_kernel<T, false>;
-  const int64_t most = std::max<int64_t>(1, INT32_MAX / (int64_t(heads) * items));
-  for (int64_t at = 0; at < a.x.rows; at += most) {
-    const int64_t rows = std::min(most, a.x.rows - at);
-    const uint64_t n = uint64_t(rows) * heads * items;
-    const uint32_t wide = a.positions.dtype == ETC_IDS_I64;
-    const Ids ids{static_cast<const char*>(a.positions.data) + at * (wide ? 8 : 4), wide};
-    hipLaunchKernelGGL(kernel, dim3(uint32_t((n + kFlatThreads - 1) / kFlatThreads)), dim3(kFlatThreads), 0, stream, t, n, heads,
-                       items, cmat<T>(a.x, at), ids, mat<T>(a.out, at));
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  return d.layout == ETC_ROTARY_HALF ? launch_layout<T, true>(a, t, stream) : launch_layout<T, false>(a, t, stream);
 }
 
 }  // namespace
