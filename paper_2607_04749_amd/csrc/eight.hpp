@@ -165,6 +165,24 @@ struct Raw8 {
   }
 };
 
+// A lane's block of kC columns in a row that a workgroup holds whole (cols >= kC).
+// A row's last block is its last kC columns: the first `again` of them are the
+// block's before it too.  Both lanes work out the same for those and store it, so
+// nothing is shifted and stores are whole; only sums over the row leave them out.
+template <uint32_t kC, bool kWhole>
+struct Span {
+  uint64_t at;
+  uint32_t again;
+  bool in;  // whether there is such a block
+  __device__ __forceinline__ Span(uint64_t col, uint32_t cols) : at(col), again(0), in(col < cols) {
+    if (!kWhole && in && cols - col < kC) {
+      at = cols - kC;
+      again = uint32_t(col - at);
+    }
+  }
+  __device__ __forceinline__ bool counts(uint32_t e) const { return kWhole || e >= again; }
+};
+
 // The sum over a wavefront, in every lane, in an order of its own.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

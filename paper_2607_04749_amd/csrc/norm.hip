@@ -62,19 +62,18 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<co
                                                                float* rstd) {
   constexpr uint32_t kC = kLaneCols<T>;
   const int64_t i = blockIdx.x;
-  const bool shorter = in.cols < kC;
-  Raw<T, kC, kWhole> rx[kB], rr[kB], rw[kB];
+  auto span = [&](uint32_t b) { return Span<kC, kWhole>(uint64_t(b * blockDim.x + threadIdx.x) * kC, in.cols); };
+  Raw<T, kC, true> rx[kB], rr[kB], rw[kB];
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
-    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-    const uint32_t width = block_width<kC>(col, in.cols);
+    const auto p = span(b);
     rx[b].zero();
     rr[b].zero();
     rw[b].zero();
-    if (!width) continue;
-    rx[b].template load<true>(x.p + i * x.ld + col, width, shorter);
-    if (residual.p) rr[b].template load<true>(residual.p + i * residual.ld + col, width, shorter);
-    rw[b].load(weight + col, width, shorter);
+    if (!p.in) continue;
+    rx[b].template load<true>(x.p + i * x.ld + p.at, kC, false);
+    if (residual.p) rr[b].template load<true>(residual.p + i * residual.ld + p.at, kC, false);
+    rw[b].load(weight + p.at, kC, false);
   }
   compiler_fence();
   float s[kB][kC], y[kB][kC];
@@ -82,20 +81,18 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<co
   uint32_t largest = 0;
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
-    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-    const uint32_t width = block_width<kC>(col, in.cols);
+    const auto p = span(b);
     float r[kC], w[kC];
-    rx[b].widen(s[b], width);
-    rr[b].widen(r, width);
-    rw[b].widen(w, width);
+    rx[b].widen(s[b], kC);
+    rr[b].widen(r, kC);
+    rw[b].widen(w, kC);
 #pragma unroll
     for (uint32_t e = 0; e < kC; ++e) {
       s[b][e] += r[e];
       y[b][e] = s[b][e] * w[e];
-      total += s[b][e] * s[b][e];  // past the row's end all are 0
+      total += p.counts(e) ? s[b][e] * s[b][e] : 0.0f;
       if (k8) largest = max(largest, magnitude(y[b][e]));
     }
-    if (sum.p && width) store_block<kWhole, true>(sum.p + i * sum.ld + col, width, s[b]);
   }
   row_reduce<k8 != kNone8>(&total, &largest);
   const float r = 1.0f / sqrtf(total * in.per_col + in.eps);
@@ -108,23 +105,23 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<co
   }
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
-    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-    const uint32_t width = block_width<kC>(col, in.cols);
-    if (!width) continue;
+    const auto p = span(b);
+    if (!p.in) continue;
+    if (sum.p) store_block<true, true>(sum.p + i * sum.ld + p.at, kC, s[b]);
     if (k8) {
-      Raw8<kC, kWhole> q;
+      Raw8<kC, true> q;
       q.template narrow<k8 ? k8 : kInt8>(y[b], factor);
-      q.template store<true>(out8.p + i * out8.ld + col, width);
+      q.template store<true>(out8.p + i * out8.ld + p.at, kC);
     }
     if (out.p) {
 #pragma unroll
       for (uint32_t e = 0; e < kC; ++e) y[b][e] *= r;
-      store_block<kWhole, true>(out.p + i * out.ld + col, width, y[b]);
+      store_block<true, true>(out.p + i * out.ld + p.at, kC, y[b]);
     }
   }
 }
 
-// Rows that no workgroup's registers hold: read twice, the second time from the
+// Rows that no workgroup's registers hold, or of less than a block: read twice, the second time from the
 // caches.  One block after the other, so that a row may be written where it stands.
 template <typename T, bool kWhole, Kind8 k8>
 __global__ __launch_bounds__(kMostWaves * 64) void norm_long_kernel(NormIn in, Mat<const T> x, Mat<const T> residual,
@@ -139,9 +136,9 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_long_kernel(NormIn in, M
       const uint32_t width = block_width<kC>(col, in.cols);
       Raw<T, kC, kWhole> raw, rr, rw;
       rr.zero();
-      raw.load(x.p + i * x.ld + col, width, false);
-      if (residual.p) rr.load(residual.p + i * residual.ld + col, width, false);
-      rw.load(weight + col, width, false);
+      raw.load(x.p + i * x.ld + col, width, in.cols < kC);
+      if (residual.p) rr.load(residual.p + i * residual.ld + col, width, in.cols < kC);
+      rw.load(weight + col, width, in.cols < kC);
       float s[kC], v[kC], w[kC];
       raw.widen(s, width);
       rr.widen(v, width);
@@ -181,9 +178,12 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_long_kernel(NormIn in, M
 template <typename T, bool kWhole, Kind8 k8>
 hipError_t launch(const etc_norm_args& a, hipStream_t stream) {
   const uint32_t blocks = blocks_per_row(a.x.cols, kLaneCols<T>);
-  uint32_t per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
+#ifndef PB
+#define PB 2
+#endif
+  uint32_t per = blocks <= 64 ? 1 : blocks <= PB * 64 * kMostWaves ? PB : kMostBlocks;
   const uint32_t waves = std::min((blocks + 64 * per - 1) / (64 * per), kMostWaves);
-  const auto kernel = blocks > waves * 64 * per ? norm_long_kernel<T, kWhole, k8>
+  const auto kernel = blocks > waves * 64 * per || a.x.cols < kLaneCols<T> ? norm_long_kernel<T, kWhole, k8>
                       : per == 1                ? norm_kernel<T, 1, kWhole, k8>
                       : per == 2                ? norm_kernel<T, 2, kWhole, k8>
                                                 : norm_kernel<T, kMostBlocks, kWhole, k8>;

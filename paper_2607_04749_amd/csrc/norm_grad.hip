@@ -16,35 +16,37 @@ namespace etc {
 namespace {
 
 constexpr uint32_t kMostWaves = 16;
-constexpr uint32_t kMostBlocks = 4;
+constexpr uint32_t kMostBlocks = 2;
 constexpr uint32_t kAllWaves = 4096;  // wavefronts of a launch that sums
 
 struct Shape {
   uint32_t rows, cols;
   uint32_t per, waves, parts;  // blocks of a lane, wavefronts of a row, workgroups that sum
-  bool longer;                 // than the registers of a workgroup
+  bool longer;                 // than the registers of a workgroup, or less than a block
 };
 
 Shape shape_of(uint64_t rows, uint64_t cols, uint32_t block) {
   const uint64_t blocks = (cols + block - 1) / block;
   Shape s{uint32_t(rows), uint32_t(cols), 0, 0, 0, false};
-  s.per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
+  s.per = blocks <= 64 * kMostWaves ? 1 : kMostBlocks;
   s.waves = uint32_t(std::min<uint64_t>((blocks + 64 * s.per - 1) / (64 * s.per), kMostWaves));
-  s.longer = blocks > uint64_t(s.waves) * 64 * s.per;
+  s.longer = blocks > uint64_t(s.waves) * 64 * s.per || cols < block;
   s.parts = uint32_t(std::min<uint64_t>(rows, kAllWaves / s.waves));
   return s;
 }
 
-__device__ __forceinline__ float row_sum(float sum) {
-  __shared__ float sums[kMostWaves];
+// The sum over the `waves` wavefronts that share a row; all wavefronts of the
+// workgroup call it, with `turn` 0 and 1 in turn: who writes a turn's sums has passed the barrier of the other
+// turn, before which all have read this one's.
+__device__ __forceinline__ float row_sum(float sum, uint32_t waves, uint32_t turn) {
+  __shared__ float sums[2][kMostWaves];
   sum = wave_sum(sum);
-  const uint32_t waves = blockDim.x / 64;
-  if (waves == 1) return sum;
-  __syncthreads();  // the row before has been read
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+  if (blockDim.x == 64) return sum;
+  if (threadIdx.x % 64 == 0) sums[turn][threadIdx.x / 64] = sum;
   __syncthreads();
+  const uint32_t first = threadIdx.x / 64 / waves * waves;
   float total = 0.0f;
-  for (uint32_t w = 0; w < waves; ++w) total += sums[w];
+  for (uint32_t w = 0; w < waves; ++w) total += sums[turn][min(first + w, kMostWaves - 1)];
   return total;
 }
 
@@ -53,12 +55,13 @@ struct Input {  // a block of x
   static constexpr uint32_t kC = kLaneCols<T>;
   Raw<T, kC, kWhole> raw;
   Raw8<kC, kWhole> raw8;
-  float scale;
+  float scale, before;  // of the block's last column; of its first ones, which may be of the group before
+  uint32_t again = 0;   // how many of those there are
 
   __device__ __forceinline__ void zero() {
     if (k8) raw8.zero();
     else raw.zero();
-    scale = 0.0f;
+    scale = before = 0.0f;
   }
   __device__ __forceinline__ void load(const Mat<const T>& x, const Mat8& x8, int64_t i, uint64_t col, uint32_t width, bool shorter) {
     if (k8) {
@@ -68,13 +71,21 @@ struct Input {  // a block of x
       raw.template load<true>(x.p + i * x.ld + col, width, shorter);
     }
   }
+  template <bool kAll>
+  __device__ __forceinline__ void load(const Mat<const T>& x, const Mat8& x8, int64_t i, const Span<kC, kAll>& p) {
+    load(x, x8, i, p.at, kC, false);
+    if (kAll || !k8) return;
+    again = p.again;
+    before = scale;
+    scale = x8.scale[i * x8.sld + ((p.at + kC - 1) >> x8.shift)];
+  }
   // times r
   __device__ __forceinline__ void widen(float (&v)[kC], uint32_t width, float r) const {
     if constexpr (k8 != kNone8) {
       raw8.template widen<k8>(v, width);
-      const float f = scale * r;
+      const float f = scale * r, f0 = before * r;
 #pragma unroll
-      for (uint32_t e = 0; e < kC; ++e) v[e] *= f;
+      for (uint32_t e = 0; e < kC; ++e) v[e] *= e < again ? f0 : f;
     } else {
       raw.widen(v, width);
 #pragma unroll
@@ -82,6 +93,8 @@ struct Input {  // a block of x
     }
   }
 };
+
+bool is_few(const Shape& s) { return s.rows && !s.longer && s.rows <= 1024 && (s.per == 1 || s.rows <= 128); }
 
 // n of kC fp32 sums
 template <uint32_t kC, bool kWhole>
@@ -101,86 +114,210 @@ __device__ __forceinline__ void store_sums(float* p, uint32_t n, const float (&v
   }
 }
 
-template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kSum>
-__global__ __launch_bounds__(kMostWaves * 64) void norm_grad_kernel(uint32_t rows, uint32_t cols, float per_col, Mat<const T> grad,
-                                                                    Mat<const T> x, Mat8 x8, const T* weight, Mat<const T> dsum,
-                                                                    Mat<T> dx, const float* rstd, float* partial) {
-  constexpr uint32_t kC = kLaneCols<T>;
-  const bool shorter = cols < kC;
-  Raw<T, kC, kWhole> rw[kB];
-  float sums[kB][kC] = {};
-#pragma unroll
-  for (uint32_t b = 0; b < kB; ++b) {
-    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-    const uint32_t width = block_width<kC>(col, cols);
-    rw[b].zero();
-    if (width) rw[b].load(weight + col, width, shorter);
+struct In {
+  uint32_t rows, cols;
+  float per_col;  // 1 / cols
+};
+
+// Lane `lane` of the `lanes` that share a row: kB blocks of it, `lanes` blocks apart.
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8>
+struct Row {
+  static constexpr uint32_t kC = kLaneCols<T>;
+  typedef Raw<T, kC, true> Block;
+  Block grad[kB], dsum[kB];
+  Input<T, true, k8> x[kB];
+  float r;
+
+  __device__ __forceinline__ static Span<kC, kWhole> span(const In& in, uint32_t b, uint32_t lane, uint32_t lanes) {
+    return Span<kC, kWhole>(uint64_t(b * lanes + lane) * kC, in.cols);
   }
-  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const int64_t i = int64_t(row);
-    const float r = rstd[i];
-    Raw<T, kC, kWhole> rg[kB], rd[kB];
-    Input<T, kWhole, k8> rx[kB];
+
+  __device__ __forceinline__ static void load_weight(const In& in, uint32_t lane, uint32_t lanes, const T* weight, Block (&w)[kB]) {
 #pragma unroll
     for (uint32_t b = 0; b < kB; ++b) {
-      const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-      const uint32_t width = block_width<kC>(col, cols);
-      rg[b].zero();
-      rd[b].zero();
-      rx[b].zero();
-      if (!width) continue;
-      rg[b].template load<true>(grad.p + i * grad.ld + col, width, shorter);
-      rx[b].load(x, x8, i, col, width, shorter);
-      if (dsum.p) rd[b].template load<true>(dsum.p + i * dsum.ld + col, width, shorter);
+      const auto p = span(in, b, lane, lanes);
+      w[b].zero();
+      if (p.in) w[b].load(weight + p.at, kC, false);
     }
-    compiler_fence();
-    float dot = 0.0f;
-    float dn[kB][kC], n[kB][kC];
+  }
+
+  __device__ __forceinline__ void load(const In& in, int64_t i, uint32_t lane, uint32_t lanes, const Mat<const T>& g,
+                                       const Mat<const T>& x16, const Mat8& x8, const Mat<const T>& d, const float* rstd) {
+    r = rstd[i];
 #pragma unroll
     for (uint32_t b = 0; b < kB; ++b) {
-      const uint32_t width = block_width<kC>(uint64_t(b * blockDim.x + threadIdx.x) * kC, cols);
-      float w[kC];
-      rg[b].widen(dn[b], width);
-      rx[b].widen(n[b], width, r);
-      rw[b].widen(w, width);
+      const auto p = span(in, b, lane, lanes);
+      grad[b].zero();
+      dsum[b].zero();
+      x[b].zero();
+      if (!p.in) continue;
+      grad[b].template load<true>(g.p + i * g.ld + p.at, kC, false);
+      x[b].load(x16, x8, i, p);
+      if (d.p) dsum[b].template load<true>(d.p + i * d.ld + p.at, kC, false);
+    }
+  }
+
+  // the lane's part of the products dn n; kSum: adds grad n to the columns' sums
+  template <bool kSum>
+  __device__ __forceinline__ float products(const In& in, uint32_t lane, uint32_t lanes, const Block (&weight)[kB],
+                                            float (&sums)[kB][kC]) const {
+    float dot = 0.0f;
+#pragma unroll
+    for (uint32_t b = 0; b < kB; ++b) {
+      const auto p = span(in, b, lane, lanes);
+      float g[kC], n[kC], w[kC];
+      grad[b].widen(g, kC);
+      x[b].widen(n, kC, r);
+      weight[b].widen(w, kC);
 #pragma unroll
       for (uint32_t e = 0; e < kC; ++e) {
-        if (kSum) sums[b][e] += dn[b][e] * n[b][e];
-        dn[b][e] *= w[e];
-        dot += dn[b][e] * n[b][e];
+        if (kSum) sums[b][e] += g[e] * n[e];
+        dot += p.counts(e) ? g[e] * w[e] * n[e] : 0.0f;
       }
     }
-    const float mean = row_sum(dot) * per_col;
+    return dot;
+  }
+
+  __device__ __forceinline__ void store(const In& in, int64_t i, uint32_t lane, uint32_t lanes, const Block (&weight)[kB], float mean,
+                                        const Mat<T>& dx) const {
 #pragma unroll
     for (uint32_t b = 0; b < kB; ++b) {
-      const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-      const uint32_t width = block_width<kC>(col, cols);
-      if (!width) continue;
-      float d[kC];
-      rd[b].widen(d, width);
+      const auto p = span(in, b, lane, lanes);
+      if (!p.in) continue;
+      float g[kC], n[kC], w[kC], d[kC];
+      grad[b].widen(g, kC);
+      x[b].widen(n, kC, r);
+      weight[b].widen(w, kC);
+      dsum[b].widen(d, kC);
 #pragma unroll
-      for (uint32_t e = 0; e < kC; ++e) d[e] += r * (dn[b][e] - n[b][e] * mean);
-      store_block<kWhole, true>(dx.p + i * dx.ld + col, width, d);
+      for (uint32_t e = 0; e < kC; ++e) d[e] += r * (g[e] * w[e] - n[e] * mean);
+      store_block<true, true>(dx.p + i * dx.ld + p.at, kC, d);
     }
+  }
+};
+
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kSum>
+__global__ __launch_bounds__(kMostWaves * 64) void norm_grad_kernel(In in, Mat<const T> grad, Mat<const T> x, Mat8 x8,
+                                                                    const T* weight, Mat<const T> dsum, Mat<T> dx,
+                                                                    const float* rstd, float* partial) {
+  using R = Row<T, kB, kWhole, k8>;
+  constexpr uint32_t kC = kLaneCols<T>;
+  const uint32_t lane = threadIdx.x, lanes = blockDim.x;
+  typename R::Block w[kB];
+  R::load_weight(in, lane, lanes, weight, w);
+  float sums[kB][kC] = {};
+  uint32_t turn = 0;
+  for (uint64_t row = blockIdx.x; row < in.rows; row += gridDim.x, turn = 1 - turn) {
+    R now;
+    now.load(in, int64_t(row), lane, lanes, grad, x, x8, dsum, rstd);
+    compiler_fence();
+    const float dot = now.template products<kSum>(in, lane, lanes, w, sums);
+    now.store(in, int64_t(row), lane, lanes, w, row_sum(dot, blockDim.x / 64, turn) * in.per_col, dx);
   }
   if (!kSum) return;
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
-    const uint64_t col = uint64_t(b * blockDim.x + threadIdx.x) * kC;
-    const uint32_t width = block_width<kC>(col, cols);
-    if (width) store_sums<kC, kWhole>(partial + uint64_t(blockIdx.x) * cols + col, width, sums[b]);
+    const auto p = R::span(in, b, lane, lanes);
+    if (p.in) store_sums<kC, true>(partial + uint64_t(blockIdx.x) * in.cols + p.at, kC, sums[b]);
   }
 }
 
-// Rows that no workgroup's registers hold: read twice, the second time from the
+// Few rows, in one launch: the first workgroups have kFewBlocks blocks of columns and
+// all rows, and so the whole of dweight's sums; the others have rows, as many at
+// once as their wavefronts hold.  grad and x are read twice, the second time from the caches.
+constexpr uint32_t kFewThreads = 1024, kBatch = 2;
+constexpr uint32_t kXcds = 8;
+
+template <typename T, uint32_t kFewBlocks, bool kWhole, Kind8 k8>
+__device__ __forceinline__ void few_columns(const In& in, uint32_t slab, const Mat<const T>& grad, const Mat<const T>& x,
+                                            const Mat8& x8, const float* rstd, float* dweight, uint32_t accumulate) {
+  constexpr uint32_t kC = kLaneCols<T>, kWaves = kFewThreads / 64, kFewDown = kFewThreads / kFewBlocks;
+  __shared__ float shared[kWaves][kFewBlocks * kC];
+  const uint32_t across = threadIdx.x % kFewBlocks, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint64_t left = uint64_t(slab) * kFewBlocks * kC, col = left + across * kC;
+  if (left >= in.cols) return;
+  const uint32_t width = block_width<kC>(col, in.cols);
+  const bool mine = threadIdx.x < kFewBlocks * kC && left + threadIdx.x < in.cols;
+  const float before = mine && accumulate ? dweight[left + threadIdx.x] : 0.0f;
+  float sum[kC] = {};
+  if (width) {
+    for (uint32_t i0 = threadIdx.x / kFewBlocks; i0 < in.rows; i0 += kFewDown * kBatch) {
+      Raw<T, kC, kWhole> rg[kBatch];
+      Input<T, kWhole, k8> rx[kBatch];
+      float r[kBatch];
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        const uint32_t i = i0 + b * kFewDown < in.rows ? i0 + b * kFewDown : i0;
+        rg[b].load(grad.p + int64_t(i) * grad.ld + col, width, in.cols < kC);
+        rx[b].load(x, x8, i, col, width, in.cols < kC);
+        r[b] = rstd[i];
+      }
+      compiler_fence();
+#pragma unroll
+      for (uint32_t b = 0; b < kBatch; ++b) {
+        if (i0 + b * kFewDown >= in.rows) break;
+        float g[kC], n[kC];
+        rg[b].widen(g, width);
+        rx[b].widen(n, width, r[b]);
+#pragma unroll
+        for (uint32_t e = 0; e < kC; ++e) sum[e] += g[e] * n[e];
+      }
+    }
+  }
+  // over the wavefront's rows, which lie kFewBlocks lanes apart, then over the wavefronts
+#pragma unroll
+  for (uint32_t e = 0; e < kC; ++e) {
+#pragma unroll
+    for (uint32_t d = kFewBlocks; d < 64; d *= 2) sum[e] += __shfl_xor(sum[e], int(d));
+    if (lane < kFewBlocks) shared[wave][lane * kC + e] = sum[e];
+  }
+  __syncthreads();
+  if (!mine) return;
+  float all = 0.0f;
+#pragma unroll
+  for (uint32_t w = 0; w < kWaves; ++w) all += shared[w][threadIdx.x];
+  dweight[left + threadIdx.x] = before + all;
+}
+
+template <typename T, uint32_t kB, uint32_t kFewBlocks, bool kWhole, Kind8 k8>
+__global__ __launch_bounds__(kFewThreads) void norm_grad_few_kernel(In in, uint32_t slabs, uint32_t waves, Mat<const T> grad,
+                                                                    Mat<const T> x, Mat8 x8, const T* weight, Mat<const T> dsum,
+                                                                    Mat<T> dx, const float* rstd, float* dweight,
+                                                                    uint32_t accumulate) {
+  constexpr uint32_t kC = kLaneCols<T>;
+  if (blockIdx.x < slabs) {  // neighbours, which share lines, on one XCD
+    few_columns<T, kFewBlocks, kWhole, k8>(in, blockIdx.x % kXcds * (slabs / kXcds) + blockIdx.x / kXcds, grad, x, x8, rstd, dweight, accumulate);
+    return;
+  }
+  const uint32_t wave = threadIdx.x / 64, group = wave / waves, groups = kFewThreads / 64 / waves;
+  const uint32_t lanes = waves * 64, lane = threadIdx.x - group * lanes;
+  const uint32_t row = (blockIdx.x - slabs) * groups + group;
+  const bool mine = group < groups && row < in.rows;  // the others take part in the barriers
+  const int64_t i = mine ? row : 0;
+  using R = Row<T, kB, kWhole, k8>;
+  typename R::Block w[kB];
+  R now;
+  if (mine) {
+    now.load(in, i, lane, lanes, grad, x, x8, dsum, rstd);
+    R::load_weight(in, lane, lanes, weight, w);
+  }
+  compiler_fence();
+  float none[kB][kC], dot = 0.0f;
+  if (mine) dot = now.template products<false>(in, lane, lanes, w, none);
+  const float mean = row_sum(dot, waves, 0) * in.per_col;
+  if (mine) now.store(in, i, lane, lanes, w, mean, dx);
+}
+
+// Rows that no workgroup's registers hold, or of less than a block: read twice, the second time from the
 // caches, with the columns' sums in the workgroup's row of the workspace.
 template <typename T, bool kWhole, Kind8 k8, bool kSum>
-__global__ __launch_bounds__(kMostWaves * 64) void norm_grad_long_kernel(uint32_t rows, uint32_t cols, float per_col,
-                                                                         Mat<const T> grad, Mat<const T> x, Mat8 x8,
+__global__ __launch_bounds__(kMostWaves * 64) void norm_grad_long_kernel(In in, Mat<const T> grad, Mat<const T> x, Mat8 x8,
                                                                          const T* weight, Mat<const T> dsum, Mat<T> dx,
                                                                          const float* rstd, float* partial) {
   constexpr uint32_t kC = kLaneCols<T>;
-  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+  const uint32_t rows = in.rows, cols = in.cols;
+  uint32_t turn = 0;
+  for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x, turn = 1 - turn) {
     const int64_t i = int64_t(row);
     const float r = rstd[i];
     float dot = 0.0f, mean = 0.0f;
@@ -190,10 +327,11 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_grad_long_kernel(uint32_
         Raw<T, kC, kWhole> rg, rd, rw;
         Input<T, kWhole, k8> rx;
         rd.zero();
-        rg.load(grad.p + i * grad.ld + col, width, false);
-        rx.load(x, x8, i, col, width, false);
-        rw.load(weight + col, width, false);
-        if (pass && dsum.p) rd.load(dsum.p + i * dsum.ld + col, width, false);
+        const bool shorter = cols < kC;
+        rg.load(grad.p + i * grad.ld + col, width, shorter);
+        rx.load(x, x8, i, col, width, shorter);
+        rw.load(weight + col, width, shorter);
+        if (pass && dsum.p) rd.load(dsum.p + i * dsum.ld + col, width, shorter);
         float g[kC], n[kC], w[kC], d[kC];
         rg.widen(g, width);
         rx.widen(n, width, r);
@@ -214,7 +352,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_grad_long_kernel(uint32_
         for (uint32_t e = 0; e < kC; ++e) d[e] += r * (g[e] * w[e] - n[e] * mean);
         store_block<kWhole>(dx.p + i * dx.ld + col, width, d);
       }
-      if (pass == 0) mean = row_sum(dot) * per_col;
+      if (pass == 0) mean = row_sum(dot, blockDim.x / 64, turn) * in.per_col;
     }
   }
 }
@@ -257,11 +395,10 @@ template <typename T, bool kWhole, Kind8 k8, bool kSum>
 hipError_t launch_rows(const etc_norm_grad_args& a, const Shape& s, hipStream_t stream) {
   const auto kernel = s.longer     ? norm_grad_long_kernel<T, kWhole, k8, kSum>
                       : s.per == 1 ? norm_grad_kernel<T, 1, kWhole, k8, kSum>
-                      : s.per == 2 ? norm_grad_kernel<T, 2, kWhole, k8, kSum>
                                    : norm_grad_kernel<T, kMostBlocks, kWhole, k8, kSum>;
   const uint32_t threads = s.waves * 64;
   auto run = [&](int64_t first, uint32_t rows, uint32_t wgs) -> hipError_t {
-    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), 0, stream, rows, s.cols, 1.0f / float(s.cols), cmat<T>(a.grad, first),
+    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), 0, stream, In{rows, s.cols, 1.0f / float(s.cols)}, cmat<T>(a.grad, first),
                        cmat<T>(a.x, first), mat8(a.x8, first), static_cast<const T*>(a.weight.data), cmat<T>(a.dsum, first),
                        mat<T>(a.dx, first), a.rstd + first, static_cast<float*>(a.workspace));
     return hipGetLastError();
@@ -274,6 +411,20 @@ template <typename T, bool kWhole, Kind8 k8>
 hipError_t launch_sum(const etc_norm_grad_args& a, hipStream_t stream) {
   const Shape s = shape_of(uint64_t(a.grad.rows), uint64_t(a.grad.cols), kLaneCols<T>);
   if (!a.dweight.data) return launch_rows<T, kWhole, k8, false>(a, s, stream);
+  if (is_few(s)) {
+    // blocks of a workgroup that sums columns: two where there are few workgroups and many rows
+    const uint32_t blocks = blocks_per_row(s.cols, kLaneCols<T>), narrow = s.rows > 512 && blocks <= 512 ? 2 : 4;
+    const uint32_t slabs = (blocks + narrow - 1) / narrow;
+    const uint32_t padded = (slabs + kXcds - 1) / kXcds * kXcds, groups = kFewThreads / 64 / s.waves;
+    const auto kernel = s.per != 1    ? norm_grad_few_kernel<T, kMostBlocks, 4, kWhole, k8>
+                        : narrow == 2 ? norm_grad_few_kernel<T, 1, 2, kWhole, k8>
+                                      : norm_grad_few_kernel<T, 1, 4, kWhole, k8>;
+    hipLaunchKernelGGL(kernel, dim3(padded + (s.rows + groups - 1) / groups), dim3(kFewThreads), 0, stream,
+                       In{s.rows, s.cols, 1.0f / float(s.cols)}, padded, s.waves, cmat<T>(a.grad, 0), cmat<T>(a.x, 0), mat8(a.x8, 0),
+                       static_cast<const T*>(a.weight.data), cmat<T>(a.dsum, 0), mat<T>(a.dx, 0), a.rstd,
+                       static_cast<float*>(a.dweight.data), uint32_t(a.accumulate != 0));
+    return hipGetLastError();
+  }
   if (s.rows) {
     const hipError_t e = launch_rows<T, kWhole, k8, true>(a, s, stream);
     if (e != hipSuccess) return e;
