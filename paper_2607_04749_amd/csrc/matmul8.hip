@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "eight.hpp"
 
@@ -199,7 +200,13 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
 // Tiles of 64 kF x 64 kF of the output by four wavefronts, each of which has a
 // quarter in registers.  Stages of 128 columns of the operands stand in kCopies parts of the LDS:
 // while one is multiplied the others are filled, straight from memory
-// (kDirect: rows at multiples of 16 bytes), or, one of them, by way of registers.
+// (kDirect: rows at multiples of 16 bytes), or two parts in turn by way of registers, which
+// hold the kSets stages behind.
+
+template <uint32_t... kS, typename F>
+__device__ __forceinline__ void for_each_below(std::integer_sequence<uint32_t, kS...>, F f) {
+  (f(std::integral_constant<uint32_t, kS>()), ...);
+}
 
 struct Tiles {
   uint32_t m, n;  // tiles down and across
@@ -237,25 +244,32 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
     offset[0][i] = uint32_t(min(uint64_t(row), p.m - 1 - m0)) * uint32_t(p.xld) + chunk;
     offset[1][i] = uint32_t(min(uint64_t(row), p.n - 1 - n0)) * uint32_t(p.wld) + chunk;
   }
-  Raw8<16, false> staged[2][kLoads];
+  constexpr uint32_t kSets = kDirect || kF == 4 ? 1 : 2;
+  constexpr uint32_t kFar = kDirect ? kCopies - 1 : kSets;  // stages between one that starts and the one that is multiplied
+  Raw8<16, false> staged[kSets][2][kLoads];
   // load `i` of operand o, of 128 columns from k on, into copy c or on its way there in registers
-  auto start = [&](uint64_t k, uint32_t c, uint32_t o, uint32_t i) {
+  auto start = [&](uint64_t k, uint32_t c, auto set, uint32_t o, uint32_t i) {
     if constexpr (kDirect)
       load_direct(base[o] + k + offset[o][i], &buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024]);
-    else staged[o][i].load(base[o] + k + offset[o][i], 16, false);
+    else staged[set()][o][i].load(base[o] + k + offset[o][i], 16, false);
   };
-  auto place = [&](uint32_t c) {
+  auto place = [&](uint32_t c, auto set) {
 #pragma unroll
     for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
       for (uint32_t i = 0; i < kLoads; ++i)
-        place16(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16], staged[o][i]);
+        place16(&buffer[c * kCopy + o * kOperand + (wave * kLoads + i) * 1024 + lane * 16], staged[set()][o][i]);
     }
   };
-  // until all wavefronts have filled their part of a copy, with at most kLater loads of others under way
-  auto finish = [&](uint32_t c, auto later) {
-    if (!kDirect) place(c);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(later)::value) : "memory");
+  using Zero = std::integral_constant<uint32_t, 0>;
+  // until all wavefronts have filled their part of a copy, with at most `later` direct loads of others under way
+  auto finish = [&](uint32_t c, auto set, auto later) {
+    if constexpr (kDirect) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(later)::value) : "memory");
+    } else {
+      place(c, set);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
   };
 
   const uint32_t left[2] = {wave % 2 * (kTile / 2), wave / 2 * (kTile / 2)};  // the wavefront's rows of x and of w
@@ -269,11 +283,13 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
   i32x16 acc[kF][kF] = {};  // [of w][of x]
   i32x4 x[2][kF], w[2][kF];
   // Multiplies copy c, whose first operands are in x[0] and w[0].  kMore: leaves those of the next copy there.
-  // kFill: meanwhile starts to fill the copy before with the columns from k on.  The order is kept as it
+  // kFill: meanwhile starts the stage from column k on, into the copy before (kDirect) or into register set
+  // kSet, whose stage has been placed; the next stage is in the set behind it.  The order is kept as it
   // stands: loads, and reads of the next step's operands, one by one between matrix instructions.
-  auto multiply = [&](uint32_t c, auto fill, auto more, uint64_t k) {
+  auto multiply = [&](uint32_t c, auto set, auto fill, auto more, uint64_t k) {
     constexpr bool kFill = decltype(fill)::value, kMore = decltype(more)::value;
-    constexpr uint32_t kEach = kF * kF, kReads = 2 * kF;
+    constexpr uint32_t kEach = kF * kF, kReads = 2 * kF, kSet = decltype(set)::value;
+    using Behind = std::integral_constant<uint32_t, (kSet + 1) % kSets>;
     const uint32_t after = c + 1 == kCopies ? 0 : c + 1, before = c ? c - 1 : kCopies - 1;
 #pragma unroll
     for (uint32_t step = 0; step < 4; ++step) {
@@ -282,9 +298,10 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
       for (uint32_t q = 0; q < kEach; ++q) {
         if (kFill && step == 0) {
 #pragma unroll
-          for (uint32_t d = q * 2 * kLoads / kEach; d < (q + 1) * 2 * kLoads / kEach; ++d) start(k, before, d / kLoads, d % kLoads);
+          for (uint32_t d = q * 2 * kLoads / kEach; d < (q + 1) * 2 * kLoads / kEach; ++d) start(k, before, set, d / kLoads, d % kLoads);
         }
-        if (kMore && step == 3 && q == kEach / 2) finish(after, std::integral_constant<uint32_t, kFill ? (kCopies - 2) * 2 * kLoads : 0>());
+        if (kMore && step == 3 && q == kEach / 2)
+          finish(after, Behind(), std::integral_constant<uint32_t, kFill ? (kCopies - 2) * 2 * kLoads : 0>());
         __builtin_amdgcn_sched_barrier(0);
         acc[q / kF][q % kF] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[now][q / kF], x[now][q % kF], acc[q / kF][q % kF], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -307,33 +324,46 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i)
-          load_tail(staged[o][i], base[o] + offset[o][i] - chunk, uint64_t(stages - 1) * kDepth + chunk, p.k);
+          load_tail(staged[0][o][i], base[o] + offset[o][i] - chunk, uint64_t(stages - 1) * kDepth + chunk, p.k);
       }
-      if (kDirect) place(0);
+      if (kDirect) place(0, Zero());
     }
     auto column = [&](uint32_t s) { return uint64_t(s - rest) * kDepth; };
-#pragma unroll
-    for (uint32_t s = 0; s + 1 < kCopies; ++s) {
-      if (s < rest || s >= stages) continue;
+    // stage s's copy, and its register set
+    auto start_stage = [&](auto s) {
+      constexpr uint32_t kS = decltype(s)::value;
+      if (kS < rest || kS >= stages) return;
 #pragma unroll
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) start(column(s), s, o, i);
+        for (uint32_t i = 0; i < kLoads; ++i) start(column(kS), kS % kCopies, std::integral_constant<uint32_t, kS % kSets>(), o, i);
       }
-    }
-    finish(0, std::integral_constant<uint32_t, 0>());
+    };
+    for_each_below(std::make_integer_sequence<uint32_t, kFar>(), start_stage);
+    finish(0, Zero(), Zero());
 #pragma unroll
     for (uint32_t b = 0; b < kF; ++b) x[0][b] = read(0, 0, 0, b), w[0][b] = read(0, 0, 1, b);
     uint32_t s = 0, c = 0;
-    for (; s + kCopies - 1 < stages; ++s) {
-      multiply(c, std::true_type(), std::true_type(), column(s + kCopies - 1));
-      c = c + 1 == kCopies ? 0 : c + 1;
+    auto next_copy = [&] { c = c + 1 == kCopies ? 0 : c + 1; };
+    if constexpr (kSets == 1) {
+      for (; s + kFar < stages; ++s, next_copy()) multiply(c, Zero(), std::true_type(), std::true_type(), column(s + kFar));
+      for (; s + 1 < stages; ++s, next_copy()) multiply(c, Zero(), std::false_type(), std::true_type(), 0);
+      multiply(c, Zero(), std::false_type(), std::false_type(), 0);
+    } else {  // in rounds of kSets stages, whose registers are named in the code
+      auto turn = [&](auto set, auto sure) {
+        if (decltype(sure)::value || s + kFar < stages) multiply(c, set, std::true_type(), std::true_type(), column(s + kFar));
+        else if (s + 1 < stages) multiply(c, set, std::false_type(), std::true_type(), 0);
+        else if (s < stages) multiply(c, set, std::false_type(), std::false_type(), 0);
+        ++s;
+        next_copy();
+      };
+      auto round = [&](auto sure) {
+        turn(Zero(), sure);
+        turn(std::integral_constant<uint32_t, 1>(), sure);
+      };
+      while (s + kFar + kSets <= stages) round(std::true_type());
+      while (s < stages) round(std::false_type());
     }
-    for (; s + 1 < stages; ++s) {
-      multiply(c, std::false_type(), std::true_type(), 0);
-      c = c + 1 == kCopies ? 0 : c + 1;
-    }
-    multiply(c, std::false_type(), std::false_type(), 0);
   }
   // Each wavefront turns 32 rows of its quarter at a time round in a part of the
   // LDS of its own, so that it stores whole rows of 32 kF columns.
@@ -378,12 +408,173 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
   }
 }
 
+// ---------------------------------------------------------------------------
+// Tiles of 64 x 64 where larger ones would leave CUs idle.  Each of the four
+// wavefronts has the whole tile, for one of the four steps of 32 columns in each
+// stage: four matrix instructions to four reads, where a quarter of the tile each had one to two
+// and waited for LDS (300 x 1280 x 8192: 20.1 us).  The wavefronts' sums are added up in LDS at the end.
+
+template <typename T, bool kDirect>
+__global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles tiles) {
+  constexpr uint32_t kTile = 64, kLoads = 2, kOperand = kTile * kDepth, kCopy = 2 * kOperand;
+  constexpr uint32_t kCopies = kDirect ? 4 : 2, kSets = 4;  // stages in LDS; behind them, in registers (kDirect: none)
+  constexpr uint32_t kPitch = kTile * 4 + 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t buffer[4 * kTile * kPitch];
+  static_assert(kCopies * kCopy <= sizeof buffer, "LDS");
+  uint32_t tm, tn;
+  place_tile(tiles, &tm, &tn);
+  const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint64_t m0 = uint64_t(tm) * kTile, n0 = uint64_t(tn) * kTile;
+  const uint8_t* rows[2][kLoads];
+#pragma unroll
+  for (uint32_t i = 0; i < kLoads; ++i) {
+    const uint32_t row = (wave * kLoads + i) * 8 + lane / 8;  // rows past the end repeat the last one
+    rows[0][i] = p.x + int64_t(min(m0 + row, uint64_t(p.m) - 1)) * p.xld;
+    rows[1][i] = p.w + int64_t(min(n0 + row, uint64_t(p.n) - 1)) * p.wld;
+  }
+  const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+  const uint32_t rest = p.k % kDepth != 0, stages = p.k / kDepth + rest;
+  auto target = [&](uint32_t s, uint32_t o, uint32_t i) { return &buffer[s % kCopies * kCopy + o * kOperand + (wave * kLoads + i) * 1024]; };
+  Raw8<16, false> staged[kSets][2][kLoads];
+  auto start = [&](uint32_t s, auto set) {  // a stage of whole columns: those past whole stages come first
+    const uint64_t k = uint64_t(s - rest) * kDepth + chunk;
+#pragma unroll
+    for (uint32_t o = 0; o < 2; ++o) {
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i) {
+        if constexpr (kDirect) load_direct(rows[o][i] + k, target(s, o, i));
+        else staged[set()][o][i].load(rows[o][i] + k, 16, false);
+      }
+    }
+  };
+  auto place = [&](uint32_t s, auto set) {
+#pragma unroll
+    for (uint32_t o = 0; o < 2; ++o) {
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i) place16(target(s, o, i) + lane * 16, staged[set()][o][i]);
+    }
+  };
+  const uint32_t at = lane % 32 * kDepth + ((wave * 2 + lane / 32) ^ lane % 8) * 16;
+  i32x16 acc[2][2] = {};  // [of w][of x]
+  i32x4 x[2], w[2];
+  auto read = [&](uint32_t s) {
+#pragma unroll
+    for (uint32_t b = 0; b < 2; ++b) {
+      x[b] = *reinterpret_cast<const i32x4*>(&buffer[s % kCopies * kCopy + at + b * 32 * kDepth]);
+      w[b] = *reinterpret_cast<const i32x4*>(&buffer[s % kCopies * kCopy + kOperand + at + b * 32 * kDepth]);
+    }
+  };
+  using Zero = std::integral_constant<uint32_t, 0>;
+  // Multiplies stage s, whose operands are in x and w, and reads stage s + 1 (which register set `next` holds) behind it.
+  // kFill: starts a stage, into the copy that has been read or into the set that has been placed.
+  auto turn = [&](uint32_t s, auto next, auto fill) {
+    i32x4 u[2] = {x[0], x[1]}, v[2] = {w[0], w[1]};
+    constexpr bool kFill = decltype(fill)::value;
+    if constexpr (kDirect) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kFill ? (kCopies - 2) * 2 * kLoads : 0) : "memory");
+    } else {
+      place(s + 1, next);
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    read(s + 1);
+    if constexpr (kFill) start(kDirect ? s + kCopies : s + 1 + kSets, next);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+#pragma unroll
+      for (uint32_t j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v[i], u[j], acc[i][j], 0, 0, 0);
+    }
+  };
+  if (stages) {
+    if (rest) {
+#pragma unroll
+      for (uint32_t o = 0; o < 2; ++o) {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) load_tail(staged[0][o][i], rows[o][i], uint64_t(stages - 1) * kDepth + chunk, p.k);
+      }
+      if (kDirect) place(0, Zero());
+    }
+    for_each_below(std::make_integer_sequence<uint32_t, kDirect ? kCopies : kSets>(), [&](auto s) {
+      if (s() >= rest && s() < stages) start(s(), std::integral_constant<uint32_t, s() % kSets>());
+    });
+    if constexpr (kDirect) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    } else {
+      place(0, Zero());
+      if (kSets < stages) start(kSets, Zero());
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    read(0);
+    uint32_t s = 0;
+    if constexpr (kDirect) {
+      for (; s + kCopies < stages; ++s) turn(s, Zero(), std::true_type());
+      for (; s + 1 < stages; ++s) turn(s, Zero(), std::false_type());
+    } else {
+      // in rounds of kSets stages, whose registers are named in the code: turn s places set (s + 1) % kSets
+      for (; s + 2 * kSets < stages; s += kSets)
+        for_each_below(std::make_integer_sequence<uint32_t, kSets>(),
+                       [&](auto d) { turn(s + d(), std::integral_constant<uint32_t, (d() + 1) % kSets>(), std::true_type()); });
+      for (; s + 1 < stages; s += kSets)
+        for_each_below(std::make_integer_sequence<uint32_t, kSets>(), [&](auto d) {
+          using Next = std::integral_constant<uint32_t, (d() + 1) % kSets>;
+          if (s + d() + 1 + kSets < stages) turn(s + d(), Next(), std::true_type());
+          else if (s + d() + 1 < stages) turn(s + d(), Next(), std::false_type());
+        });
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+#pragma unroll
+      for (uint32_t j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+    }
+  }
+  __syncthreads();  // all have read their operands
+#pragma unroll
+  for (uint32_t i = 0; i < 2; ++i) {
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j) {
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q)
+        *reinterpret_cast<i32x4*>(buffer + (wave * kTile + j * 32 + lane % 32) * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * 4) =
+            i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    }
+  }
+  __syncthreads();
+  constexpr uint32_t kC = kLaneCols<T>, kAcross = kTile / kC;  // lanes to a row
+  for (uint32_t e = threadIdx.x; e < kTile * kAcross; e += 256) {
+    const uint32_t r = e / kAcross, c = e % kAcross * kC;
+    const uint64_t m = m0 + r, n = n0 + c;
+    if (m >= p.m || n >= p.n) continue;
+    const float scale_x = p.x_scale(uint32_t(m));
+    float v[kC];
+#pragma unroll
+    for (uint32_t b = 0; b < kC; b += 4) {
+      i32x4 sum = {};
+#pragma unroll
+      for (uint32_t f = 0; f < 4; ++f) sum += *reinterpret_cast<const i32x4*>(buffer + (f * kTile + r) * kPitch + (c + b) * 4);
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t column = uint32_t(min(n + b + k, uint64_t(p.n) - 1));
+        v[b + k] = float(sum[k]) * scale_x * p.w_scale(column) + (p.bias ? float(static_cast<const T*>(p.bias)[column]) : 0.0f);
+      }
+    }
+    store_block<false, true>(static_cast<T*>(p.out) + int64_t(m) * p.ld + int64_t(n), block_width<kC>(n, p.n), v);
+  }
+}
+
 template <typename T, uint32_t kF, uint32_t kCopies, bool kDirect>
 hipError_t launch_tiles(const Product& p, hipStream_t stream) {
   constexpr uint32_t kTile = 64 * kF;
   Tiles t{(p.m + kTile - 1) / kTile, (p.n + kTile - 1) / kTile, 0};
   t.count = t.m * t.n;
   hipLaunchKernelGGL((matmul8_tile_kernel<T, kF, kCopies, kDirect>), dim3(t.count), dim3(256), 0, stream, p, t);
+  return hipGetLastError();
+}
+
+template <typename T, bool kDirect>
+hipError_t launch_split(const Product& p, hipStream_t stream) {
+  Tiles t{(p.m + 63) / 64, (p.n + 63) / 64, 0};
+  t.count = t.m * t.n;
+  hipLaunchKernelGGL((matmul8_split_kernel<T, kDirect>), dim3(t.count), dim3(256), 0, stream, p, t);
   return hipGetLastError();
 }
 
@@ -422,7 +613,7 @@ hipError_t launch_block(const Product& p, hipStream_t stream) {
   if (tiles(256) >= kCus) return direct ? launch_tiles<T, 4, 2, true>(p, stream) : launch_tiles<T, 4, 2, false>(p, stream);
   if (tiles(128) >= 2 * kCus) return direct ? launch_tiles<T, 2, 2, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
   if (tiles(128) >= kCus) return direct ? launch_tiles<T, 2, 4, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
-  return direct ? launch_tiles<T, 1, 4, true>(p, stream) : launch_tiles<T, 1, 2, false>(p, stream);
+  return direct ? launch_split<T, true>(p, stream) : launch_split<T, false>(p, stream);
 }
 
 // Blocks of the output that a launch takes: offsets within them, and workgroups, in 32 bits.
