@@ -40,7 +40,7 @@ constexpr uint32_t kThreads = 256;
 struct Blocks {
   uint32_t n;            // lanes with work
   uint32_t heads;
-  uint32_t units;        // pairs of blocks in a head, of which the first `turned` turn
+  uint32_t units;        // of a lane (pairs of blocks; pairs) in a head, of which the first `turned` turn
   uint32_t turned;
   Divisor by_token, by_unit;  // lanes of a token, units of a head
 };
@@ -106,27 +106,39 @@ __global__ __launch_bounds__(kThreads) void rotary_block_kernel(Turns t, Blocks 
   }
 }
 
-// Any other sizes: a lane has one pair, or one column past the pairs.
-template <typename T, bool kHalf>
-__global__ __launch_bounds__(kThreads) void rotary_pair_kernel(Turns t, uint32_t n, uint32_t heads, Divisor by_item, Divisor by_head,
-                                                               Mat<const T> x, Ids positions, Mat<T> out) {
+// Any other sizes: a lane has a pair, or a column past the pairs, of kHeads heads of a token.
+template <typename T, bool kHalf, uint32_t kHeads>
+__global__ __launch_bounds__(kThreads) void rotary_pair_kernel(Turns t, Blocks g, Mat<const T> x, Ids positions, Mat<T> out) {
   const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
-  if (at >= n) return;
-  const uint32_t rest = by_item.div(at), item = at - rest * by_item.d;
-  const uint32_t i = by_head.div(rest);
-  const int64_t head = int64_t(rest - i * by_head.d) * t.head_dim;
-  const T* from = x.p + int64_t(i) * x.ld + head;
-  T* to = out.p + int64_t(i) * out.ld + head;
-  if (item >= t.pairs) {
-    to[item + t.pairs] = from[item + t.pairs];
-    return;
+  if (at >= g.n) return;
+  const uint32_t i = g.by_token.div(at), in_token = at - i * g.by_token.d;
+  const uint32_t slice = g.by_unit.div(in_token), item = in_token - slice * g.by_unit.d;
+  const bool turns = item < g.turned;
+  const uint32_t ja = turns && !kHalf ? 2 * item : turns ? item : item + t.pairs, jb = kHalf ? item + t.pairs : 2 * item + 1;
+  const uint32_t head0 = slice * kHeads;
+  T a[kHeads], b[kHeads];
+#pragma unroll
+  for (uint32_t h = 0; h < kHeads; ++h) {
+    if (head0 + h >= g.heads) break;
+    const T* from = x.p + int64_t(i) * x.ld + int64_t(head0 + h) * t.head_dim;
+    a[h] = from[ja];
+    if (turns) b[h] = from[jb];
   }
-  const uint32_t ja = kHalf ? item : 2 * item, jb = kHalf ? item + t.pairs : 2 * item + 1;
-  float c, s;
-  angle(double(positions.at(i)) * t.freq[item], t.scale, t.sign, &c, &s);
-  const float a = float(from[ja]), b = float(from[jb]);
-  to[ja] = T(a * c - b * s);
-  to[jb] = T(b * c + a * s);
+  compiler_fence();
+  float c = 1.0f, s = 0.0f;
+  if (turns) angle(double(positions.at(i)) * t.freq[item], t.scale, t.sign, &c, &s);
+#pragma unroll
+  for (uint32_t h = 0; h < kHeads; ++h) {
+    if (head0 + h >= g.heads) break;
+    T* to = out.p + int64_t(i) * out.ld + int64_t(head0 + h) * t.head_dim;
+    if (turns) {
+      const float u = float(a[h]), v = float(b[h]);
+      to[ja] = T(u * c - v * s);
+      to[jb] = T(v * c + u * s);
+    } else {
+      to[ja] = a[h];
+    }
+  }
 }
 
 template <typename T, bool kHalf>
@@ -138,7 +150,7 @@ hipError_t launch_layout(const etc_rotary_args& a, const Turns& t, hipStream_t s
   const uint32_t past = in_place ? 0 : t.head_dim - 2 * t.pairs;
   const uint32_t items = blocks ? t.pairs / kC + (past / kC + 1) / 2 : t.pairs + past;  // lanes of a head
   // sines once for several heads, where that leaves lanes enough
-  const uint32_t each = !blocks ? 1 : int64_t(a.x.rows) * heads * items >= (1 << 20) ? 4 : 1;
+  const uint32_t each = int64_t(a.x.rows) * heads * items >= (1 << 20) ? 4 : 1;
   const uint32_t lanes = (heads + each - 1) / each * items;  // of a token
   const int64_t most = std::max<int64_t>(1, INT32_MAX / lanes);
   for (int64_t at = 0; at < a.x.rows; at += most) {
@@ -147,14 +159,10 @@ hipError_t launch_layout(const etc_rotary_args& a, const Turns& t, hipStream_t s
     const Ids ids{static_cast<const char*>(a.positions.data) + at * (wide ? 8 : 4), wide};
     const uint32_t n = rows * lanes;
     const dim3 wgs((n + kThreads - 1) / kThreads), threads(kThreads);
-    if (blocks) {
-      const Blocks g{n, heads, items, t.pairs / kC, Divisor(lanes), Divisor(items)};
-      const auto kernel = each == 1 ? rotary_block_kernel<T, kHalf, 1> : rotary_block_kernel<T, kHalf, 4>;
-      hipLaunchKernelGGL(kernel, wgs, threads, 0, stream, t, g, cmat<T>(a.x, at), ids, mat<T>(a.out, at));
-    } else {
-      hipLaunchKernelGGL((rotary_pair_kernel<T, kHalf>), wgs, threads, 0, stream, t, n, heads, Divisor(items), Divisor(heads),
-                         cmat<T>(a.x, at), ids, mat<T>(a.out, at));
-    }
+    const Blocks g{n, heads, items, blocks ? t.pairs / kC : t.pairs, Divisor(lanes), Divisor(items)};
+    const auto kernel = blocks ? each == 1 ? rotary_block_kernel<T, kHalf, 1> : rotary_block_kernel<T, kHalf, 4>
+                               : each == 1 ? rotary_pair_kernel<T, kHalf, 1> : rotary_pair_kernel<T, kHalf, 4>;
+    hipLaunchKernelGGL(kernel, wgs, threads, 0, stream, t, g, cmat<T>(a.x, at), ids, mat<T>(a.out, at));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
