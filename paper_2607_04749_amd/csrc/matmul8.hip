@@ -30,7 +30,16 @@ struct Product {
 
   __device__ __forceinline__ float x_scale(uint32_t i) const { return sx ? sx[int64_t(i) * sxld] : 1.0f; }
   __device__ __forceinline__ float w_scale(uint32_t j) const { return sw ? sw[int64_t(j) * swld] : 1.0f; }
+  template <typename T>
+  __device__ __forceinline__ float bias_of(uint64_t j) const {
+    return bias ? float(static_cast<const T*>(bias)[j]) : -0.0f;  // which leaves every number as it is
+  }
 };
+
+// An element of the output from its sum, the same in all kernels to the bit.
+__device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale, float bias) {
+  return __builtin_fmaf(float(sum) * x_scale, w_scale, bias);
+}
 
 // Four neighbouring columns n .. n + 3 of row m, as far as there are any.
 template <typename T>
@@ -40,8 +49,7 @@ __device__ __forceinline__ void store4(const Product& p, uint32_t m, uint64_t n,
 #pragma unroll
   for (uint32_t e = 0; e < 4; ++e) {
     if (e >= width) break;
-    v[e] = float(sums[e]) * x_scale * p.w_scale(uint32_t(n) + e);
-    if (p.bias) v[e] += float(static_cast<const T*>(p.bias)[n + e]);
+    v[e] = scaled(sums[e], x_scale, p.w_scale(uint32_t(n) + e), p.bias_of<T>(n + e));
   }
   T* out = static_cast<T*>(p.out) + int64_t(m) * p.ld + int64_t(n);
   Raw<T, 4, false> raw;
@@ -378,7 +386,7 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
     for (uint32_t e = 0; e < 16; ++e) {
       const uint64_t n = min(n1 + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4, uint64_t(p.n) - 1);
       scale_w[i][e] = p.w_scale(uint32_t(n));
-      bias[i][e] = p.bias ? float(static_cast<const T*>(p.bias)[n]) : 0.0f;
+      bias[i][e] = p.bias_of<T>(n);
     }
   }
   __syncthreads();  // all have read their operands
@@ -392,7 +400,7 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
         float v[4];
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e)
-          v[e] = float(acc[i][j][4 * q + e]) * scale_x * scale_w[i][4 * q + e] + bias[i][4 * q + e];
+          v[e] = scaled(acc[i][j][4 * q + e], scale_x, scale_w[i][4 * q + e], bias[i][4 * q + e]);
         store_block<true>(reinterpret_cast<T*>(part + lane % 32 * kPitch) + i * 32 + q * 8 + lane / 32 * 4, 4, v);
       }
     }
@@ -554,7 +562,7 @@ __global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles 
 #pragma unroll
       for (uint32_t k = 0; k < 4; ++k) {
         const uint32_t column = uint32_t(min(n + b + k, uint64_t(p.n) - 1));
-        v[b + k] = float(sum[k]) * scale_x * p.w_scale(column) + (p.bias ? float(static_cast<const T*>(p.bias)[column]) : 0.0f);
+        v[b + k] = scaled(sum[k], scale_x, p.w_scale(column), p.bias_of<T>(column));
       }
     }
     store_block<false, true>(static_cast<T*>(p.out) + int64_t(m) * p.ld + int64_t(n), block_width<kC>(n, p.n), v);
@@ -610,6 +618,9 @@ hipError_t launch_block(const Product& p, hipStream_t stream) {
     return launch_few<16>(p, wide, direct, stream);
   }
   auto tiles = [&](uint64_t tile) { return ((p.m + tile - 1) / tile) * ((p.n + tile - 1) / tile); };
+  // the larger tiles' kernels have the distances of a tile's rows in 32 bits
+  const bool near = p.xld <= 1 << 24 && p.wld <= 1 << 24;
+  if (!near) return direct ? launch_split<T, true>(p, stream) : launch_split<T, false>(p, stream);
   if (tiles(256) >= kCus) return direct ? launch_tiles<T, 4, 2, true>(p, stream) : launch_tiles<T, 4, 2, false>(p, stream);
   if (tiles(128) >= 2 * kCus) return direct ? launch_tiles<T, 2, 2, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
   if (tiles(128) >= kCus) return direct ? launch_tiles<T, 2, 4, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
@@ -617,7 +628,7 @@ hipError_t launch_block(const Product& p, hipStream_t stream) {
 }
 
 // Blocks of the output that a launch takes: offsets within them, and workgroups, in 32 bits.
-constexpr int64_t kMostRows = 1 << 20, kMostCols = 1 << 20;
+constexpr int64_t kMostRows = 1 << 19, kMostCols = 1 << 20;
 
 template <typename T>
 hipError_t launch_type(const etc_matmul8_args& a, hipStream_t stream) {

@@ -414,7 +414,9 @@ template <typename T, bool kWhole, Kind8 k8>
 hipError_t launch_sum(const etc_norm_grad_args& a, hipStream_t stream) {
   const Shape s = shape_of(uint64_t(a.grad.rows), uint64_t(a.grad.cols), kLaneCols<T>);
   if (!a.dweight.data) return launch_rows<T, kWhole, k8, false>(a, s, stream);
-  if (is_few(s)) {
+  // in place, rows are written while other workgroups would still sum their columns
+  const bool in_place = a.dx.data == a.grad.data || a.dx.data == a.x.data;
+  if (is_few(s) && !in_place) {
     // blocks of a workgroup that sums columns: two where there are few workgroups and many rows
     const uint32_t blocks = blocks_per_row(s.cols, kLaneCols<T>), narrow = s.rows > 512 && blocks <= 512 ? 2 : 4;
     const uint32_t slabs = (blocks + narrow - 1) / narrow;

@@ -22,11 +22,17 @@ struct Turns {
   uint32_t pairs, head_dim;
 };
 
-__device__ __forceinline__ void angle(double turns, float scale, float sign, float* c, float* s) {
-  const float part = float(turns - rint(turns));
+// Products and sums are fused where it is written, so that all kernels round alike.
+__device__ __forceinline__ void angle(double position, double freq, float scale, float sign, float* c, float* s) {
+  const float part = float(__builtin_fma(position, freq, -rint(position * freq)));
   sincospif(2.0f * part, s, c);
   *c *= scale;
   *s *= scale * sign;
+}
+
+__device__ __forceinline__ void turn(float a, float b, float c, float s, float* to_a, float* to_b) {
+  *to_a = __builtin_fmaf(a, c, -(b * s));
+  *to_b = __builtin_fmaf(b, c, a * s);
 }
 
 // A lane has two blocks of 16 bytes, half the pairs' columns apart, of kHeads heads of
@@ -88,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Turns t, Blocks g, Mat
 #pragma unroll
     for (uint32_t e = 0; e < kC; ++e) {
       const uint32_t pair = kHalf ? ja + e : e < kC / 2 ? ja / 2 + e : jb / 2 + e - kC / 2;
-      angle(position * t.freq[min(pair, uint32_t(ETC_ROTARY_PAIRS - 1))], t.scale, t.sign, &c[e], &s[e]);
+      angle(position, t.freq[min(pair, uint32_t(ETC_ROTARY_PAIRS - 1))], t.scale, t.sign, &c[e], &s[e]);
     }
   }
 #pragma unroll
@@ -103,13 +109,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Turns t, Blocks g, Mat
 #pragma unroll
       for (uint32_t e = 0; e < kC; ++e) {
         if (kHalf) {
-          p[e] = u[e] * c[e] - v[e] * s[e];
-          q[e] = v[e] * c[e] + u[e] * s[e];
+          turn(u[e], v[e], c[e], s[e], &p[e], &q[e]);
         } else if (e % 2 == 0) {
-          p[e] = u[e] * c[e / 2] - u[e + 1] * s[e / 2];
-          p[e + 1] = u[e + 1] * c[e / 2] + u[e] * s[e / 2];
-          q[e] = v[e] * c[kC / 2 + e / 2] - v[e + 1] * s[kC / 2 + e / 2];
-          q[e + 1] = v[e + 1] * c[kC / 2 + e / 2] + v[e] * s[kC / 2 + e / 2];
+          turn(u[e], u[e + 1], c[e / 2], s[e / 2], &p[e], &p[e + 1]);
+          turn(v[e], v[e + 1], c[kC / 2 + e / 2], s[kC / 2 + e / 2], &q[e], &q[e + 1]);
         }
       }
       a[h].narrow(p);

@@ -223,11 +223,12 @@ def test_norm_grad_in_place():
     """dx may be grad, x or dsum itself."""
     say("norm_grad in place")
     rng = np.random.default_rng(5)
-    for dtype, cols in (("bf16", 4096), ("f32", 20001), ("bf16", 681)):
-        r = (1 + rng.random(7)).astype(np.float32)
-        (g, gn, _), (x, xn, _), (d, dn, _), (w, wn, _) = (rand(rng, n, cols, dtype) for n in (7, 7, 7, 1))
+    for rows, dtype, cols in ((7, "bf16", 4096), (7, "f32", 20001), (7, "bf16", 681), (1000, "bf16", 2048), (1024, "f32", 681),
+                              (3000, "bf16", 264)):
+        r = (1 + rng.random(rows)).astype(np.float32)
+        (g, gn, _), (x, xn, _), (d, dn, _), (w, wn, _) = (rand(rng, n, cols, dtype) for n in (rows, rows, rows, 1))
         want = block_ref.norm_grad(gn, xn, wn[0], r, dn, np.zeros(cols))
-        ws, _ = workspace(etc.etc_norm_grad_bytes(7, cols))
+        ws, _ = workspace(etc.etc_norm_grad_bytes(rows, cols))
         for k in range(3):
             a = [g.clone(), x.clone(), d.clone()]
             dw = torch.empty(cols, device=DEV)
@@ -363,6 +364,11 @@ PRODUCT = [
     (67, 1280, 8192, "bf16", False, True, (0, 0, 0), 0), (300, 520, 4096, "bf16", True, True, (16, 32, 8), 16),
     (1000, 1000, 1000, "f32", True, True, (0, 0, 0), 0), (513, 257, 2048, "bf16", False, True, (0, 0, 1), 0),
     (2048, 4096, 512, "bf16", True, True, (0, 0, 0), 0), (4100, 2056, 272, "f32", False, True, (0, 0, 0), 0),
+    (200, 100, 0, "bf16", True, True, (0, 0, 0), 0), (300, 40, 8, "bf16", False, True, (0, 0, 0), 0), (2500, 4096, 7, "f32", True, True, (0, 0, 0), 0),
+    (5000, 4096, 9, "bf16", False, True, (0, 0, 0), 0), (2500, 4096, 130, "bf16", True, True, (0, 0, 0), 0),
+    (1500, 4096, 1152, "bf16", True, True, (0, 0, 0), 0), (1500, 4090, 1151, "bf16", True, True, (0, 0, 0), 0),
+    (5001, 4099, 1000, "bf16", True, True, (1, 3, 1), 0), (5001, 4096, 1168, "f32", True, True, (0, 16, 3), 16),
+    (700, 1000, 3001, "f32", True, True, (0, 0, 0), 3), (700, 1000, 127, "f32", True, True, (0, 0, 0), 0),
 ] + [(m, n, k, dtype, n % 2 == 1, (m + n) % 3 > 0, more, shift)
      for m in (1, 2, 7, 15, 16, 17, 31, 33, 64, 65, 127, 129, 200)
      for n, k, dtype, more, shift in ((1, 64, "bf16", (0, 0, 0), 0), (15, 63, "f32", (1, 0, 1), 1), (17, 65, "bf16", (0, 3, 3), 3),
@@ -397,18 +403,55 @@ def test_matmul8_largest_sums(m, n, k):
     assert np.array_equal(out.cpu().numpy(), want[None, :].repeat(m, 0))
 
 
-def test_matmul8_rows_are_alone():
-    """A row has the same bits in a batch of one and of many."""
-    say("matmul8: rows alone")
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("k", (384, 200))
+def test_matmul8_rows_are_alone(k, dtype):
+    """A row has the same bits in a batch of one and of many, whichever kernel has it."""
+    say("matmul8: rows alone", k, dtype)
     rng = np.random.default_rng(9)
-    x, w = operand(ints(rng, 700, 2048), rng.random(700).astype(np.float32)), operand(ints(rng, 1000, 2048), rng.random(1000).astype(np.float32))
-    bias = torch.randn(1000, device=DEV).bfloat16()
-    out = torch.empty(700, 1000, dtype=torch.bfloat16, device=DEV)
-    etc.etc_matmul8(x, w, out, bias=bias)
-    for a, b in ((0, 1), (699, 700), (100, 117), (30, 130), (0, 400)):
-        part = torch.empty(b - a, 1000, dtype=torch.bfloat16, device=DEV)
-        etc.etc_matmul8(etc.Matrix8(x.data[a:b], x.scale[a:b]), w, part, bias=bias)
-        assert torch.equal(part, out[a:b])
+    x, w = (operand(ints(rng, n, k), rng.random(n).astype(np.float32)) for n in (5000, 4096))
+    for bias in (torch.randn(4096, device=DEV).to(DT[dtype]), None):
+        out = torch.empty(5000, 4096, dtype=DT[dtype], device=DEV)
+        etc.etc_matmul8(x, w, out, bias=bias)
+        for a, b in ((0, 1), (4999, 5000), (100, 117), (30, 130), (0, 400), (1000, 2500), (2000, 4500)):
+            part = torch.empty(b - a, 4096, dtype=DT[dtype], device=DEV)
+            etc.etc_matmul8(etc.Matrix8(x.data[a:b], x.scale[a:b]), w, part, bias=bias)
+            assert torch.equal(part.view(torch.int16 if dtype == "bf16" else torch.int32),
+                               out[a:b].view(torch.int16 if dtype == "bf16" else torch.int32)), (a, b)
+
+
+def test_matmul8_rows_far_apart():
+    """Rows of which a tile's 256 lie past 2^32 bytes of each other."""
+    say("matmul8: rows far apart")
+    rng = np.random.default_rng(14)
+    ld, rows = (1 << 24) + 16, 260
+    full = torch.zeros((rows - 1) * ld + 64, dtype=torch.int8, device=DEV)
+    far = torch.as_strided(full, (rows, 64), (ld, 1))
+    x, w = ints(rng, rows, 64), ints(rng, 70000, 64)
+    far.copy_(torch.from_numpy(x).to(DEV))
+    near = operand(w, None)
+    out = torch.empty(rows, 70000, device=DEV)
+    etc.etc_matmul8(etc.Matrix8(far), near, out)
+    want = torch.from_numpy(x).double() @ torch.from_numpy(w).double().t()
+    assert torch.equal(out.double().cpu(), want)
+    out = torch.empty(70000, rows, device=DEV)
+    etc.etc_matmul8(near, etc.Matrix8(far), out)
+    assert torch.equal(out.double().cpu(), want.t())
+
+
+def test_rotary_rows_are_alone():
+    """A token's heads have the same bits in a batch of one and of many."""
+    say("rotary: rows alone")
+    rng = np.random.default_rng(15)
+    pos = torch.from_numpy(rng.integers(0, 1 << 20, 6000)).to(DEV)
+    for dtype in ("bf16", "f32"):
+        for layout, head_dim, dim in (("half", 128, 128), ("interleaved", 128, 128), ("half", 80, 52), ("interleaved", 81, 52)):
+            x, _, _ = rand(rng, 6000, 40 * head_dim, dtype)
+            rot, many, one = etc.Rotary(dim, layout=layout, scale=1.3), torch.empty_like(x), torch.empty_like(x[:1])
+            etc.etc_rotary(x, many, pos, rot, head_dim)
+            for i in (0, 1, 3000, 5999):
+                etc.etc_rotary(x[i:i + 1], one, pos[i:i + 1], rot, head_dim)
+                assert torch.equal(one[0], many[i]), (dtype, layout, head_dim, i)
 
 
 def test_matmul8_scales_that_are_not_finite():
