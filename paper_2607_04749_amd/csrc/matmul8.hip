@@ -417,69 +417,68 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of 64 x 64 where larger ones would leave CUs idle.  Each of the four
+// Tiles of 32 kA x 32 kB where larger ones would leave CUs idle.  Each of the four
 // wavefronts has the whole tile, for one of the four steps of 32 columns in each
-// stage: four matrix instructions to four reads, where a quarter of the tile each had one to two
-// and waited for LDS (300 x 1280 x 8192: 20.1 us).  The wavefronts' sums are added up in LDS at the end.
+// stage: kA kB matrix instructions to kA + kB reads, where a quarter of a tile of 64 x 64 each had one to two
+// and waited for LDS.  The wavefronts' sums are added up in LDS at the end.
 
-template <typename T, bool kDirect>
-__global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles tiles) {
-  constexpr uint32_t kTile = 64, kLoads = 2, kOperand = kTile * kDepth, kCopy = 2 * kOperand;
-  constexpr uint32_t kCopies = kDirect ? 4 : 2, kSets = 4;  // stages in LDS; behind them, in registers (kDirect: none)
-  constexpr uint32_t kPitch = kTile * 4 + 16;
-  __shared__ __attribute__((aligned(1024))) uint8_t buffer[4 * kTile * kPitch];
-  static_assert(kCopies * kCopy <= sizeof buffer, "LDS");
+template <typename T, uint32_t kA, uint32_t kB, bool kDirect>
+__global__ __launch_bounds__(256, kA * kB > 4 ? 1 : 2) void matmul8_split_kernel(Product p, Tiles tiles) {
+  constexpr uint32_t kStageBytes = (kA + kB) * 32 * kDepth, kLoads = kA + kB;  // loads of a wavefront, of 8 rows each
+  // stages in LDS; behind them, in registers (kDirect: none)
+  constexpr uint32_t kCopies = kDirect ? 4 : 2, kSets = kA * kB > 4 ? 2 : 3;
+  constexpr uint32_t kRows = 32 * kA, kCols = 32 * kB, kPitch = kCols * 4 + 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t buffer[std::max(4 * kRows * kPitch, kCopies * kStageBytes)];
   uint32_t tm, tn;
   place_tile(tiles, &tm, &tn);
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint64_t m0 = uint64_t(tm) * kTile, n0 = uint64_t(tn) * kTile;
-  const uint8_t* rows[2][kLoads];
+  const uint64_t m0 = uint64_t(tm) * kRows, n0 = uint64_t(tn) * kCols;
+  const uint8_t* rows[kLoads];  // kA of x, then kB of w
 #pragma unroll
   for (uint32_t i = 0; i < kLoads; ++i) {
-    const uint32_t row = (wave * kLoads + i) * 8 + lane / 8;  // rows past the end repeat the last one
-    rows[0][i] = p.x + int64_t(min(m0 + row, uint64_t(p.m) - 1)) * p.xld;
-    rows[1][i] = p.w + int64_t(min(n0 + row, uint64_t(p.n) - 1)) * p.wld;
+    const uint32_t row = (wave * (i < kA ? kA : kB) + (i < kA ? i : i - kA)) * 8 + lane / 8;  // rows past the end repeat the last one
+    rows[i] = i < kA ? p.x + int64_t(min(m0 + row, uint64_t(p.m) - 1)) * p.xld : p.w + int64_t(min(n0 + row, uint64_t(p.n) - 1)) * p.wld;
   }
   const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
   const uint32_t rest = p.k % kDepth != 0, stages = p.k / kDepth + rest;
-  auto target = [&](uint32_t s, uint32_t o, uint32_t i) { return &buffer[s % kCopies * kCopy + o * kOperand + (wave * kLoads + i) * 1024]; };
-  Raw8<16, false> staged[kSets][2][kLoads];
+  auto target = [&](uint32_t s, uint32_t i) {
+    return &buffer[s % kCopies * kStageBytes + (i < kA ? wave * kA + i : 4 * kA + wave * kB + i - kA) * 1024];
+  };
+  Raw8<16, false> staged[kSets][kLoads];
   auto start = [&](uint32_t s, auto set) {  // a stage of whole columns: those past whole stages come first
     const uint64_t k = uint64_t(s - rest) * kDepth + chunk;
 #pragma unroll
-    for (uint32_t o = 0; o < 2; ++o) {
-#pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) {
-        if constexpr (kDirect) load_direct(rows[o][i] + k, target(s, o, i));
-        else staged[set()][o][i].load(rows[o][i] + k, 16, false);
-      }
+    for (uint32_t i = 0; i < kLoads; ++i) {
+      if constexpr (kDirect) load_direct(rows[i] + k, target(s, i));
+      else staged[set()][i].load(rows[i] + k, 16, false);
     }
   };
   auto place = [&](uint32_t s, auto set) {
 #pragma unroll
-    for (uint32_t o = 0; o < 2; ++o) {
-#pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) place16(target(s, o, i) + lane * 16, staged[set()][o][i]);
-    }
+    for (uint32_t i = 0; i < kLoads; ++i) place16(target(s, i) + lane * 16, staged[set()][i]);
   };
   const uint32_t at = lane % 32 * kDepth + ((wave * 2 + lane / 32) ^ lane % 8) * 16;
-  i32x16 acc[2][2] = {};  // [of w][of x]
-  i32x4 x[2], w[2];
+  i32x16 acc[kB][kA] = {};  // [of w][of x]
+  i32x4 x[kA], w[kB];
   auto read = [&](uint32_t s) {
+    const uint8_t* from = &buffer[s % kCopies * kStageBytes + at];
 #pragma unroll
-    for (uint32_t b = 0; b < 2; ++b) {
-      x[b] = *reinterpret_cast<const i32x4*>(&buffer[s % kCopies * kCopy + at + b * 32 * kDepth]);
-      w[b] = *reinterpret_cast<const i32x4*>(&buffer[s % kCopies * kCopy + kOperand + at + b * 32 * kDepth]);
-    }
+    for (uint32_t b = 0; b < kA; ++b) x[b] = *reinterpret_cast<const i32x4*>(from + b * 32 * kDepth);
+#pragma unroll
+    for (uint32_t b = 0; b < kB; ++b) w[b] = *reinterpret_cast<const i32x4*>(from + (kA + b) * 32 * kDepth);
   };
   using Zero = std::integral_constant<uint32_t, 0>;
   // Multiplies stage s, whose operands are in x and w, and reads stage s + 1 (which register set `next` holds) behind it.
   // kFill: starts a stage, into the copy that has been read or into the set that has been placed.
   auto turn = [&](uint32_t s, auto next, auto fill) {
-    i32x4 u[2] = {x[0], x[1]}, v[2] = {w[0], w[1]};
+    i32x4 u[kA], v[kB];
+#pragma unroll
+    for (uint32_t b = 0; b < kA; ++b) u[b] = x[b];
+#pragma unroll
+    for (uint32_t b = 0; b < kB; ++b) v[b] = w[b];
     constexpr bool kFill = decltype(fill)::value;
     if constexpr (kDirect) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kFill ? (kCopies - 2) * 2 * kLoads : 0) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kFill ? (kCopies - 2) * kLoads : 0) : "memory");
     } else {
       place(s + 1, next);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -488,18 +487,15 @@ __global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles 
     if constexpr (kFill) start(kDirect ? s + kCopies : s + 1 + kSets, next);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kB; ++i) {
 #pragma unroll
-      for (uint32_t j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v[i], u[j], acc[i][j], 0, 0, 0);
+      for (uint32_t j = 0; j < kA; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v[i], u[j], acc[i][j], 0, 0, 0);
     }
   };
   if (stages) {
     if (rest) {
 #pragma unroll
-      for (uint32_t o = 0; o < 2; ++o) {
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) load_tail(staged[0][o][i], rows[o][i], uint64_t(stages - 1) * kDepth + chunk, p.k);
-      }
+      for (uint32_t i = 0; i < kLoads; ++i) load_tail(staged[0][i], rows[i], uint64_t(stages - 1) * kDepth + chunk, p.k);
       if (kDirect) place(0, Zero());
     }
     for_each_below(std::make_integer_sequence<uint32_t, kDirect ? kCopies : kSets>(), [&](auto s) {
@@ -530,25 +526,25 @@ __global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles 
         });
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < kB; ++i) {
 #pragma unroll
-      for (uint32_t j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+      for (uint32_t j = 0; j < kA; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[i], x[j], acc[i][j], 0, 0, 0);
     }
   }
   __syncthreads();  // all have read their operands
 #pragma unroll
-  for (uint32_t i = 0; i < 2; ++i) {
+  for (uint32_t i = 0; i < kB; ++i) {
 #pragma unroll
-    for (uint32_t j = 0; j < 2; ++j) {
+    for (uint32_t j = 0; j < kA; ++j) {
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q)
-        *reinterpret_cast<i32x4*>(buffer + (wave * kTile + j * 32 + lane % 32) * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * 4) =
+        *reinterpret_cast<i32x4*>(buffer + (wave * kRows + j * 32 + lane % 32) * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * 4) =
             i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     }
   }
   __syncthreads();
-  constexpr uint32_t kC = kLaneCols<T>, kAcross = kTile / kC;  // lanes to a row
-  for (uint32_t e = threadIdx.x; e < kTile * kAcross; e += 256) {
+  constexpr uint32_t kC = kLaneCols<T>, kAcross = kCols / kC;  // lanes to a row
+  for (uint32_t e = threadIdx.x; e < kRows * kAcross; e += 256) {
     const uint32_t r = e / kAcross, c = e % kAcross * kC;
     const uint64_t m = m0 + r, n = n0 + c;
     if (m >= p.m || n >= p.n) continue;
@@ -558,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void matmul8_split_kernel(Product p, Tiles 
     for (uint32_t b = 0; b < kC; b += 4) {
       i32x4 sum = {};
 #pragma unroll
-      for (uint32_t f = 0; f < 4; ++f) sum += *reinterpret_cast<const i32x4*>(buffer + (f * kTile + r) * kPitch + (c + b) * 4);
+      for (uint32_t f = 0; f < 4; ++f) sum += *reinterpret_cast<const i32x4*>(buffer + (f * kRows + r) * kPitch + (c + b) * 4);
 #pragma unroll
       for (uint32_t k = 0; k < 4; ++k) {
         const uint32_t column = uint32_t(min(n + b + k, uint64_t(p.n) - 1));
@@ -578,11 +574,12 @@ hipError_t launch_tiles(const Product& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, bool kDirect>
-hipError_t launch_split(const Product& p, hipStream_t stream) {
-  Tiles t{(p.m + 63) / 64, (p.n + 63) / 64, 0};
+template <typename T, uint32_t kA, uint32_t kB>
+hipError_t launch_split(const Product& p, bool direct, hipStream_t stream) {
+  Tiles t{(p.m + 32 * kA - 1) / (32 * kA), (p.n + 32 * kB - 1) / (32 * kB), 0};
   t.count = t.m * t.n;
-  hipLaunchKernelGGL((matmul8_split_kernel<T, kDirect>), dim3(t.count), dim3(256), 0, stream, p, t);
+  const auto kernel = direct ? matmul8_split_kernel<T, kA, kB, true> : matmul8_split_kernel<T, kA, kB, false>;
+  hipLaunchKernelGGL(kernel, dim3(t.count), dim3(256), 0, stream, p, t);
   return hipGetLastError();
 }
 
@@ -600,31 +597,60 @@ hipError_t launch_few(const Product& p, bool wide, bool direct, hipStream_t stre
 }
 
 template <typename T>
+hipError_t launch_few_groups(const Product& p, uint32_t groups, bool direct, hipStream_t stream) {
+  constexpr bool wide = sizeof(T) == 4;
+  if (groups == 1) return launch_few<1>(p, wide, direct, stream);
+  if (groups == 2) return launch_few<2>(p, wide, direct, stream);
+  if (groups == 3) return launch_few<3>(p, wide, direct, stream);
+  if (groups == 4) return launch_few<4>(p, wide, direct, stream);
+  if (groups <= 6) return launch_few<6>(p, wide, direct, stream);
+  if (groups <= 8) return launch_few<8>(p, wide, direct, stream);
+  if (groups <= 10) return launch_few<10>(p, wide, direct, stream);
+  if (groups <= 12) return launch_few<12>(p, wide, direct, stream);
+  return launch_few<16>(p, wide, direct, stream);
+}
+
+// What a CU reads into its LDS, some 32 bytes a clock whichever kernel it is, decides: the
+// kernel is the one whose workgroups together read the fewest rows to a CU, and among
+// equals the one of the smallest tiles.
+template <typename T>
 hipError_t launch_block(const Product& p, hipStream_t stream) {
   const bool direct = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.w) | uintptr_t(p.xld) | uintptr_t(p.wld)) & 15) == 0;
-  constexpr bool wide = sizeof(T) == 4;
-  if (p.m <= 128) {
-    // rows of a workgroup: as many as leave a workgroup to each CU
-    const uint32_t across = (p.n + 15) / 16, split = std::max(1u, std::min((p.m + 7) / 8, kCus / across));
-    const uint32_t groups = ((p.m + 7) / 8 + split - 1) / split;
-    if (groups == 1) return launch_few<1>(p, wide, direct, stream);
-    if (groups == 2) return launch_few<2>(p, wide, direct, stream);
-    if (groups == 3) return launch_few<3>(p, wide, direct, stream);
-    if (groups == 4) return launch_few<4>(p, wide, direct, stream);
-    if (groups <= 6) return launch_few<6>(p, wide, direct, stream);
-    if (groups <= 8) return launch_few<8>(p, wide, direct, stream);
-    if (groups <= 10) return launch_few<10>(p, wide, direct, stream);
-    if (groups <= 12) return launch_few<12>(p, wide, direct, stream);
-    return launch_few<16>(p, wide, direct, stream);
-  }
-  auto tiles = [&](uint64_t tile) { return ((p.m + tile - 1) / tile) * ((p.n + tile - 1) / tile); };
   // the larger tiles' kernels have the distances of a tile's rows in 32 bits
   const bool near = p.xld <= 1 << 24 && p.wld <= 1 << 24;
-  if (!near) return direct ? launch_split<T, true>(p, stream) : launch_split<T, false>(p, stream);
-  if (tiles(256) >= kCus) return direct ? launch_tiles<T, 4, 2, true>(p, stream) : launch_tiles<T, 4, 2, false>(p, stream);
-  if (tiles(128) >= 2 * kCus) return direct ? launch_tiles<T, 2, 2, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
-  if (tiles(128) >= kCus) return direct ? launch_tiles<T, 2, 4, true>(p, stream) : launch_tiles<T, 2, 2, false>(p, stream);
-  return direct ? launch_split<T, true>(p, stream) : launch_split<T, false>(p, stream);
+  auto count = [&](uint64_t down, uint64_t across) { return (p.m + down - 1) / down * ((p.n + across - 1) / across); };
+  auto rows = [&](uint64_t down, uint64_t across) { return (count(down, across) + kCus - 1) / kCus * (down + across); };
+  // few rows to a workgroup: as many as leave one to each CU
+  const uint32_t eighths = (p.m + 7) / 8, split = std::max(1u, std::min(eighths, kCus / ((p.n + 15) / 16)));
+  const uint32_t groups = (eighths + split - 1) / split;
+  enum Which { kFew, k32x64, k64x64, k96x64, k128x64, k96x96, k128x128, k256x256 } which = kFew;
+  uint64_t best = groups <= 16 ? rows(8 * groups, 16) : UINT64_MAX;
+  auto offer = [&](Which kernel, uint64_t down, uint64_t across) {
+    const uint64_t r = rows(down, across);
+    if (r < best) best = r, which = kernel;
+  };
+  offer(k32x64, 32, 64);
+  offer(k64x64, 64, 64);
+  offer(k96x64, 96, 64);
+  offer(k128x64, 128, 64);
+  offer(k96x96, 96, 96);
+  if (near) {
+    offer(k128x128, 128, 128);
+    offer(k256x256, 256, 256);
+  }
+  switch (which) {
+    case kFew: return launch_few_groups<T>(p, groups, direct, stream);
+    case k32x64: return launch_split<T, 1, 2>(p, direct, stream);
+    case k64x64: return launch_split<T, 2, 2>(p, direct, stream);
+    case k96x64: return launch_split<T, 3, 2>(p, direct, stream);
+    case k128x64: return launch_split<T, 4, 2>(p, direct, stream);
+    case k96x96: return launch_split<T, 3, 3>(p, direct, stream);
+    case k128x128:
+      if (!direct) return launch_tiles<T, 2, 2, false>(p, stream);
+      return count(128, 128) <= kCus ? launch_tiles<T, 2, 4, true>(p, stream) : launch_tiles<T, 2, 2, true>(p, stream);
+    case k256x256: return direct ? launch_tiles<T, 4, 2, true>(p, stream) : launch_tiles<T, 4, 2, false>(p, stream);
+  }
+  return hipErrorInvalidValue;
 }
 
 // Blocks of the output that a launch takes: offsets within them, and workgroups, in 32 bits.
