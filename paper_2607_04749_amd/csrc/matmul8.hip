@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
 // and waited for LDS.  The wavefronts' sums are added up in LDS at the end.
 
 template <typename T, uint32_t kA, uint32_t kB, bool kDirect>
-__global__ __launch_bounds__(256, kA * kB > 4 ? 1 : 2) void matmul8_split_kernel(Product p, Tiles tiles) {
+__global__ __launch_bounds__(256, kDirect && kA * kB <= 4 ? 2 : 1) void matmul8_split_kernel(Product p, Tiles tiles) {
   constexpr uint32_t kStageBytes = (kA + kB) * 32 * kDepth, kLoads = kA + kB;  // loads of a wavefront, of 8 rows each
   // stages in LDS; behind them, in registers (kDirect: none)
   constexpr uint32_t kCopies = kDirect ? 4 : 2, kSets = kA * kB > 4 ? 2 : 3;
