@@ -58,13 +58,17 @@ __device__ __forceinline__ void store4(const Product& p, uint32_t m, uint64_t n,
 }
 
 // Operands stand in LDS as rows of 128 columns, whose 8 chunks of 16 bytes are
-// permuted: row r has chunk c at place c ^ (r % 8), so that reads of one chunk of 8
-// rows touch all banks.  They come straight from memory (`direct`, 16 bytes a lane
+// permuted: row r has chunk c at place c ^ (r / 2 % 8), so that reads of one chunk of 16
+// rows touch all 64 banks once.  They come straight from memory (`direct`, 16 bytes a lane
 // at multiples of 16, 8 rows to an instruction, whose lanes take the chunks in the order
 // of their places), or by way of registers.  Neighbouring lanes have neighbouring
 // chunks: fragments of matrix instructions, whose neighbours are rows, took four times as long to load.
 constexpr uint32_t kDepth = 128;
 constexpr uint32_t kCus = 256;
+
+// The column in its row of the chunk that lane `lane` of the load of rows 8 g .. 8 g + 7 fills; the other
+// parity of g has it flipped by 64.
+__device__ __forceinline__ uint32_t chunk_of(uint32_t lane, uint32_t g) { return (lane % 8 ^ (lane / 16 + g % 2 * 4)) * 16; }
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
@@ -109,7 +113,7 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
   if (n0 >= p.n) return;
   uint8_t* slots = memory + wave * kSlots * kStage<kG>;
   // rows past the end repeat the last one; what comes of them is not stored
-  const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+  const uint32_t chunks[2] = {chunk_of(lane, 0), chunk_of(lane, 1)};  // of w's and x's loads alike: both begin with an even one
   const uint8_t* rows[kLoads];
 #pragma unroll
   for (uint32_t i = 0; i < kLoads; ++i)
@@ -119,19 +123,19 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
   // the columns past whole stages are the last wavefront's, loaded first and multiplied last
   const bool rest = wave == waves - 1 && p.k % kDepth;
   Raw8<16, false> tail[kLoads];
-  const uint32_t tail_width = block_width<16>(uint64_t(whole) * kDepth + chunk, p.k);
+  auto tail_width = [&](uint32_t i) { return block_width<16>(uint64_t(whole) * kDepth + chunks[i % 2], p.k); };
   if (rest) {
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
       tail[i].zero();
-      if (tail_width) tail[i].load(rows[i] + uint64_t(whole) * kDepth + chunk, tail_width, p.k < 16);
+      if (tail_width(i)) tail[i].load(rows[i] + uint64_t(whole) * kDepth + chunks[i % 2], tail_width(i), p.k < 16);
     }
     compiler_fence();
   }
   const uint32_t from = uint32_t(uint64_t(whole) * wave / waves), to = uint32_t(uint64_t(whole) * (wave + 1) / waves);
 
   i32x4 acc[kM] = {};
-  const uint32_t at = lane % 16 * kDepth + (lane / 16 ^ lane % 8) * 16;
+  const uint32_t at = lane % 16 * kDepth + (lane / 16 ^ lane / 2 % 8) * 16;
   auto multiply = [&](const uint8_t* slot) {
 #pragma unroll
     for (uint32_t step = 0; step < 2; ++step) {
@@ -139,7 +143,7 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
 #pragma unroll
       for (uint32_t t = 0; t < kM; ++t) {
         // of a last group of 8 rows, lanes 8 .. 15 read the same again
-        const uint32_t row = kG % 2 && t == kM - 1 ? at & ~(8 * kDepth) : at;
+        const uint32_t row = kG % 2 && t == kM - 1 ? (at & ~(8 * kDepth)) ^ (at & 8 * kDepth) / (8 * kDepth) * 64 : at;
         const i32x4 x = *reinterpret_cast<const i32x4*>(slot + 2048 + t * 2048 + (row ^ step * 64));
         acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc[t], 0, 0, 0);
       }
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
   if constexpr (kDirect) {
     auto start = [&](uint32_t s) {
 #pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) load_direct(rows[i] + uint64_t(s) * kDepth + chunk, slots + s % kSlots * kStage<kG> + i * 1024);
+      for (uint32_t i = 0; i < kLoads; ++i) load_direct(rows[i] + uint64_t(s) * kDepth + chunks[i % 2], slots + s % kSlots * kStage<kG> + i * 1024);
     };
     const uint32_t first = min(from + kSlots, to);
     for (uint32_t s = from; s < first; ++s) start(s);
@@ -167,7 +171,7 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
       for (uint32_t b = 0; b < kSlots; ++b) {
         if (s0 + b >= to) break;
 #pragma unroll
-        for (uint32_t i = 0; i < kLoads; ++i) r[b][i].load(rows[i] + uint64_t(s0 + b) * kDepth + chunk, 16, false);
+        for (uint32_t i = 0; i < kLoads; ++i) r[b][i].load(rows[i] + uint64_t(s0 + b) * kDepth + chunks[i % 2], 16, false);
       }
       compiler_fence();
 #pragma unroll
@@ -182,7 +186,7 @@ __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product
   if (rest) {
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
-      tail[i].shift(tail_width);
+      tail[i].shift(tail_width(i));
       place16(slots + i * 1024 + lane * 16, tail[i]);
     }
     multiply(slots);
@@ -234,9 +238,9 @@ __device__ __forceinline__ void place_tile(const Tiles& t, uint32_t* tm, uint32_
 }
 
 template <typename T, uint32_t kF, uint32_t kCopies, bool kDirect>
-__global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
+__global__ __launch_bounds__(256, kF == 4 || kCopies == 4 ? 1 : 2) void matmul8_tile_kernel(Product p, Tiles tiles) {
   constexpr uint32_t kTile = 64 * kF;
-  constexpr uint32_t kLoads = kTile / 32;  // of a wavefront, of 8 rows each, for one operand
+  constexpr uint32_t kLoads = kTile / 32;  // of a wavefront, of 8 rows each, for one operand; even, so that load i's parity is its rows'
   constexpr uint32_t kOperand = kTile * kDepth, kCopy = 2 * kOperand;
   __shared__ __attribute__((aligned(1024))) uint8_t buffer[kCopies * kCopy];  // of x's and w's rows
   uint32_t tm, tn;
@@ -244,13 +248,13 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint64_t m0 = uint64_t(tm) * kTile, n0 = uint64_t(tn) * kTile;
   const uint8_t* base[2] = {p.x + int64_t(m0) * p.xld, p.w + int64_t(n0) * p.wld};
-  const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
   uint32_t offset[2][kLoads];
+  const uint32_t chunks[2] = {chunk_of(lane, 0), chunk_of(lane, 1)};
 #pragma unroll
-  for (uint32_t i = 0; i < kLoads; ++i) {
-    const uint32_t row = (wave * kLoads + i) * 8 + lane / 8;  // rows past the end repeat the last one
-    offset[0][i] = uint32_t(min(uint64_t(row), p.m - 1 - m0)) * uint32_t(p.xld) + chunk;
-    offset[1][i] = uint32_t(min(uint64_t(row), p.n - 1 - n0)) * uint32_t(p.wld) + chunk;
+  for (uint32_t i = 0; i < kLoads; ++i) {  // rows past the end repeat the last one
+    const uint64_t row = (wave * kLoads + i) * 8 + lane / 8;
+    offset[0][i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.xld) + chunks[i % 2];
+    offset[1][i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.wld) + chunks[i % 2];
   }
   constexpr uint32_t kSets = kDirect || kF == 4 ? 1 : 2;
   constexpr uint32_t kFar = kDirect ? kCopies - 1 : kSets;  // stages between one that starts and the one that is multiplied
@@ -283,7 +287,7 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
   const uint32_t left[2] = {wave % 2 * (kTile / 2), wave / 2 * (kTile / 2)};  // the wavefront's rows of x and of w
   uint32_t place0[2];  // of a lane's operand in the first step; in step s, s * 32 is added to its chunk's place
 #pragma unroll
-  for (uint32_t o = 0; o < 2; ++o) place0[o] = o * kOperand + (left[o] + lane % 32) * kDepth + (lane / 32 ^ lane % 8) * 16;
+  for (uint32_t o = 0; o < 2; ++o) place0[o] = o * kOperand + (left[o] + lane % 32) * kDepth + (lane / 32 ^ lane / 2 % 8) * 16;
   auto read = [&](uint32_t c, uint32_t step, uint32_t o, uint32_t b) {
     return *reinterpret_cast<const i32x4*>(&buffer[c * kCopy + (place0[o] ^ step * 32) + b * 32 * kDepth]);
   };
@@ -332,7 +336,7 @@ __global__ __launch_bounds__(256, kF * kF * kCopies > 8 ? 1 : 2) void matmul8_ti
       for (uint32_t o = 0; o < 2; ++o) {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i)
-          load_tail(staged[0][o][i], base[o] + offset[o][i] - chunk, uint64_t(stages - 1) * kDepth + chunk, p.k);
+          load_tail(staged[0][o][i], base[o] + offset[o][i] - chunks[i % 2], uint64_t(stages - 1) * kDepth + chunks[i % 2], p.k);
       }
       if (kDirect) place(0, Zero());
     }
@@ -439,25 +443,27 @@ __global__ __launch_bounds__(256, kDirect && kA * kB <= 4 ? 2 : 1) void matmul8_
     const uint32_t row = (wave * (i < kA ? kA : kB) + (i < kA ? i : i - kA)) * 8 + lane / 8;  // rows past the end repeat the last one
     rows[i] = i < kA ? p.x + int64_t(min(m0 + row, uint64_t(p.m) - 1)) * p.xld : p.w + int64_t(min(n0 + row, uint64_t(p.n) - 1)) * p.wld;
   }
-  const uint32_t chunk = (lane % 8 ^ lane / 8) * 16;
+  // of loads of an even group of 8 rows and of an odd one
+  const uint32_t chunks[2] = {chunk_of(lane, 0), chunk_of(lane, 1)};
+  auto chunk = [&](uint32_t i) { return chunks[(i < kA ? wave * kA + i : wave * kB + i - kA) % 2]; };
   const uint32_t rest = p.k % kDepth != 0, stages = p.k / kDepth + rest;
   auto target = [&](uint32_t s, uint32_t i) {
     return &buffer[s % kCopies * kStageBytes + (i < kA ? wave * kA + i : 4 * kA + wave * kB + i - kA) * 1024];
   };
   Raw8<16, false> staged[kSets][kLoads];
   auto start = [&](uint32_t s, auto set) {  // a stage of whole columns: those past whole stages come first
-    const uint64_t k = uint64_t(s - rest) * kDepth + chunk;
+    const uint64_t k = uint64_t(s - rest) * kDepth;
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) {
-      if constexpr (kDirect) load_direct(rows[i] + k, target(s, i));
-      else staged[set()][i].load(rows[i] + k, 16, false);
+      if constexpr (kDirect) load_direct(rows[i] + k + chunk(i), target(s, i));
+      else staged[set()][i].load(rows[i] + k + chunk(i), 16, false);
     }
   };
   auto place = [&](uint32_t s, auto set) {
 #pragma unroll
     for (uint32_t i = 0; i < kLoads; ++i) place16(target(s, i) + lane * 16, staged[set()][i]);
   };
-  const uint32_t at = lane % 32 * kDepth + ((wave * 2 + lane / 32) ^ lane % 8) * 16;
+  const uint32_t at = lane % 32 * kDepth + ((wave * 2 + lane / 32) ^ lane / 2 % 8) * 16;
   i32x16 acc[kB][kA] = {};  // [of w][of x]
   i32x4 x[kA], w[kB];
   auto read = [&](uint32_t s) {
@@ -495,7 +501,7 @@ __global__ __launch_bounds__(256, kDirect && kA * kB <= 4 ? 2 : 1) void matmul8_
   if (stages) {
     if (rest) {
 #pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) load_tail(staged[0][i], rows[i], uint64_t(stages - 1) * kDepth + chunk, p.k);
+      for (uint32_t i = 0; i < kLoads; ++i) load_tail(staged[0][i], rows[i], uint64_t(stages - 1) * kDepth + chunk(i), p.k);
       if (kDirect) place(0, Zero());
     }
     for_each_below(std::make_integer_sequence<uint32_t, kDirect ? kCopies : kSets>(), [&](auto s) {
@@ -605,9 +611,7 @@ hipError_t launch_few_groups(const Product& p, uint32_t groups, bool direct, hip
   if (groups == 4) return launch_few<4>(p, wide, direct, stream);
   if (groups <= 6) return launch_few<6>(p, wide, direct, stream);
   if (groups <= 8) return launch_few<8>(p, wide, direct, stream);
-  if (groups <= 10) return launch_few<10>(p, wide, direct, stream);
-  if (groups <= 12) return launch_few<12>(p, wide, direct, stream);
-  return launch_few<16>(p, wide, direct, stream);
+  return launch_few<10>(p, wide, direct, stream);
 }
 
 // What a CU reads into its LDS, some 32 bytes a clock whichever kernel it is, decides: the
@@ -624,7 +628,7 @@ hipError_t launch_block(const Product& p, hipStream_t stream) {
   const uint32_t eighths = (p.m + 7) / 8, split = std::max(1u, std::min(eighths, kCus / ((p.n + 15) / 16)));
   const uint32_t groups = (eighths + split - 1) / split;
   enum Which { kFew, k32x64, k64x64, k96x64, k128x64, k96x96, k128x128, k256x256 } which = kFew;
-  uint64_t best = groups <= 16 ? rows(8 * groups, 16) : UINT64_MAX;
+  uint64_t best = groups <= 10 ? rows(8 * groups, 16) : UINT64_MAX;
   auto offer = [&](Which kernel, uint64_t down, uint64_t across) {
     const uint64_t r = rows(down, across);
     if (r < best) best = r, which = kernel;

@@ -391,6 +391,29 @@ def test_matmul8(case):
     assert untouched(full, out)
 
 
+@pytest.mark.parametrize("m,n", [(m, 2057) for m in (5, 16, 21, 30, 40, 44, 57, 63, 72, 75)] + [(2053, 1), (1640, 270)] + [
+    (9, 12295), (33, 8200), (65, 8200), (97, 8200), (33, 16390), (193, 8200), (193, 16390), (257, 21772)])
+def test_matmul8_sizes_of_every_tile(m, n):
+    """Rows and columns that lead to each of the kernels' tiles, with less than a stage of columns and several, whole and not."""
+    say("matmul8: tiles", m, n)
+    g = torch.Generator(device=DEV).manual_seed(m * n)
+    for k in (100, 128, 640, 952, 1280):
+        for odd in (0, 1):
+            x, w = (torch.randint(-128, 128, (r, k + 16 * odd + odd), dtype=torch.int8, device=DEV, generator=g)[:, odd:k + odd] for r in (m, n))
+            sx, sw = (torch.rand(r, device=DEV, generator=g) + 0.5 for r in (m, n))
+            # exact: every sum lies far below 2^53
+            want = (x.double() @ w.double().T) * sx.double()[:, None] * sw.double()[None, :]
+            for dtype in ("bf16", "f32"):
+                say(m, n, k, odd, dtype)
+                out = torch.full((m + 1, n), 7, dtype=DT[dtype], device=DEV)
+                etc.etc_matmul8(etc.Matrix8(x, sx), etc.Matrix8(w, sw), out[:m])
+                # two products in 32 bits (the sum is below 2^24, so exact), then the output's own rounding
+                half = torch.finfo(DT[dtype]).eps / 2
+                bound = want.abs() * ((1 + half) * (1 + 2.0**-24) ** 2 - 1)
+                assert bool(((out[:m].double() - want).abs() <= bound * 1.001).all()), (k, odd, dtype)
+                assert bool((out[m] == 7).all())
+
+
 @pytest.mark.parametrize("m,n,k", ((5, 40, 131071), (130, 70, 131071), (300, 300, 40000)))
 def test_matmul8_largest_sums(m, n, k):
     """All operands -128 or 127: sums at the ends of 32 bits, exactly."""
