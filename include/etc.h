@@ -660,7 +660,7 @@ ETC_API int etc_norm(const etc_norm_args* args, void* stream);
  * that reaches the sum past the norm.  x is given as a matrix of grad's type,
  * or, with x.data NULL, as x8: as etc_store8 kept it.  grad, weight, dsum and dx are
  * of one type; dweight (ETC_DTYPE_F32, one row) may be absent.  dx may be grad,
- * x or dsum itself.  workspace: etc_norm_grad_workspace's bytes; only read or
+ * x or dsum itself (same data and ld).  workspace: etc_norm_grad_workspace's bytes; only read or
  * written with dweight, and may be NULL without. */
 typedef struct {
   etc_matrix grad, x;
@@ -736,9 +736,10 @@ ETC_API int etc_rotary_init(etc_rotary_desc* out, int32_t dim, int32_t layout, d
  * of a row, cols / head_dim heads) and pair (a, b),
  *   a' = scale (a cos - b sin),  b' = scale (b cos + a sin),
  * or, with `backward`, the gradient: sin negated.  Columns past the pairs are
- * copied.  Row i turns by positions[i], any whole number; angles are worked out
- * in 64 bits.  x and out are of one type and out may be x itself, so that the query and key
- * heads of a projection's output are turned where they are. */
+ * copied.  Row i turns by positions[i], of a magnitude below 2^53.  Whole turns
+ * are dropped in 64 bits: an angle of t turns is off by 2^-26 + t 2^-52 of a turn at
+ * most.  x and out are of one type and out may be x itself (same data and ld), so
+ * that the query and key heads of a projection's output are turned where they are. */
 typedef struct {
   etc_matrix x, out;
   etc_ids positions;

@@ -42,6 +42,11 @@ int check_like8(const etc_matrix8& m, const char* what, Use use, const etc_matri
   return ETC_OK;
 }
 
+// Whether `out` is `in` with other distances between its rows: rows would be written over others not read yet.
+bool crosses(const etc_matrix& out, const etc_matrix& in) {
+  return out.data && out.data == in.data && in.rows > 1 && in.cols && out.ld != in.ld;
+}
+
 // fp32 numbers, `n` of them (none: no pointer is needed)
 int check_numbers(const void* p, const char* what, int64_t n, bool needed) {
   if (n == 0 || (!p && !needed)) return ETC_OK;
@@ -72,6 +77,8 @@ int etc_norm(const etc_norm_args* a, void* stream) {
   if (a->x.rows == 0 || a->x.cols == 0) return ETC_OK;
   if (!a->out.data && !a->out8.data) return fail(ETC_ERR_INVALID_ARG, "out or out8 is needed");
   if (a->sum.data && a->sum.data == a->out.data) return fail(ETC_ERR_INVALID_ARG, "sum and out are the same");
+  if (crosses(a->sum, a->x) || crosses(a->sum, a->residual) || crosses(a->out, a->x) || crosses(a->out, a->residual))
+    return fail(ETC_ERR_INVALID_ARG, "sum and out may be x or residual itself, with its ld");
   return launched(etc::launch_norm(*a, static_cast<hipStream_t>(stream)), "norm");
 }
 
@@ -93,6 +100,8 @@ int etc_norm_grad(const etc_norm_grad_args* a, void* stream) {
   if (!a->x8.data && (rc = check_like(a->x, "x", kIn, a->grad))) return rc;
   if (a->dsum.data && (rc = check_like(a->dsum, "dsum", kIn, a->grad))) return rc;
   if ((rc = check_numbers(a->rstd, "rstd", a->grad.rows, a->grad.cols != 0))) return rc;
+  if (crosses(a->dx, a->grad) || crosses(a->dx, a->x) || crosses(a->dx, a->dsum))
+    return fail(ETC_ERR_INVALID_ARG, "dx may be grad, x or dsum itself, with its ld");
   if (a->reserved != 0) return fail(ETC_ERR_INVALID_ARG, "reserved must be 0");
   if (a->dweight.data) {
     if ((rc = check_row(a->dweight, "dweight", kOut, a->grad.cols, ETC_DTYPE_F32))) return rc;
@@ -192,8 +201,7 @@ int etc_rotary(const etc_rotary_args* a, void* stream) {
   if (a->head_dim < 2 * d.pairs) return fail(ETC_ERR_INVALID_ARG, "head_dim is below the columns that turn");
   if (a->x.cols % a->head_dim != 0) return fail(ETC_ERR_INVALID_ARG, "x's columns must be whole heads");
   if (a->x.rows == 0 || a->x.cols == 0) return ETC_OK;
-  if (a->x.data == a->out.data && a->x.rows > 1 && a->x.ld != a->out.ld)
-    return fail(ETC_ERR_INVALID_ARG, "out may be x itself, with its ld");
+  if (crosses(a->out, a->x)) return fail(ETC_ERR_INVALID_ARG, "out may be x itself, with its ld");
   return launched(etc::launch_rotary(*a, static_cast<hipStream_t>(stream)), "rotary");
 }
 

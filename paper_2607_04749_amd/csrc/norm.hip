@@ -178,10 +178,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_long_kernel(NormIn in, M
 template <typename T, bool kWhole, Kind8 k8>
 hipError_t launch(const etc_norm_args& a, hipStream_t stream) {
   const uint32_t blocks = blocks_per_row(a.x.cols, kLaneCols<T>);
-#ifndef PB
-#define PB 2
-#endif
-  uint32_t per = blocks <= 64 ? 1 : blocks <= PB * 64 * kMostWaves ? PB : kMostBlocks;
+  const uint32_t per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
   const uint32_t waves = std::min((blocks + 64 * per - 1) / (64 * per), kMostWaves);
   const auto kernel = blocks > waves * 64 * per || a.x.cols < kLaneCols<T> ? norm_long_kernel<T, kWhole, k8>
                       : per == 1                ? norm_kernel<T, 1, kWhole, k8>

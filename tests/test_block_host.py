@@ -114,6 +114,9 @@ REFUSED = [
     (lambda: norm(out=NONE), INVALID), (lambda: norm(out=NONE, out8=mat8(3, 15)), INVALID),
     (lambda: norm(out8=mat8(3, 16, group=32)), INVALID), (lambda: norm(out8=mat8(3, 16, dtype=0)), INVALID),
     (lambda: norm(out8=mat8(3, 16, scale=0)), INVALID), (lambda: norm(out8=mat8(3, 16, scale=PTR + 2)), ALIGN),
+    (lambda: norm(sum=mat(3, 16, ld=24)), INVALID), (lambda: norm(out=mat(3, 16, ld=24)), INVALID),
+    (lambda: norm(residual=mat(3, 16, ptr=4 * PTR), sum=mat(3, 16, ptr=4 * PTR, ld=24)), INVALID),
+    (lambda: norm_grad(dx=mat(3, 16, ptr=4 * PTR, ld=24), dsum=mat(3, 16, ptr=4 * PTR)), INVALID),
     (lambda: norm(out8=mat8(3, 16, ld=15)), INVALID), (lambda: norm(out8=mat8(3, 16, sld=0)), INVALID),
     (lambda: norm(rstd=PTR + 1), ALIGN), (lambda: norm(eps=0.0), INVALID), (lambda: norm(eps=-1.0), INVALID),
     (lambda: norm(eps=NAN), INVALID), (lambda: norm(eps=INF), INVALID), (lambda: norm(eps=1e39), INVALID),
