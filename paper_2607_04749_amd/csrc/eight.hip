@@ -89,13 +89,16 @@ __device__ __forceinline__ uint32_t row_top(uint32_t top) {
   return top;
 }
 
-// One scale a row: a workgroup has a row, a lane kB blocks of it.
-template <typename T, uint32_t kB, bool kWhole, Kind8 k8>
-__global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t cols, Mat<const T> x, const float* col_scale,
+// One scale a row: a workgroup has a row, a lane kB blocks of it.  kShared: rows of half a wavefront or less, as
+// many to a workgroup as it has runs of `lanes` lanes for (FIGURES).
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kShared>
+__global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t rows, uint32_t cols, uint32_t lanes, Mat<const T> x, const float* col_scale,
                                                                      Mat8 out) {
   constexpr uint32_t kC = kLaneCols<T>;
-  const int64_t i = blockIdx.x;
-  auto span = [&](uint32_t b) { return Span<kC, kWhole>(uint64_t(b * blockDim.x + threadIdx.x) * kC, cols); };
+  const uint32_t lane = kShared ? threadIdx.x % lanes : threadIdx.x;
+  const int64_t i = kShared ? blockIdx.x * (kSharedThreads / lanes) + threadIdx.x / lanes : blockIdx.x;
+  if (kShared && i >= rows) return;
+  auto span = [&](uint32_t b) { return Span<kC, kWhole>(uint64_t(b * blockDim.x + lane) * kC, cols); };
   Raw<T, kC, true> raw[kB];
   Raw<float, kC, true> factors[kB];
 #pragma unroll
@@ -116,7 +119,9 @@ __global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t co
     top = max(top, block_top(v[b]));
   }
   float scale, factor;
-  scale_of<k8>(row_top(top), &scale, &factor);
+  if constexpr (kShared) top = lanes_max(top, lanes);
+  else top = row_top(top);
+  scale_of<k8>(top, &scale, &factor);
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
     const auto p = span(b);
@@ -125,12 +130,12 @@ __global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t co
     q.template narrow<k8>(v[b], factor);
     q.template store<true>(out.p + i * out.ld + p.at, kC);
   }
-  if (threadIdx.x == 0) out.scale[i * out.sld] = scale;
+  if (lane == 0) out.scale[i * out.sld] = scale;
 }
 
 // Rows that no workgroup's registers hold, or of less than a block: read twice, the second time from the caches.
 template <typename T, bool kWhole, Kind8 k8>
-__global__ __launch_bounds__(kMostWaves * 64) void store8_long_kernel(uint32_t cols, Mat<const T> x, const float* col_scale,
+__global__ __launch_bounds__(kMostWaves * 64) void store8_long_kernel(uint32_t, uint32_t cols, uint32_t, Mat<const T> x, const float* col_scale,
                                                                       Mat8 out) {
   constexpr uint32_t kC = kLaneCols<T>;
   const int64_t i = blockIdx.x;
@@ -207,12 +212,16 @@ hipError_t launch_store(const etc_store8_args& a, hipStream_t stream) {
   const uint32_t blocks = blocks_per_row(a.x.cols, kC);
   const uint32_t per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
   const uint32_t waves = std::min((blocks + 64 * per - 1) / (64 * per), kMostWaves);
-  const auto kernel = blocks > waves * 64 * per || a.x.cols < kC ? store8_long_kernel<T, kWhole, k8>
-                      : per == 1                ? store8_row_kernel<T, 1, kWhole, k8>
-                      : per == 2                ? store8_row_kernel<T, 2, kWhole, k8>
-                                                : store8_row_kernel<T, kMostBlocks, kWhole, k8>;
-  return for_row_groups(a.x.rows, waves * 64, [&](int64_t first, uint32_t rows) -> hipError_t {
-    hipLaunchKernelGGL(kernel, dim3(rows), dim3(waves * 64), 0, stream, uint32_t(a.x.cols), cmat<T>(a.x, first), a.col_scale,
+  const uint32_t lanes = lanes_of_row(blocks);
+  const bool longer = blocks > waves * 64 * per || a.x.cols < kC, shared = !longer && lanes <= 32;
+  const auto kernel = longer     ? store8_long_kernel<T, kWhole, k8>
+                      : shared   ? store8_row_kernel<T, 1, kWhole, k8, true>
+                      : per == 1 ? store8_row_kernel<T, 1, kWhole, k8, false>
+                      : per == 2 ? store8_row_kernel<T, 2, kWhole, k8, false>
+                                 : store8_row_kernel<T, kMostBlocks, kWhole, k8, false>;
+  const uint32_t threads = shared ? kSharedThreads : waves * 64, at_once = shared ? kSharedThreads / lanes : 1;
+  return for_row_groups(a.x.rows, threads, [&](int64_t first, uint32_t rows) -> hipError_t {
+    hipLaunchKernelGGL(kernel, dim3((rows + at_once - 1) / at_once), dim3(threads), 0, stream, rows, uint32_t(a.x.cols), lanes, cmat<T>(a.x, first), a.col_scale,
                        mat8(a.out, first));
     return hipGetLastError();
   });

@@ -189,6 +189,11 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (uint32_t d = 1; d < 64; d *= 2) v += __shfl_xor(v, int(d));
   return v;
 }
+// over runs of `lanes` (a power of two) neighbouring lanes
+__device__ __forceinline__ float lanes_sum(float v, uint32_t lanes) {
+  for (uint32_t d = 1; d < lanes; d *= 2) v += __shfl_xor(v, int(d));
+  return v;
+}
 // the largest over runs of `lanes` (a power of two) neighbouring lanes
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t lanes) {
   for (uint32_t d = 1; d < lanes; d *= 2) {
@@ -197,6 +202,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t lanes) {
   }
   return v;
 }
+
+// Rows of at most half a wavefront's blocks share wavefronts: the lanes of a row, or 64.
+inline uint32_t lanes_of_row(uint32_t blocks) {
+  uint32_t lanes = 1;
+  while (lanes < blocks && lanes < 64) lanes *= 2;
+  return lanes;
+}
+constexpr uint32_t kSharedThreads = 256;  // of a workgroup whose wavefronts have several rows each
 
 // Calls launch(first row, rows) for runs of rows whose workgroups of `threads`, one a row, have fewer than
 // 2^32 lanes, until one fails.

@@ -22,7 +22,7 @@ constexpr uint32_t kMostWaves = 16;
 constexpr uint32_t kMostBlocks = 4;  // blocks of a lane's row in registers
 
 struct NormIn {
-  uint32_t cols;
+  uint32_t rows, cols, lanes;  // lanes of a row (kShared)
   float eps, per_col;  // 1 / cols
 };
 
@@ -57,14 +57,17 @@ __device__ __forceinline__ void row_scale(uint32_t largest, float r, float* scal
   *factor = *factor == 0.0f ? 0.0f : *factor * r;  // r may be NaN where the scale is
 }
 
-// A workgroup has a row, a lane kB blocks of it, one workgroup's width apart.
-template <typename T, uint32_t kB, bool kWhole, Kind8 k8>
+// A workgroup has a row, a lane kB blocks of it, one workgroup's width apart.  kShared: rows of half a wavefront or less, as
+// many to a workgroup as it has lanes for (FIGURES).
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kShared>
 __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<const T> x, Mat<const T> residual,
                                                                const T* weight, Mat<T> sum, Mat<T> out, Mat8 out8,
                                                                float* rstd) {
   constexpr uint32_t kC = kLaneCols<T>;
-  const int64_t i = blockIdx.x;
-  auto span = [&](uint32_t b) { return Span<kC, kWhole>(uint64_t(b * blockDim.x + threadIdx.x) * kC, in.cols); };
+  const uint32_t lane = kShared ? threadIdx.x % in.lanes : threadIdx.x;
+  const int64_t i = kShared ? blockIdx.x * (kSharedThreads / in.lanes) + threadIdx.x / in.lanes : blockIdx.x;
+  if (kShared && i >= in.rows) return;
+  auto span = [&](uint32_t b) { return Span<kC, kWhole>(uint64_t(b * blockDim.x + lane) * kC, in.cols); };
   Raw<T, kC, true> rx[kB], rr[kB], rw[kB];
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
@@ -96,14 +99,19 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<co
       if (k8) largest = max(largest, magnitude(y[b][e]));
     }
   }
-  row_reduce<k8 != kNone8>(&total, &largest);
+  if constexpr (kShared) {
+    total = lanes_sum(total, in.lanes);
+    if (k8) largest = lanes_max(largest, in.lanes);
+  } else {
+    row_reduce<k8 != kNone8>(&total, &largest);
+  }
   const float r = 1.0f / sqrtf(total * in.per_col + in.eps);
-  if (rstd && threadIdx.x == 0) rstd[i] = r;
+  if (rstd && lane == 0) rstd[i] = r;
   float factor = 0.0f;
   if (k8) {
     float scale;
     row_scale<k8 ? k8 : kInt8>(largest, r, &scale, &factor);
-    if (threadIdx.x == 0) out8.scale[i * out8.sld] = scale;
+    if (lane == 0) out8.scale[i * out8.sld] = scale;
   }
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
@@ -184,13 +192,17 @@ hipError_t launch(const etc_norm_args& a, hipStream_t stream) {
   // 58.9; a single row 3.6, 3.1 and 3.8.  Whatever the rows, so that a row has the same bits in any batch.
   const uint32_t per = blocks <= 64 ? 1 : blocks <= 2 * 64 * kMostWaves ? 2 : kMostBlocks;
   const uint32_t waves = std::min((blocks + 64 * per - 1) / (64 * per), kMostWaves);
-  const auto kernel = blocks > waves * 64 * per || a.x.cols < kLaneCols<T> ? norm_long_kernel<T, kWhole, k8>
-                      : per == 1                ? norm_kernel<T, 1, kWhole, k8>
-                      : per == 2                ? norm_kernel<T, 2, kWhole, k8>
-                                                : norm_kernel<T, kMostBlocks, kWhole, k8>;
-  const NormIn in{uint32_t(a.x.cols), float(a.eps), 1.0f / float(a.x.cols)};
-  return for_row_groups(a.x.rows, waves * 64, [&](int64_t first, uint32_t rows) -> hipError_t {
-    hipLaunchKernelGGL(kernel, dim3(rows), dim3(waves * 64), 0, stream, in, cmat<T>(a.x, first), cmat<T>(a.residual, first),
+  const uint32_t lanes = lanes_of_row(blocks);
+  const bool longer = blocks > waves * 64 * per || a.x.cols < kLaneCols<T>, shared = !longer && lanes <= 32;
+  const auto kernel = longer     ? norm_long_kernel<T, kWhole, k8>
+                      : shared   ? norm_kernel<T, 1, kWhole, k8, true>
+                      : per == 1 ? norm_kernel<T, 1, kWhole, k8, false>
+                      : per == 2 ? norm_kernel<T, 2, kWhole, k8, false>
+                                 : norm_kernel<T, kMostBlocks, kWhole, k8, false>;
+  const uint32_t threads = shared ? kSharedThreads : waves * 64, at_once = shared ? kSharedThreads / lanes : 1;
+  return for_row_groups(a.x.rows, threads, [&](int64_t first, uint32_t rows) -> hipError_t {
+    const NormIn in{rows, uint32_t(a.x.cols), lanes, float(a.eps), 1.0f / float(a.x.cols)};
+    hipLaunchKernelGGL(kernel, dim3((rows + at_once - 1) / at_once), dim3(threads), 0, stream, in, cmat<T>(a.x, first), cmat<T>(a.residual, first),
                        static_cast<const T*>(a.weight.data), mat<T>(a.sum, first), mat<T>(a.out, first),
                        mat8(a.out8, first), a.rstd ? a.rstd + first : nullptr);
     return hipGetLastError();

@@ -20,6 +20,7 @@ namespace {
 
 constexpr uint32_t kMostWaves = 16;
 constexpr uint32_t kMostBlocks = 2;
+constexpr uint32_t kCus = 256;
 constexpr uint32_t kAllWaves = 4096;  // wavefronts of a launch that sums
 // Rows of a workgroup at least: its sums take as much to write and read again as a row does.  2048 x 681
 // bf16, in us: 13.5 with one, 11.3 with two, 11.5 with four, 15.4 with eight; 8192 x 256: 18.5, 18.5, 13.7, 14.9.
@@ -28,16 +29,25 @@ constexpr uint32_t kRowsAPart = 4;
 struct Shape {
   uint32_t rows, cols;
   uint32_t per, waves, parts;  // blocks of a lane, wavefronts of a row, workgroups that sum
+  uint32_t lanes, joined;      // of a row within a wavefront, or 0: longer ones; wavefronts whose sums a workgroup joins
   bool longer;                 // than the registers of a workgroup, or less than a block
 };
 
 Shape shape_of(uint64_t rows, uint64_t cols, uint32_t block) {
   const uint64_t blocks = (cols + block - 1) / block;
-  Shape s{uint32_t(rows), uint32_t(cols), 0, 0, 0, false};
+  Shape s{uint32_t(rows), uint32_t(cols), 0, 0, 0, 0, 1, false};
   s.per = blocks <= 64 * kMostWaves ? 1 : kMostBlocks;
   s.waves = uint32_t(std::min<uint64_t>((blocks + 64 * s.per - 1) / (64 * s.per), kMostWaves));
   s.longer = blocks > uint64_t(s.waves) * 64 * s.per || cols < block;
-  s.parts = uint32_t(std::min<uint64_t>((rows + kRowsAPart - 1) / kRowsAPart, kAllWaves / s.waves));
+  uint64_t of_part = kRowsAPart;
+  if (!s.longer && blocks <= 64) {
+    s.lanes = lanes_of_row(uint32_t(blocks));
+    of_part *= 64 / s.lanes;
+    // as few sums as leave each CU a workgroup
+    s.joined = rows >= of_part * 16 * kCus ? 16 : rows >= of_part * 4 * kCus ? 4 : 1;
+    of_part *= s.joined;
+  }
+  s.parts = uint32_t(std::min<uint64_t>((rows + of_part - 1) / of_part, kAllWaves / (s.waves * s.joined)));
   return s;
 }
 
@@ -126,6 +136,7 @@ __device__ __forceinline__ void store_sums(float* p, uint32_t n, const float (&v
 struct In {
   uint32_t rows, cols;
   float per_col;  // 1 / cols
+  uint32_t lanes;  // of a row (kShared)
 };
 
 // Lane `lane` of the `lanes` that share a row: kB blocks of it, `lanes` blocks apart.
@@ -205,25 +216,46 @@ struct Row {
   }
 };
 
-template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kSum>
+// kShared: rows within a wavefront, which has as many at a time as it has runs of `lanes` lanes for; a workgroup's
+// wavefronts meet only at the end, to join their sums (FIGURES).
+template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kSum, bool kShared>
 __global__ __launch_bounds__(kMostWaves * 64) void norm_grad_kernel(In in, Mat<const T> grad, Mat<const T> x, Mat8 x8,
                                                                     const T* weight, Mat<const T> dsum, Mat<T> dx,
                                                                     const float* rstd, float* partial) {
   using R = Row<T, kB, kWhole, k8>;
   constexpr uint32_t kC = kLaneCols<T>;
-  const uint32_t lane = threadIdx.x, lanes = blockDim.x;
+  const uint32_t lanes = kShared ? in.lanes : blockDim.x, lane = kShared ? threadIdx.x % lanes : threadIdx.x;
+  const uint32_t at_once = kShared ? blockDim.x / lanes : 1, mine = kShared ? threadIdx.x / lanes : 0;
   typename R::Block w[kB];
   R::load_weight(in, lane, lanes, weight, w);
   float sums[kB][kC] = {};
   uint32_t turn = 0;
-  for (uint64_t row = blockIdx.x; row < in.rows; row += gridDim.x, turn = 1 - turn) {
+  for (uint64_t row = uint64_t(blockIdx.x) * at_once + mine; row < in.rows; row += uint64_t(gridDim.x) * at_once, turn = 1 - turn) {
     R now;
     now.load(in, int64_t(row), lane, lanes, grad, x, x8, dsum, rstd);
     compiler_fence();
     const float dot = now.template products<kSum>(in, lane, lanes, w, sums);
-    now.store(in, int64_t(row), lane, lanes, w, row_sum(dot, blockDim.x / 64, turn) * in.per_col, dx);
+    float all;
+    if constexpr (kShared) all = lanes_sum(dot, lanes);
+    else all = row_sum(dot, blockDim.x / 64, turn);
+    now.store(in, int64_t(row), lane, lanes, w, all * in.per_col, dx);
   }
   if (!kSum) return;
+  if constexpr (kShared) {  // over the wavefront's rows, then over the wavefronts
+    extern __shared__ __attribute__((aligned(16))) float joined[];
+#pragma unroll
+    for (uint32_t e = 0; e < kC; ++e)
+      for (uint32_t d = lanes; d < 64; d *= 2) sums[0][e] += __shfl_xor(sums[0][e], int(d));
+    if (blockDim.x > 64) {
+      if (threadIdx.x % 64 < lanes) store_sums<kC, true>(joined + (threadIdx.x / 64 * lanes + lane) * kC, kC, sums[0]);
+      __syncthreads();
+    }
+    if (mine) return;
+    for (uint32_t v = 1; v < blockDim.x / 64; ++v) {
+#pragma unroll
+      for (uint32_t e = 0; e < kC; ++e) sums[0][e] += joined[(v * lanes + lane) * kC + e];
+    }
+  }
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
     const auto p = R::span(in, b, lane, lanes);
@@ -403,17 +435,22 @@ __global__ __launch_bounds__(kJoinCols* kJoinRows) void dweight_kernel(const flo
 template <typename T, bool kWhole, Kind8 k8, bool kSum>
 hipError_t launch_rows(const etc_norm_grad_args& a, const Shape& s, hipStream_t stream) {
   const auto kernel = s.longer     ? norm_grad_long_kernel<T, kWhole, k8, kSum>
-                      : s.per == 1 ? norm_grad_kernel<T, 1, kWhole, k8, kSum>
-                                   : norm_grad_kernel<T, kMostBlocks, kWhole, k8, kSum>;
-  const uint32_t threads = s.waves * 64;
+                      : s.lanes    ? norm_grad_kernel<T, 1, kWhole, k8, kSum, true>
+                      : s.per == 1 ? norm_grad_kernel<T, 1, kWhole, k8, kSum, false>
+                                   : norm_grad_kernel<T, kMostBlocks, kWhole, k8, kSum, false>;
+  // without sums a wavefront has its rows and ends
+  const uint32_t joined = kSum ? s.joined : 1, at_once = s.lanes ? 64 / s.lanes : 1, threads = s.waves * joined * 64;
+  const uint32_t lds = joined > 1 ? joined * s.lanes * kLaneCols<T> * uint32_t(sizeof(float)) : 0;
   auto run = [&](int64_t first, uint32_t rows, uint32_t wgs) -> hipError_t {
-    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), 0, stream, In{rows, s.cols, 1.0f / float(s.cols)}, cmat<T>(a.grad, first),
+    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), lds, stream, In{rows, s.cols, 1.0f / float(s.cols), s.lanes}, cmat<T>(a.grad, first),
                        cmat<T>(a.x, first), mat8(a.x8, first), static_cast<const T*>(a.weight.data), cmat<T>(a.dsum, first),
                        mat<T>(a.dx, first), a.rstd + first, static_cast<float*>(a.workspace));
     return hipGetLastError();
   };
   if (kSum) return run(0, s.rows, s.parts);
-  return for_row_groups(a.grad.rows, threads, [&](int64_t first, uint32_t rows) { return run(first, rows, rows); });
+  return for_row_groups(a.grad.rows, threads, [&](int64_t first, uint32_t rows) {
+    return run(first, rows, (rows + at_once - 1) / at_once);
+  });
 }
 
 template <typename T, bool kWhole, Kind8 k8>
@@ -423,7 +460,8 @@ hipError_t launch_sum(const etc_norm_grad_args& a, hipStream_t stream) {
   // in place, rows are written while other workgroups would still sum their columns
   const bool in_place = a.dx.data == a.grad.data || a.dx.data == a.x.data;
   if (is_few(s) && !in_place) {
-    // blocks of a workgroup that sums columns: two where there are few workgroups and many rows
+    // blocks of a workgroup that sums columns: two where there are few workgroups and many rows, whose reads then come
+    // all at once (1021 x 681 fp32 in 8.5 us, four 9.3, one 11; 1024 x 2048 bf16 10.6, 11.7, 13.9)
     const uint32_t blocks = blocks_per_row(s.cols, kLaneCols<T>), narrow = s.rows > 512 && blocks <= 512 ? 2 : 4;
     const uint32_t slabs = (blocks + narrow - 1) / narrow;
     const uint32_t padded = (slabs + kXcds - 1) / kXcds * kXcds, groups = kFewThreads / 64 / s.waves;
@@ -431,7 +469,7 @@ hipError_t launch_sum(const etc_norm_grad_args& a, hipStream_t stream) {
                         : narrow == 2 ? norm_grad_few_kernel<T, 1, 2, kWhole, k8>
                                       : norm_grad_few_kernel<T, 1, 4, kWhole, k8>;
     hipLaunchKernelGGL(kernel, dim3(padded + (s.rows + groups - 1) / groups), dim3(kFewThreads), 0, stream,
-                       In{s.rows, s.cols, 1.0f / float(s.cols)}, padded, s.waves, cmat<T>(a.grad, 0), cmat<T>(a.x, 0), mat8(a.x8, 0),
+                       In{s.rows, s.cols, 1.0f / float(s.cols), 0}, padded, s.waves, cmat<T>(a.grad, 0), cmat<T>(a.x, 0), mat8(a.x8, 0),
                        static_cast<const T*>(a.weight.data), cmat<T>(a.dsum, 0), mat<T>(a.dx, 0), a.rstd,
                        static_cast<float*>(a.dweight.data), uint32_t(a.accumulate != 0));
     return hipGetLastError();

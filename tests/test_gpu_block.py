@@ -346,6 +346,54 @@ def test_read_rows_may_repeat():
     close(y, tuple(v.repeat(4, 0) for v in block_ref.norm(xn, wn[0], xn)["out"]), "norm")
 
 
+SHORT = [(rows, cols, dtype) for rows, cols, dtype in (
+    (1, 8, "bf16"), (3, 9, "bf16"), (257, 16, "bf16"), (1025, 100, "bf16"), (5003, 128, "bf16"), (1030, 255, "bf16"), (4099, 256, "bf16"),
+    (17000, 512, "bf16"), (17001, 257, "bf16"), (70001, 128, "bf16"), (70003, 121, "bf16"), (33000, 8, "bf16"), (2, 4, "f32"), (1027, 5, "f32"),
+    (5001, 128, "f32"), (4100, 256, "f32"), (17003, 129, "f32"), (70001, 63, "f32"))]
+
+
+@pytest.mark.parametrize("rows,cols,dtype", SHORT)
+def test_short_rows(rows, cols, dtype):
+    """Rows that share wavefronts, in counts on both sides of where workgroups join their sums; none reaches another."""
+    say("short rows", rows, cols, dtype)
+    rng = np.random.default_rng([rows, cols, 5])
+    x, xn, _ = rand(rng, rows, cols, dtype, more=3)
+    g, gn, _ = rand(rng, rows, cols, dtype, shift=1)
+    w, wn, _ = rand(rng, 1, cols, dtype)
+    out, ofull = blank(rows, cols, dtype, 3, 1)
+    m8, view, full8, scale, fs = blank8(rows, cols, "i8", 0, 3, 1)
+    rstd = torch.empty(rows, device=DEV)
+    etc.etc_norm(x, w[0], out=out, out8=m8, rstd=rstd, eps=1e-5)
+    want = block_ref.norm(xn, wn[0], None, 1e-5)
+    close(rstd, want["rstd"], "rstd")
+    close(out, want["out"], "out")
+    block_ref.check_norm8(view.cpu().numpy(), scale[:, 0].cpu().numpy().astype(np.float64), "i8", want["out"])
+    assert untouched(ofull, out) and marked(full8, view) and untouched(fs, scale)
+    etc.etc_store8(x, m8)
+    data, s = block_ref.store8(xn, "i8", 0)
+    assert np.array_equal(view.cpu().numpy(), data.view(np.uint8)) and np.array_equal(scale.cpu().numpy(), s)
+    assert marked(full8, view) and untouched(fs, scale)
+    r = (1 + rng.random(rows)).astype(np.float32)
+    at = torch.from_numpy(r).to(DEV)
+    for with_dweight in (True, False):
+        dx, full = blank(rows, cols, dtype, 1, 0)
+        dw, before, wfull = rand(rng, 1, cols, "f32")
+        ws, end = workspace(etc.etc_norm_grad_bytes(rows, cols))
+        etc.etc_norm_grad(g, x, w, at, dx, dweight=dw[0] if with_dweight else None, workspace=ws, accumulate=True)
+        want = block_ref.norm_grad(gn, xn, wn[0], r, None, before[0], True, False)
+        close(dx, want["dx"], "dx")
+        if with_dweight:
+            close(dw[0], want["dweight"], "dweight")
+        assert untouched(full, dx) and untouched(wfull, dw) and bool((end == 0xEE).all())
+    # a row that is not finite leaves the others as they were
+    if rows > 2:
+        x[1, cols // 2] = float("nan")
+        again, _ = blank(rows, cols, dtype)
+        etc.etc_norm(x, w[0], out=again, out8=m8, eps=1e-5)
+        assert bool(again[1].isnan().all()) and bool(scale[1].isnan().all()) and bool((view[1] == 0).all())
+        assert torch.equal(again[2:], out[2:]) and torch.equal(again[0], out[0]) and bool(scale[2:].isfinite().all())
+
+
 def ints(rng, rows, cols, lo=-127, hi=127):
     return rng.integers(lo, hi + 1, (rows, cols), dtype=np.int64).astype(np.int8)
 
