@@ -4,8 +4,8 @@
 //
 // HBM bound: x and residual are read once, s and y written once.  A row stays in
 // the registers of its workgroup between the pass that sums and the one that
-// multiplies.  The largest |s weight| is found beside the sum: r cancels out of
-// data = y (t / max |y|), so that 8 bits cost no second reduction.
+// multiplies.  The largest |s weight| is found beside the sum, and r times it is
+// the largest |y|, so that 8 bits cost no second reduction.
 // 8192 rows of 4096 bf16 with residual, sum and int8 output (235 MB): 39.1 us, 6.0 TB/s.
 // One row of 4096: 3.0 us, of which 2 are the launch; the rest is two waits, for memory and for the barrier.
 #include <hip/hip_runtime.h>
@@ -50,11 +50,12 @@ __device__ __forceinline__ void row_reduce(float* sum, uint32_t* largest) {
   *largest = top;
 }
 
-// From the largest |s weight|: the scale of y = s weight r, and what s weight is multiplied with.
+// From the largest |s weight|: the scale of y = s weight r, and what y is multiplied with.  Rounding keeps the
+// order of products with r, so that this is the largest |y|.  (r in the factor would save a product: with a small eps
+// it is infinite for a row of zeros.)
 template <Kind8 k>
 __device__ __forceinline__ void row_scale(uint32_t largest, float r, float* scale, float* factor) {
   scale_of<k>(magnitude(r * __uint_as_float(largest)), scale, factor);
-  *factor = *factor == 0.0f ? 0.0f : *factor * r;  // r may be NaN where the scale is
 }
 
 // A workgroup has a row, a lane kB blocks of it, one workgroup's width apart.  kShared: rows of half a wavefront or less, as
@@ -119,16 +120,14 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_kernel(NormIn in, Mat<co
     const auto p = span(b);
     if (!p.in) continue;
     if (sum.p) store_block<true, true>(sum.p + i * sum.ld + p.at, kC, s[b]);
+#pragma unroll
+    for (uint32_t e = 0; e < kC; ++e) y[b][e] *= r;
     if (k8) {
       Raw8<kC, true> q;
       q.template narrow<k8 ? k8 : kInt8>(y[b], factor);
       q.template store<true>(out8.p + i * out8.ld + p.at, kC);
     }
-    if (out.p) {
-#pragma unroll
-      for (uint32_t e = 0; e < kC; ++e) y[b][e] *= r;
-      store_block<true, true>(out.p + i * out.ld + p.at, kC, y[b]);
-    }
+    if (out.p) store_block<true, true>(out.p + i * out.ld + p.at, kC, y[b]);
   }
 }
 
@@ -163,16 +162,14 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_long_kernel(NormIn in, M
       }
       if (pass == 0) continue;
       if (sum.p) store_block<kWhole>(sum.p + i * sum.ld + col, width, s);
+#pragma unroll
+      for (uint32_t e = 0; e < kC; ++e) w[e] *= r;
       if (k8) {
         Raw8<kC, kWhole> q;
         q.template narrow<k8 ? k8 : kInt8>(w, factor);
         q.store(out8.p + i * out8.ld + col, width);
       }
-      if (out.p) {
-#pragma unroll
-        for (uint32_t e = 0; e < kC; ++e) w[e] *= r;
-        store_block<kWhole>(out.p + i * out.ld + col, width, w);
-      }
+      if (out.p) store_block<kWhole>(out.p + i * out.ld + col, width, w);
     }
     if (pass) break;
     row_reduce<k8 != kNone8>(&total, &largest);
