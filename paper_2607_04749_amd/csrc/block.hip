@@ -47,6 +47,12 @@ bool crosses(const etc_matrix& out, const etc_matrix& in) {
   return out.data && out.data == in.data && in.rows > 1 && in.cols && out.ld != in.ld;
 }
 
+// Without elements no pointer tells that 8-bit data are given: they are what has their type and grad's sizes.
+bool kept_without_elements(const etc_matrix8& m, const etc_matrix& grad) {
+  return (grad.rows == 0 || grad.cols == 0) && (m.dtype == ETC_DTYPE_I8 || m.dtype == ETC_DTYPE_E4M3) && m.rows == grad.rows &&
+         m.cols == grad.cols;
+}
+
 // fp32 numbers, `n` of them (none: no pointer is needed)
 int check_numbers(const void* p, const char* what, int64_t n, bool needed) {
   if (n == 0 || (!p && !needed)) return ETC_OK;
@@ -96,8 +102,8 @@ int etc_norm_grad(const etc_norm_grad_args* a, void* stream) {
   if ((rc = check_matrix(a->grad, "grad", kIn)) || (rc = check_like(a->dx, "dx", kOut, a->grad))) return rc;
   if (a->grad.cols && (rc = check_row(a->weight, "weight", kIn, a->grad.cols, a->grad.dtype))) return rc;
   if (a->x.data && a->x8.data) return fail(ETC_ERR_INVALID_ARG, "x and x8 are both given");
-  if (a->x8.data && (rc = check_like8(a->x8, "x8", kIn, a->grad))) return rc;
-  if (!a->x8.data && (rc = check_like(a->x, "x", kIn, a->grad))) return rc;
+  const bool kept = a->x8.data || (!a->x.data && kept_without_elements(a->x8, a->grad));
+  if ((rc = kept ? check_like8(a->x8, "x8", kIn, a->grad) : check_like(a->x, "x", kIn, a->grad))) return rc;
   if (a->dsum.data && (rc = check_like(a->dsum, "dsum", kIn, a->grad))) return rc;
   if ((rc = check_numbers(a->rstd, "rstd", a->grad.rows, a->grad.cols != 0))) return rc;
   if (crosses(a->dx, a->grad) || crosses(a->dx, a->x) || crosses(a->dx, a->dsum))

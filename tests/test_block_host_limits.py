@@ -1,0 +1,28 @@
+"""The operators around a block's projections at the ends of what they take, without
+a GPU."""
+import pytest
+
+from paper_2607_04749_amd import etc
+from test_block_host import E4M3, I8, mat8, norm_grad
+from test_ops_host import F32, INVALID, NONE, OK, mat
+
+
+@pytest.mark.parametrize("dtype", (I8, E4M3))
+@pytest.mark.parametrize("group", (0, 32))
+def test_kept_activations_of_no_elements(dtype, group):
+    """The backward of a batch without tokens: no work, whether its input was kept in 8 bits or not.  What is given
+    has to fit all the same."""
+    for t in (etc.DTYPE_BF16, F32):
+        e, e8 = mat(0, 16, t, ptr=0), mat8(0, 16, dtype, group, ptr=0, scale=0)
+        w = mat(1, 16, t)
+        assert norm_grad(grad=e, x=NONE, x8=e8, dx=e, weight=w, rstd=0) == OK, etc.last_error()
+        assert norm_grad(grad=e, x=NONE, x8=e8, dx=e, weight=w, rstd=0, dweight=mat(1, 16, F32), accumulate=1) == OK
+        assert norm_grad(grad=e, x=NONE, x8=mat8(0, 8, dtype, group, ptr=0, scale=0), dx=e, weight=w, rstd=0) == INVALID
+        assert norm_grad(grad=e, x=NONE, x8=mat8(3, 16, dtype, group, ptr=0, scale=0), dx=e, weight=w, rstd=0) == INVALID
+        assert norm_grad(grad=e, x=NONE, x8=mat8(0, 16, dtype, 16, ptr=0, scale=0), dx=e, weight=w, rstd=0) == INVALID
+        assert norm_grad(grad=e, x=NONE, dx=e, weight=w, rstd=0) == INVALID
+        for rows in (0, 3):
+            none, none8 = mat(rows, 0, t, ptr=0), mat8(rows, 0, dtype, group, ptr=0, scale=0)
+            assert norm_grad(grad=none, x=NONE, x8=none8, dx=none, weight=NONE, rstd=0) == OK
+            assert norm_grad(grad=none, x=none, dx=none, weight=NONE, rstd=0) == OK
+    assert norm_grad(x=NONE, x8=mat8(3, 16, dtype, group, ptr=0)) == INVALID
