@@ -608,7 +608,8 @@ ETC_API int etc_adam(const etc_adam_args* args, void* stream);
  * in 8 bits, kept for the backward pass or taken by a product of 8-bit
  * integers; and the rotary positions behind it.  What is said of the operators
  * above holds here too: contiguous rows, sums in 32 bits in an order that the
- * arguments' sizes decide, no atomics, a call without work returns ETC_OK, the same errors.
+ * arguments' sizes and types decide (and, for etc_norm_grad's dweight, whether dx is grad
+ * or x itself), no atomics, a call without work returns ETC_OK, the same errors.
  * A row's norm, its 8 bits, its product and its rotation have the same
  * bits whatever other rows the call has. */
 
@@ -660,7 +661,9 @@ ETC_API int etc_norm(const etc_norm_args* args, void* stream);
  * that reaches the sum past the norm.  x is given as a matrix of grad's type,
  * or, with x.data NULL, as x8: as etc_store8 kept it.  grad, weight, dsum and dx are
  * of one type; dweight (ETC_DTYPE_F32, one row) may be absent.  dx may be grad,
- * x or dsum itself (same data and ld).  workspace: etc_norm_grad_workspace's bytes; only read or
+ * x or dsum itself (same data and ld).  Where dx is grad or x, dweight's sums may have another
+ * order, and so other last bits, than where it is neither; either way they repeat.
+ * workspace: etc_norm_grad_workspace's bytes; only read or
  * written with dweight, and may be NULL without. */
 typedef struct {
   etc_matrix grad, x;

@@ -458,7 +458,9 @@ template <typename T, bool kWhole, Kind8 k8>
 hipError_t launch_sum(const etc_norm_grad_args& a, hipStream_t stream) {
   const Shape s = shape_of(uint64_t(a.grad.rows), uint64_t(a.grad.cols), kLaneCols<T>);
   if (!a.dweight.data) return launch_rows<T, kWhole, k8, false>(a, s, stream);
-  // in place, rows are written while other workgroups would still sum their columns
+  // In place, rows are written while other workgroups would still sum their columns.  (One launch for the columns and
+  // one for the rows behind it would give dweight the same bits either way; in us, with that and with sums by rows: 1024 rows
+  // of 2048 bf16 12.6, 9.5; of 4096 fp32 24.6, 17.5; 64 of 4096 bf16 6.5, 8.1.)
   const bool in_place = a.dx.data == a.grad.data || a.dx.data == a.x.data;
   if (is_few(s) && !in_place) {
     // blocks of a workgroup that sums columns: two where there are few workgroups and many rows, whose reads then come

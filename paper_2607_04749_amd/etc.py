@@ -847,7 +847,8 @@ def etc_norm_grad(grad, x, weight, rstd, dx, dsum=None, dweight=None, workspace=
     """The norm's backward: dx = dsum + r (dn - n mean(dn n)) with n = x r, dn =
     grad * weight; dweight (float32) = or += the sum over rows of grad * n.  x:
     the norm's input (its sum, with a residual), or the Matrix8 that it was kept
-    in; rstd: etc_norm's; dx may be grad, x or dsum itself."""
+    in; rstd: etc_norm's; dx may be grad, x or dsum itself (if grad or x, dweight's
+    sums may have another order than if not)."""
     d = _device_of(dx, "dx")
     g = _matrix(grad, "grad", d)
     empty = not g[0]
