@@ -927,6 +927,11 @@ class Rotary:
         self._desc.scale = scale
         self._at = ctypes.addressof(self._desc)
 
+    def __setstate__(self, state):
+        """A copy, or what is read from a file, hands over its own memory."""
+        self.__dict__.update(state)
+        self._at = ctypes.addressof(self._desc)
+
     @property
     def freq(self):
         """Radians a position of each pair."""

@@ -1,5 +1,9 @@
 """The operators around a block's projections at the ends of what they take, without
 a GPU."""
+import copy
+import ctypes
+import pickle
+
 import pytest
 
 from paper_2607_04749_amd import etc
@@ -26,3 +30,17 @@ def test_kept_activations_of_no_elements(dtype, group):
             assert norm_grad(grad=none, x=NONE, x8=none8, dx=none, weight=NONE, rstd=0) == OK
             assert norm_grad(grad=none, x=none, dx=none, weight=NONE, rstd=0) == OK
     assert norm_grad(x=NONE, x8=mat8(3, 16, dtype, group, ptr=0)) == INVALID
+
+
+@pytest.mark.parametrize("how", (copy.copy, copy.deepcopy, lambda r: pickle.loads(pickle.dumps(r))), ids=("copy", "deepcopy", "pickle"))
+def test_copies_of_a_rotary(how):
+    """A copied model's Rotary reads memory that it holds, not the original's, which may be gone."""
+    first = etc.Rotary(64, scaling="linear", factor=4.0, layout="interleaved", scale=0.5)
+    freq, r = first.freq, how(first)
+    assert r._at == ctypes.addressof(r._desc) and r.freq == freq
+    d = etc.RotaryDesc.from_address(r._at)
+    assert (list(d.freq[:32]), d.scale, d.pairs, d.layout) == (freq, 0.5, 32, etc.ROTARY_INTERLEAVED)
+    if how is not copy.copy:
+        assert r._at != first._at
+        first._desc.freq[0] = 7.0
+        assert r.freq == freq
