@@ -730,7 +730,8 @@ typedef struct {
  *   PARTS   a pair that turns k = length freq[j] / 2 pi times in the context of
  *           training: kept from k = high on, divided by factor up to k = low, and
  *           between them freq[j] * (u + (1 - u) / factor), u = (k - low) / (high - low).
- * dim is even, 2 .. 2 ETC_ROTARY_PAIRS (BASE: from 4 on); base, factor, length > 0, high > low. */
+ * dim is even, 2 .. 2 ETC_ROTARY_PAIRS (BASE: from 4 on); base (BASE: the one in its place
+ * too), factor and length are positive and finite, and so is high - low. */
 enum { ETC_ROTARY_NONE = 0, ETC_ROTARY_LINEAR = 1, ETC_ROTARY_BASE = 2, ETC_ROTARY_PARTS = 3 };
 ETC_API int etc_rotary_init(etc_rotary_desc* out, int32_t dim, int32_t layout, double base, int32_t scaling,
                             double factor, double length, double low, double high);

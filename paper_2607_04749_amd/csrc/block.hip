@@ -167,10 +167,12 @@ int etc_rotary_init(etc_rotary_desc* out, int32_t dim, int32_t layout, double ba
   if (scaling == ETC_ROTARY_BASE) {
     if (dim < 4) return fail(ETC_ERR_INVALID_ARG, "ETC_ROTARY_BASE needs dim 4 or more");
     base *= std::pow(factor, double(dim) / (dim - 2));
+    // past 64 bits all pairs but the fastest would stand still
+    if (!std::isfinite(base)) return fail(ETC_ERR_INVALID_ARG, "base * factor^(dim / (dim - 2)) is infinite");
   }
   if (scaling == ETC_ROTARY_PARTS &&
-      (!(length > 0.0) || !(high > low) || !std::isfinite(length) || !std::isfinite(low) || !std::isfinite(high)))
-    return fail(ETC_ERR_INVALID_ARG, "length must be positive, and high above low");
+      (!(length > 0.0) || !(high > low) || !std::isfinite(length) || !std::isfinite(high - low)))
+    return fail(ETC_ERR_INVALID_ARG, "length must be positive, and high above low by a finite difference");
   etc_rotary_desc d = {};
   for (int32_t j = 0; j < dim / 2; ++j) {
     double f = std::pow(base, -2.0 * j / dim);

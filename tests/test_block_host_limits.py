@@ -44,3 +44,15 @@ def test_copies_of_a_rotary(how):
         assert r._at != first._at
         first._desc.freq[0] = 7.0
         assert r.freq == freq
+
+
+@pytest.mark.parametrize("kw", (dict(dim=4, factor=1e160), dict(dim=128, base=1e300, factor=1e9)))
+def test_a_base_past_64_bits_is_refused(kw):
+    with pytest.raises(etc.EtcError, match="infinite"):
+        etc.Rotary(scaling="base", **kw)
+
+
+@pytest.mark.parametrize("kw", (dict(low=-1e308, high=1e308), dict(low=float("-inf"), high=1.0), dict(low=1.0, high=float("inf"))))
+def test_a_ramp_past_64_bits_is_refused(kw):
+    with pytest.raises(etc.EtcError, match="difference"):
+        etc.Rotary(8, scaling="parts", factor=8.0, length=4096.0, **kw)
