@@ -916,8 +916,11 @@ class Rotary:
             raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}, not {layout!r}")
         if scaling not in _SCALINGS:
             raise ValueError(f"scaling must be None, 'linear', 'base' or 'parts', not {scaling!r}")
+        dim = index(dim)
+        if dim >= 1 << 31 or dim < 0:  # which the call would take modulo 2^32
+            raise ValueError(f"dim must be even, 2 .. {2 * ROTARY_PAIRS}, not {dim}")
         self._desc = RotaryDesc()
-        _check(_lib.etc_rotary_init(ctypes.byref(self._desc), index(dim), _LAYOUTS[layout], base, _SCALINGS[scaling],
+        _check(_lib.etc_rotary_init(ctypes.byref(self._desc), dim, _LAYOUTS[layout], base, _SCALINGS[scaling],
                                     factor, length, low, high), "etc_rotary_init")
         if freq is not None:
             if len(freq) != self._desc.pairs:

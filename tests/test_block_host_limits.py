@@ -56,3 +56,9 @@ def test_a_base_past_64_bits_is_refused(kw):
 def test_a_ramp_past_64_bits_is_refused(kw):
     with pytest.raises(etc.EtcError, match="difference"):
         etc.Rotary(8, scaling="parts", factor=8.0, length=4096.0, **kw)
+
+
+@pytest.mark.parametrize("dim", ((1 << 32) + 64, (1 << 64) + 2, 64 - (1 << 32), 1 << 31, -2))
+def test_a_dim_past_32_bits_is_refused(dim):
+    with pytest.raises(ValueError, match="dim"):
+        etc.Rotary(dim)
