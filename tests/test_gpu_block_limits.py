@@ -58,3 +58,43 @@ def test_order_of_the_weight_gradients_sums(rows, cols, dtype):
             assert torch.equal(dw, then), (to, accumulate)
             for name, now, then in (("grad", g, grad), ("x", h, x), ("dsum", d, dsum)):
                 assert name == to or torch.equal(now, then), (to, name)
+
+
+@pytest.mark.parametrize("m,n", (((1 << 19) + 5, 9), (3, (1 << 20) + 3)))
+def test_products_of_several_launches(m, n):
+    """More rows, or columns, than a launch takes: the next one's operands, scales and bias follow on.  Whole numbers and powers
+    of two: exact."""
+    say("matmul8 in several launches", m, n)
+    gen = torch.Generator(device=DEV).manual_seed(m)
+    x, w = (torch.randint(-127, 128, (r, 33), generator=gen, device=DEV, dtype=torch.int8) for r in (m, n))
+    sx, sw = (torch.exp2(torch.randint(-2, 3, (r,), generator=gen, device=DEV).float()) for r in (m, n))
+    bias = torch.randint(-9, 10, (n,), generator=gen, device=DEV).float()
+    out = torch.full((m + 1, n), 7.0, device=DEV)
+    etc.etc_matmul8(etc.Matrix8(x, sx), etc.Matrix8(w, sw), out[:m], bias=bias)
+    want = (x.double() @ w.double().t().contiguous()) * sx.double()[:, None] * sw.double() + bias.double()
+    assert torch.equal(out[:m].double(), want) and bool((out[m] == 7).all())
+
+
+def test_norms_of_several_launches():
+    """Rows past the 2^32 lanes of a launch.  A row's elements are 2^e or -2^e, so its rms is 2^e, and every result is exact."""
+    rows = (1 << 26) + 3
+    say("norm in several launches", rows)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    sign = torch.randint(0, 2, (rows, 8), generator=gen, device=DEV, dtype=torch.int8) * 2 - 1
+    e = torch.arange(rows, device=DEV) % 5
+    x = (sign * torch.exp2(e.float()).to(torch.bfloat16)[:, None])
+    w, r = torch.ones(8, dtype=torch.bfloat16, device=DEV), torch.empty(rows, device=DEV)
+    m8, out = etc.Matrix8(torch.empty_like(sign), torch.empty(rows, device=DEV)), torch.empty_like(x)
+    etc.etc_norm(x, w, out=out, out8=m8, rstd=r, eps=2.0 ** -40)
+    assert torch.equal(r, torch.exp2(-e.float())) and torch.equal(out, sign.to(torch.bfloat16))
+    assert torch.equal(m8.data, sign * 127) and bool((m8.scale == torch.tensor(1.0, device=DEV) / 127).all())
+    etc.etc_store8(x, m8)
+    assert torch.equal(m8.data, sign * 127) and torch.equal(m8.scale, torch.exp2(e.float()) / 127)
+    del m8
+    grad = torch.randint(-3, 4, (rows, 8), generator=gen, device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    etc.etc_norm_grad(grad, x, w, r, out)
+    for at in range(0, rows, 1 << 24):
+        part = slice(at, min(rows, at + (1 << 24)))
+        g, n = grad[part].float(), sign[part].float()
+        want = (g - n * (g * n).mean(1, keepdim=True)) * r[part, None]
+        assert torch.equal(out[part].float(), want), at
