@@ -107,7 +107,7 @@ constexpr uint32_t kAhead = kG == 1 ? 4 : kG == 2 ? 3 : 2;
 template <uint32_t kG>
 constexpr uint32_t kStage = (2 + kG) * 1024;  // bytes: 16 rows of w, 8 kG of x
 template <uint32_t kG>
-constexpr uint32_t kFewWaves = kG == 1 ? 6 : kG < 6 ? 16 : kG < 12 ? 8 : 4;  // at most
+constexpr uint32_t kFewWaves = kG == 1 ? 6 : kG < 6 ? 16 : 8;  // at most
 
 template <uint32_t kG, bool kDirect>
 __global__ __launch_bounds__(kFewWaves<kG> * 64) void matmul8_few_kernel(Product p, uint32_t wide, uint32_t across) {

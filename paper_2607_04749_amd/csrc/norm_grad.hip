@@ -115,21 +115,15 @@ struct Input {  // a block of x
 // 256 of 681 5.3, 8.3; 512 of 8192 13.5, 16.8; 1024 of 2048 10.7, 11.3.
 bool is_few(const Shape& s) { return s.rows && !s.longer && s.rows <= 1024 && (s.per == 1 || s.rows <= 128); }
 
-// n of kC fp32 sums
-template <uint32_t kC, bool kWhole>
-__device__ __forceinline__ void store_sums(float* p, uint32_t n, const float (&v)[kC]) {
+// kC fp32 sums
+template <uint32_t kC>
+__device__ __forceinline__ void store_sums(float* p, const float (&v)[kC]) {
 #pragma unroll
   for (uint32_t e = 0; e < kC; e += 4) {
-    if (kWhole || e + 4 <= n) {
-      uint32_t w[4];
+    uint32_t w[4];
 #pragma unroll
-      for (uint32_t k = 0; k < 4; ++k) w[k] = __float_as_uint(v[e + k]);
-      Words<float>::store4<false>(p + e, w);
-    } else {
-#pragma unroll
-      for (uint32_t k = 0; k < 4; ++k)
-        if (e + k < n) p[e + k] = v[e + k];
-    }
+    for (uint32_t k = 0; k < 4; ++k) w[k] = __float_as_uint(v[e + k]);
+    Words<float>::store4<false>(p + e, w);
   }
 }
 
@@ -248,7 +242,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_grad_kernel(In in, Mat<c
     for (uint32_t e = 0; e < kC; ++e)
       for (uint32_t d = lanes; d < 64; d *= 2) sums[0][e] += __shfl_xor(sums[0][e], int(d));
     if (blockDim.x > 64) {
-      if (threadIdx.x % 64 < lanes) store_sums<kC, true>(joined + (threadIdx.x / 64 * lanes + lane) * kC, kC, sums[0]);
+      if (threadIdx.x % 64 < lanes) store_sums(joined + (threadIdx.x / 64 * lanes + lane) * kC, sums[0]);
       __syncthreads();
     }
     if (mine) return;
@@ -260,7 +254,7 @@ __global__ __launch_bounds__(kMostWaves * 64) void norm_grad_kernel(In in, Mat<c
 #pragma unroll
   for (uint32_t b = 0; b < kB; ++b) {
     const auto p = R::span(in, b, lane, lanes);
-    if (p.in) store_sums<kC, true>(partial + uint64_t(blockIdx.x) * in.cols + p.at, kC, sums[b]);
+    if (p.in) store_sums(partial + uint64_t(blockIdx.x) * in.cols + p.at, sums[b]);
   }
 }
 
