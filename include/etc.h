@@ -625,9 +625,10 @@ enum { ETC_DTYPE_I8 = 2, ETC_DTYPE_E4M3 = 3 };
  * What the calls below write: with a the largest magnitude of the scale's
  * elements, at least 2^-100, and t = 127 or 448,
  *   scale = a / t,  data = x * (t / a), to nearest, ties to even,
- * in 32 bits.  Where x holds an infinity or NaN the scale is NaN and the data
- * are 0, so that all its elements read as NaN.  ld >= cols and scale_ld >= the
- * number of scales in a row for what is written; what is read may repeat rows. */
+ * in 32 bits (int8: the product itself is rounded once, to the whole number).
+ * Where x holds an infinity or NaN the scale is NaN and the data are 0, so that
+ * all its elements read as NaN.  ld >= cols and scale_ld >= the number of scales
+ * in a row for what is written; what is read may repeat rows. */
 typedef struct {
   void* data;
   float* scale;
@@ -641,9 +642,10 @@ typedef struct {
  *   y = s * r[i] * weight[j];
  * sum = s, out = y, out8 = y in 8 bits (group 0), rstd[i] = r[i], each where
  * given; out or out8 (or both) has to be.  x, residual, weight (one row), sum
- * and out are of one type; y is worked out from s before its rounding.  sum and
+ * and out are of one type; y is worked out from s before its rounding, as (s * weight) * r in
+ * 32 bits, which out and out8 are rounded from.  sum and
  * out may be x or residual itself (same data and ld), not both the same one.
- * Squares have to fit 32 bits: a row whose sum of them is infinite has r = 0.
+ * Squares and s * weight have to fit 32 bits: a row whose sum of squares is infinite has r = 0.
  * Matrices of no columns have nothing written. */
 typedef struct {
   etc_matrix x, residual, weight, sum, out;

@@ -7,9 +7,11 @@
 //
 // Three kernels: few rows (1 x 12288 x 4096: 10.3 us, 4.9 TB/s of weights, where a kernel that only reads
 // them takes 8.9), tiles whose sums are split over wavefronts (512 x 4096 x 4096: 18.6 us) and tiles of
-// quarters (8192 x 22016 x 4096: 664 to 740 us with the card, 2.0 to 2.2 POP/s).  The first waits for HBM, the middle one for
-// what its CUs read into their LDS, the last for power: its matrix pipes are busy for 54 % of
-// the cycles at a clock that falls to 1.9 GHz, and operands of zeros take a quarter less time (4096 x 4096 x 16384).
+// quarters (8192 x 22016 x 4096: 664 to 750 us with the card, 2.0 to 2.2 POP/s).  The first waits for HBM, the middle one for
+// what its CUs read into their LDS.  The last has two bounds.  Power holds the clock at 1.6 to 1.9 GHz: operands of zeros take as
+// many cycles at 2.3 (4096 x 4096 x 16384: 178 us, 230 with random ones).  And its matrix pipes are busy for 54 % of the cycles (64 %
+// there): in 7 % of them a CU has no wavefront (9 %), wavefronts wait for loads, LDS and barriers in 13 % of their time (10 %), and
+// a wavefront to a SIMD leaves nobody to fill the pipe while it issues what stands between matrix instructions.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -267,6 +269,7 @@ __global__ __launch_bounds__(256, kF == 4 || kCopies == 4 ? 1 : 2) void matmul8_
     offset[0][i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.xld) + chunks[i % 2];
     offset[1][i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.wld) + chunks[i % 2];
   }
+  // (kF = 2 by way of registers spills 27 of its 256, 112 bytes a lane)
   constexpr uint32_t kSets = kDirect || kF == 4 ? 1 : 2;
   constexpr uint32_t kFar = kDirect ? kCopies - 1 : kSets;  // stages between one that starts and the one that is multiplied
   Raw8<16, false> staged[kSets][2][kLoads];
@@ -627,7 +630,8 @@ hipError_t launch_few_groups(const Product& p, uint32_t groups, bool direct, hip
   return launch_few<10>(p, wide, direct, stream);
 }
 
-// What a CU reads into its LDS, some 32 bytes a clock whichever kernel it is, decides: the
+// What a CU reads into its LDS decides in most sizes.  Over a workgroup's life, start and end included, that is 29 bytes a
+// clock (772 x 2048 x 11008), 28 (300 x 1280 x 8192), 23 (67 x 1280 x 8192), 21 to 22 (128 and 512 x 4096 x 4096): the
 // kernel is the one whose workgroups together read the fewest rows to a CU, and among
 // equals the one of the smallest tiles.  In us, with the kernel that it takes and with the one of
 // the next larger tiles: 200 x 4096 x 4096 11.3 (64 x 64), 12.4; 96 x 11008 x 4096 19.6 (96 x 64), 20.0.
